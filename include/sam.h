@@ -483,6 +483,125 @@ int sam_set_argmax_variant(int32_t variant);
 int32_t sam_profile_count(void);
 int sam_profile_read(int32_t call, float* argmax_ms, float* accept_ms);
 
+/* ---------------------------------------------------------------- paged key/value cache in 4 bits */
+
+/* The target model's context, next to the draft and verify calls above: keys and values of many long agent
+ * sessions, held in 4 bits in pages that sessions share.  A step reserves pages for the K+1 proposed rows, appends
+ * their keys and values layer by layer, attends, and - once sam_step has said how many were accepted - commits that
+ * many; what was proposed and rejected is overwritten by the next step and its pages go back to the pool.
+ *
+ * Format.  16 neighbouring channels of one token and key/value head share a scale:
+ *     value = code * scale * 2^exp         code: e2m1 (0, .5, 1, 1.5, 2, 3, 4, 6 and a sign), scale: e4m3,
+ *     scale = e4m3(min(amax / (6 * 2^exp), 448)),  code = e2m1(x / (scale * 2^exp)), both to nearest, ties to even,
+ * exp = k_exp for all keys, v_exp for all values of the cache.  A scale of zero stands for sixteen zeros; a block with
+ * a NaN reads back as NaN (scale 0x7f); an infinity is stored as the largest value, 6 * 448 * 2^exp.  A value has six
+ * significant bits, so it is exact in bf16, and in fp16 before 2^exp is applied.
+ * A tile holds 16 tokens of one head in 18 * head_dim bytes: key codes [16][head_dim/2], value codes
+ * [16][head_dim/2], key scales [16][head_dim/16], value scales [16][head_dim/16]; the low nibble of a byte is the
+ * even channel.  A page holds the tiles [n_layers][n_kv_heads][page_tokens/16] of page_tokens consecutive tokens of
+ * one stream: all layers of a page are one contiguous piece.
+ *
+ * Bookkeeping lives on the device; no call here synchronises or reads it on the host (except sam_cache_status).
+ * Page p is free when ref_count[p] == 0; free_list[0 .. n_free) holds the free pages, taken from its end.  Which
+ * page a call hands out does not depend on timing.  All device pointers belong to the caller; the struct itself is
+ * host memory, read during the call only. */
+typedef struct sam_cache {
+    void*    pages;        /* device, n_pages * sam_cache_page_bytes(), 128-byte aligned; contents need no initialisation */
+    int32_t* page_table;   /* device [n_streams, max_pages]; -1 = no page */
+    int32_t* seq_len;      /* device [n_streams]; committed tokens */
+    int32_t* ref_count;    /* device [n_pages]; streams that hold the page */
+    int32_t* free_list;    /* device [n_pages] */
+    int32_t* meta;         /* device [4]: n_free, status bits (SAM_CACHE_*), two unused */
+    void*    scratch;      /* device, sam_cache_scratch_bytes(), 16-byte aligned; contents undefined between calls */
+    int64_t  scratch_bytes;
+    int32_t  n_pages, page_tokens, n_streams, max_pages, n_layers, n_kv_heads, head_dim;
+    int32_t  k_exp, v_exp; /* -24 .. 24 */
+} sam_cache;
+
+#define SAM_CACHE_OUT_OF_PAGES  1   /* a sam_cache_reserve found too few free pages and reserved none */
+#define SAM_CACHE_TABLE_FULL    2   /* a sam_cache_reserve would have needed more than max_pages pages for a stream, and reserved none */
+#define SAM_CACHE_BAD_FORK      4   /* a sam_cache_fork pair named a destination that holds tokens, or an unknown stream */
+
+#define SAM_CACHE_BF16  0           /* element types of queries, keys, values and outputs */
+#define SAM_CACHE_FP16  1
+
+#define SAM_CACHE_MAX_B 4096        /* rows of one call */
+
+/* Sizes.  page_tokens: a power of two, 16 .. 1024; head_dim: 64 or 128; page_tokens * max_pages < 2^31.
+ * Negative SAM_ERR_* on bad sizes. */
+int64_t sam_cache_page_bytes(int32_t page_tokens, int32_t n_layers, int32_t n_kv_heads, int32_t head_dim);
+int64_t sam_cache_scratch_bytes(int32_t n_streams, int32_t n_pages);
+
+/* Empties the cache: no stream holds a page, all pages are free (page 0 is handed out first), status 0. */
+int sam_cache_init(const sam_cache* c, void* cuda_stream);
+
+/* n_free and the status bits gathered since the last sam_cache_init.  Copies 8 bytes to the host and synchronises the
+ * stream: a diagnostic.  Either output may be NULL. */
+int sam_cache_status(const sam_cache* c, int32_t* n_free, int32_t* status, void* cuda_stream);
+
+/* In the calls below `streams` (device [B], distinct ids in [0, n_streams)) names the stream of each of the B rows;
+ * NULL means row b is stream b.  Ids out of range are left alone.  0 <= B <= SAM_CACHE_MAX_B; B = 0 is a no-op.
+ *
+ * Reserve: makes room for n_new[b] tokens (device [B]; <= 0: none) behind seq_len.  Pages that the table lacks are
+ * taken from the free list in order of rows, then of positions.  If the page of the first new token already holds
+ * tokens and other streams hold it too, the stream gets a copy of it (all layers) in its place - except that the last
+ * of the rows that write to such a page keeps it when every holder of the page is among them.  All or nothing: with
+ * too few free pages or too short a table nothing changes but the status bits. */
+int sam_cache_reserve(const sam_cache* c, int32_t B, const int32_t* streams, const int32_t* n_new, void* cuda_stream);
+
+/* Commit: seq_len += n_keep[b], which may be negative (roll back; -2^31 empties the stream), clamped to
+ * 0 .. page_tokens * max_pages.  The pages behind the new length, up to the table's first -1, are given up; those that
+ * nobody holds any more go onto the free list, in order of rows, then of positions (of their first mention). */
+int sam_cache_commit(const sam_cache* c, int32_t B, const int32_t* streams, const int32_t* n_keep, void* cuda_stream);
+
+/* Fork: stream dst[i] becomes a second holder of the committed pages of stream src[i], for i < n (device arrays; a
+ * dst appears once and is not a src of the same call).  dst must hold no tokens and no pages, else the pair is left
+ * out and SAM_CACHE_BAD_FORK is set.  Nothing is copied until one of the two writes (sam_cache_reserve). */
+int sam_cache_fork(const sam_cache* c, int32_t n, const int32_t* src, const int32_t* dst, void* cuda_stream);
+
+/* Compact: with L live pages, the live pages with ids >= L move to the free ids below L (lowest to lowest), tables
+ * and counts follow, and the free list hands out L, L+1, ... next.  The pages behind L can then be given back. */
+int sam_cache_compact(const sam_cache* c, void* cuda_stream);
+
+/* Copies whole pages: page from[i] of `src` onto page to[i] of `dst` (device arrays [n]; the same geometry, the same or
+ * another pool: swapping out, swapping in).  Pairs with an id out of range are left out; no page is a target twice or
+ * both source and target.  Tables, counts and free lists are the caller's to keep. */
+int sam_cache_copy_pages(const sam_cache* src, const sam_cache* dst, int32_t n, const int32_t* from, const int32_t* to,
+                         void* cuda_stream);
+
+/* Append: quantises keys and values [B, Q, n_kv_heads, head_dim] (dtype SAM_CACHE_*; strides of row, token and head in
+ * elements, channels contiguous, the same for both) of layer `layer` into positions seq_len .. seq_len + n_new[b] - 1
+ * (n_new NULL: Q; values above Q are clamped).  Positions without a page are left out.  The pages must not be
+ * shared (sam_cache_reserve sees to it). */
+int sam_cache_append(const sam_cache* c, int32_t layer, const void* k, const void* v, int32_t dtype,
+                     int64_t row_stride, int64_t token_stride, int64_t head_stride,
+                     int32_t B, int32_t Q, const int32_t* streams, const int32_t* n_new, void* cuda_stream);
+
+/* Read: positions first[b] .. first[b] + n[b] - 1 (n NULL: Q; first NULL: 0) back into k_out, v_out
+ * [B, Q, n_kv_heads, head_dim], contiguous, of dtype; what has no page, and tokens from n[b] on, read as zero.
+ * (An fp16 result above its range is infinite.) */
+int sam_cache_read(const sam_cache* c, int32_t layer, int32_t B, int32_t Q, const int32_t* streams,
+                   const int32_t* first, const int32_t* n, void* k_out, void* v_out, int32_t dtype, void* cuda_stream);
+
+/* Attend: q, out [B, Q, H, head_dim] of dtype, strides in elements, channels contiguous; H a multiple of n_kv_heads,
+ * query head h reads key/value head h / (H / n_kv_heads).  Query row i < n_new[b] (NULL: Q) of row b stands at position
+ * p = seq_len + i and sees the positions j <= p - with window > 0 those with j > p - window only - whose page is
+ * present:   out = sum_j softmax_j(scale * q.k_j) v_j,   lse = ln sum_j exp(scale * q.k_j)  (float [B, Q, H], or NULL).
+ * A row that sees nothing, and rows from n_new[b] on: out = 0, lse = -inf.  So the keys and values of the new tokens
+ * are appended first; one call serves a single token, a proposal, or a chunk of a prompt.  Masked positions are never
+ * computed with: what their bytes hold (NaN included) does not matter.
+ * workspace: sam_cache_attend_workspace_bytes() of device memory, 256-byte aligned, zero-filled once by
+ * sam_workspace_init before the first call; calls that share it must not overlap on the device. */
+int64_t sam_cache_attend_workspace_bytes(const sam_cache* c, int32_t B, int32_t Q, int32_t H);
+int sam_cache_attend(const sam_cache* c, int32_t layer, const void* q, int32_t dtype,
+                     int64_t q_row_stride, int64_t q_token_stride, int64_t q_head_stride,
+                     int32_t B, int32_t Q, int32_t H, const int32_t* streams, const int32_t* n_new,
+                     float scale, int32_t window,
+                     void* out, int64_t out_row_stride, int64_t out_token_stride, int64_t out_head_stride,
+                     float* lse, void* workspace, int64_t workspace_bytes, void* cuda_stream);
+
+/* ---------------------------------------------------------------- diagnostics */
+
 /* Number of kernels this library has enqueued in this process so far (all entry points, all
  * threads); a measurement aid with no counterpart in the paper. */
 int64_t sam_launch_count(void);

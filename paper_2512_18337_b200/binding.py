@@ -74,6 +74,20 @@ _SIGNATURES = {
     "sam_sync_renormalize": (C.c_int, [_vp, _i32, _vp, _vp, _vp, C.POINTER(_i64)]),
     "sam_growing_set_relayout_every": (C.c_int, [_vp, _i64]),
     "sam_update_stats": (C.c_int, [_vp, C.POINTER(_i64), C.POINTER(_i64), C.POINTER(_i64)]),
+    "sam_cache_page_bytes": (_i64, [_i32, _i32, _i32, _i32]),
+    "sam_cache_scratch_bytes": (_i64, [_i32, _i32]),
+    "sam_cache_init": (C.c_int, [_vp, _vp]),
+    "sam_cache_status": (C.c_int, [_vp, C.POINTER(_i32), C.POINTER(_i32), _vp]),
+    "sam_cache_reserve": (C.c_int, [_vp, _i32, _vp, _vp, _vp]),
+    "sam_cache_commit": (C.c_int, [_vp, _i32, _vp, _vp, _vp]),
+    "sam_cache_fork": (C.c_int, [_vp, _i32, _vp, _vp, _vp]),
+    "sam_cache_compact": (C.c_int, [_vp, _vp]),
+    "sam_cache_copy_pages": (C.c_int, [_vp, _vp, _i32, _vp, _vp, _vp]),
+    "sam_cache_append": (C.c_int, [_vp, _i32, _vp, _vp, _i32, _i64, _i64, _i64, _i32, _i32, _vp, _vp, _vp]),
+    "sam_cache_read": (C.c_int, [_vp, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _i32, _vp]),
+    "sam_cache_attend_workspace_bytes": (_i64, [_vp, _i32, _i32, _i32]),
+    "sam_cache_attend": (C.c_int, [_vp, _i32, _vp, _i32, _i64, _i64, _i64, _i32, _i32, _i32, _vp, _vp, C.c_float, _i32,
+                                   _vp, _i64, _i64, _i64, _vp, _vp, _i64, _vp]),
 }
 
 
@@ -483,6 +497,236 @@ def sam_last_cuda_error() -> int:
 
 def sam_launch_count() -> int:
     return int(_load().sam_launch_count())
+
+
+# ------------------------------------------------------------------ paged 4-bit key/value cache
+SAM_CACHE_OUT_OF_PAGES = 1
+SAM_CACHE_TABLE_FULL = 2
+SAM_CACHE_BAD_FORK = 4
+SAM_CACHE_BF16 = 0
+SAM_CACHE_FP16 = 1
+SAM_CACHE_MAX_B = 4096
+
+
+class _CacheStruct(C.Structure):
+    """struct sam_cache of include/sam.h."""
+    _fields_ = [(n, _vp) for n in ("pages", "page_table", "seq_len", "ref_count", "free_list", "meta", "scratch")] + \
+        [("scratch_bytes", _i64)] + \
+        [(n, _i32) for n in ("n_pages", "page_tokens", "n_streams", "max_pages", "n_layers", "n_kv_heads", "head_dim",
+                             "k_exp", "v_exp")]
+
+
+def _size(n: int, where: str) -> int:
+    if n < 0:
+        raise SamError(int(n), where)
+    return int(n)
+
+
+def sam_cache_page_bytes(page_tokens: int, n_layers: int, n_kv_heads: int, head_dim: int) -> int:
+    return _size(_load().sam_cache_page_bytes(page_tokens, n_layers, n_kv_heads, head_dim), "sam_cache_page_bytes")
+
+
+def sam_cache_scratch_bytes(n_streams: int, n_pages: int) -> int:
+    return _size(_load().sam_cache_scratch_bytes(n_streams, n_pages), "sam_cache_scratch_bytes")
+
+
+def sam_cache_init(handle, stream=None) -> None:
+    _check(_load().sam_cache_init(handle, _stream(stream)), "sam_cache_init")
+
+
+def sam_cache_status(handle, stream=None):
+    """(n_free, status bits); synchronises the stream."""
+    a, b = _i32(), _i32()
+    _check(_load().sam_cache_status(handle, C.byref(a), C.byref(b), _stream(stream)), "sam_cache_status")
+    return a.value, b.value
+
+
+def sam_cache_reserve(handle, B, streams, n_new, stream=None) -> None:
+    _check(_load().sam_cache_reserve(handle, B, _dev(streams), _dev(n_new), _stream(stream)), "sam_cache_reserve")
+
+
+def sam_cache_commit(handle, B, streams, n_keep, stream=None) -> None:
+    _check(_load().sam_cache_commit(handle, B, _dev(streams), _dev(n_keep), _stream(stream)), "sam_cache_commit")
+
+
+def sam_cache_fork(handle, n, src, dst, stream=None) -> None:
+    _check(_load().sam_cache_fork(handle, n, _dev(src), _dev(dst), _stream(stream)), "sam_cache_fork")
+
+
+def sam_cache_compact(handle, stream=None) -> None:
+    _check(_load().sam_cache_compact(handle, _stream(stream)), "sam_cache_compact")
+
+
+def sam_cache_copy_pages(src_handle, dst_handle, n, from_ids, to_ids, stream=None) -> None:
+    _check(_load().sam_cache_copy_pages(src_handle, dst_handle, n, _dev(from_ids), _dev(to_ids), _stream(stream)),
+           "sam_cache_copy_pages")
+
+
+def sam_cache_append(handle, layer, k, v, dtype, row_stride, token_stride, head_stride, B, Q, streams, n_new,
+                     stream=None) -> None:
+    """k, v: raw addresses or contiguous tensors; strides in elements."""
+    _check(_load().sam_cache_append(handle, layer, _dev(k), _dev(v), dtype, row_stride, token_stride, head_stride, B, Q,
+                                    _dev(streams), _dev(n_new), _stream(stream)), "sam_cache_append")
+
+
+def sam_cache_read(handle, layer, B, Q, streams, first, n, k_out, v_out, dtype, stream=None) -> None:
+    _check(_load().sam_cache_read(handle, layer, B, Q, _dev(streams), _dev(first), _dev(n), _dev(k_out), _dev(v_out),
+                                  dtype, _stream(stream)), "sam_cache_read")
+
+
+def sam_cache_attend_workspace_bytes(handle, B: int, Q: int, H: int) -> int:
+    return _size(_load().sam_cache_attend_workspace_bytes(handle, B, Q, H), "sam_cache_attend_workspace_bytes")
+
+
+def sam_cache_attend(handle, layer, q, dtype, q_strides, B, Q, H, streams, n_new, scale, window, out, out_strides, lse,
+                     workspace, workspace_bytes, stream=None) -> None:
+    """q, out: raw addresses or contiguous tensors; q_strides, out_strides: (row, token, head) in elements."""
+    _check(_load().sam_cache_attend(handle, layer, _dev(q), dtype, *q_strides, B, Q, H, _dev(streams), _dev(n_new),
+                                    scale, window, _dev(out), *out_strides, _dev(lse), _dev(workspace), workspace_bytes,
+                                    _stream(stream)), "sam_cache_attend")
+
+
+class SamCache:
+    """A paged 4-bit key/value cache: owns (or is given) the torch tensors behind a `sam_cache` and marshals its calls.
+
+    tensors: any of pages, page_table, seq_len, ref_count, free_list, meta that exist already; what is missing is
+    allocated.  The cache is emptied on construction when none of its books are given.  `handle` serves the
+    `sam_cache_*` functions directly; the methods below take strided tensors [B, Q, heads, head_dim]."""
+
+    BOOKS = ("page_table", "seq_len", "ref_count", "free_list", "meta")
+
+    def __init__(self, n_pages: int, page_tokens: int, n_streams: int, max_pages: int, n_layers: int, n_kv_heads: int,
+                 head_dim: int, k_exp: int = 0, v_exp: int = 0, device="cuda:0", tensors=None, stream=None):
+        import torch
+        self.page_bytes = sam_cache_page_bytes(page_tokens, n_layers, n_kv_heads, head_dim)
+        shapes = dict(page_table=(n_streams, max_pages), seq_len=(n_streams,), ref_count=(n_pages,),
+                      free_list=(n_pages,), meta=(4,))
+        given = dict(tensors or {})
+        self.pages = given.get("pages")
+        if self.pages is None:
+            self.pages = torch.empty(n_pages, n_layers, n_kv_heads, page_tokens // 16, 18 * head_dim, dtype=torch.uint8,
+                                     device=device)
+        if self.pages.numel() * self.pages.element_size() != n_pages * self.page_bytes:
+            raise ValueError("pages: n_pages * sam_cache_page_bytes() bytes are wanted")
+        for name, shape in shapes.items():
+            t = given.get(name)
+            if t is None:
+                t = torch.empty(shape, dtype=torch.int32, device=device)
+            if tuple(t.shape) != shape or t.dtype != torch.int32:
+                raise ValueError(f"{name}: an int32 tensor of shape {shape} is wanted")
+            setattr(self, name, t)
+        n_scratch = sam_cache_scratch_bytes(n_streams, n_pages)
+        self.scratch = torch.empty(n_scratch, dtype=torch.uint8, device=device)
+        self.n_streams, self.n_kv_heads, self.head_dim = n_streams, n_kv_heads, head_dim
+        self._struct = _CacheStruct(*(_dev(getattr(self, n)) for n in ("pages", *self.BOOKS, "scratch")), n_scratch,
+                                    n_pages, page_tokens, n_streams, max_pages, n_layers, n_kv_heads, head_dim, k_exp,
+                                    v_exp)
+        self.handle = C.addressof(self._struct)
+        self._ws = None
+        if not any(n in given for n in self.BOOKS):
+            sam_cache_init(self.handle, stream)
+
+    @staticmethod
+    def _empty(shape, dtype, device, stream, zero=False):
+        """A tensor that belongs to the stream that the call runs on, so that its memory is not handed on too early."""
+        import torch
+        make = torch.zeros if zero else torch.empty
+        if stream is None:
+            return make(shape, dtype=dtype, device=device)
+        if isinstance(stream, int):
+            stream = torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
+        with torch.cuda.stream(stream):
+            return make(shape, dtype=dtype, device=device)
+
+    @staticmethod
+    def _dtype(t) -> int:
+        import torch
+        if t not in (torch.bfloat16, torch.float16):
+            raise ValueError("bfloat16 or float16 is wanted")
+        return SAM_CACHE_BF16 if t == torch.bfloat16 else SAM_CACHE_FP16
+
+    def _rows(self, t, heads: Optional[int]):
+        if t.dim() != 4 or t.shape[3] != self.head_dim or (heads is not None and t.shape[2] != heads):
+            raise ValueError("a [B, Q, heads, head_dim] tensor is wanted")
+        if not t.is_cuda or (t.stride(3) != 1 and t.numel()):
+            raise ValueError("expected a CUDA tensor with contiguous channels")
+        return t.data_ptr(), t.stride()[:3]
+
+    @staticmethod
+    def _index(t, B: int):
+        if t is not None and (t.numel() != B or "int32" not in str(t.dtype)):
+            raise ValueError("an int32 tensor with one entry per row is wanted")
+        return t
+
+    def reserve(self, n_new, streams=None, stream=None) -> None:
+        B = n_new.numel()
+        sam_cache_reserve(self.handle, B, self._index(streams, B), self._index(n_new, B), stream)
+
+    def commit(self, n_keep, streams=None, stream=None) -> None:
+        B = n_keep.numel()
+        sam_cache_commit(self.handle, B, self._index(streams, B), self._index(n_keep, B), stream)
+
+    def fork(self, src, dst, stream=None) -> None:
+        n = src.numel()
+        sam_cache_fork(self.handle, n, self._index(src, n), self._index(dst, n), stream)
+
+    def compact(self, stream=None) -> None:
+        sam_cache_compact(self.handle, stream)
+
+    def copy_pages(self, to_cache: "SamCache", from_ids, to_ids, stream=None) -> None:
+        n = from_ids.numel()
+        sam_cache_copy_pages(self.handle, to_cache.handle, n, self._index(from_ids, n), self._index(to_ids, n), stream)
+
+    def status(self, stream=None):
+        return sam_cache_status(self.handle, stream)
+
+    def append(self, layer: int, k, v, n_new=None, streams=None, stream=None) -> None:
+        pk, st = self._rows(k, self.n_kv_heads)
+        pv, sv = self._rows(v, self.n_kv_heads)
+        if st != sv or k.shape != v.shape or k.dtype != v.dtype:
+            raise ValueError("keys and values of one shape, type and layout are wanted")
+        B, Q = k.shape[:2]
+        sam_cache_append(self.handle, layer, pk, pv, self._dtype(k.dtype), *st, B, Q, self._index(streams, B),
+                         self._index(n_new, B), stream)
+
+    def read(self, layer: int, first=None, n=None, max_n: Optional[int] = None, dtype=None, streams=None, out=None,
+             stream=None):
+        """(keys, values) [B, max_n, n_kv_heads, head_dim] of positions first .. first + n - 1."""
+        import torch
+        B = next((t.numel() for t in (streams, first, n) if t is not None), self.n_streams)
+        if out is None:
+            shape = (B, max_n, self.n_kv_heads, self.head_dim)
+            out = tuple(self._empty(shape, dtype or torch.bfloat16, self.pages.device, stream) for _ in range(2))
+        k, v = out
+        if k.shape != v.shape or k.dtype != v.dtype or k.shape[0] != B or tuple(k.shape[2:]) != (self.n_kv_heads, self.head_dim):
+            raise ValueError("two [B, max_n, n_kv_heads, head_dim] tensors of one type are wanted")
+        sam_cache_read(self.handle, layer, B, k.shape[1], self._index(streams, B), self._index(first, B),
+                       self._index(n, B), k, v, self._dtype(k.dtype), stream)
+        return k, v
+
+    def attend(self, layer: int, q, n_new=None, streams=None, scale: Optional[float] = None, window: int = 0, out=None,
+               lse=None, workspace=None, stream=None):
+        """(out, lse).  Without a workspace the cache keeps one, grown when a call needs more: calls that may overlap
+        on the device (several streams) bring their own, zero-filled by sam_workspace_init."""
+        import torch
+        pq, sq = self._rows(q, None)
+        B, Q, H = q.shape[:3]
+        if out is None:
+            out = self._empty(q.shape, q.dtype, q.device, stream)
+        if lse is None:
+            lse = self._empty((B, Q, H), torch.float32, q.device, stream)
+        po, so = self._rows(out, H)
+        if out.shape != q.shape or out.dtype != q.dtype or tuple(lse.shape) != (B, Q, H) or lse.dtype != torch.float32:
+            raise ValueError("out like q and a float32 lse [B, Q, H] are wanted")
+        need = sam_cache_attend_workspace_bytes(self.handle, B, Q, H)
+        if workspace is None:
+            if self._ws is None or self._ws.numel() < need:
+                self._ws = self._empty(need, torch.uint8, q.device, stream, zero=True)
+            workspace = self._ws
+        sam_cache_attend(self.handle, layer, pq, self._dtype(q.dtype), sq, B, Q, H, self._index(streams, B),
+                         self._index(n_new, B), self.head_dim ** -0.5 if scale is None else scale, window, po, so, lse,
+                         workspace, workspace.numel() * workspace.element_size(), stream)
+        return out, lse
 
 
 # ------------------------------------------------------------------ convenience holder

@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "sam.h"
+#include "sam_common.h"
 #include "sam_index.h"
 #include "sam_kernels.cuh"
 #include "argmax_bulk.cuh"
@@ -19,39 +20,6 @@
 using namespace samb200;
 
 namespace {
-
-thread_local int g_last_cuda = 0;
-std::atomic<long long> g_launches{0};   // kernels this library has enqueued (diagnostic)
-
-inline int cuda_fail(cudaError_t e) {
-    g_last_cuda = static_cast<int>(e);
-    return SAM_ERR_CUDA;
-}
-
-#define SAM_CUDA(call)                                   \
-    do {                                                 \
-        cudaError_t e__ = (call);                        \
-        if (e__ != cudaSuccess) return cuda_fail(e__);   \
-    } while (0)
-
-struct DeviceInfo {
-    int sms = 0;
-};
-
-int device_info(DeviceInfo* out) {
-    static thread_local int cached_dev = -1;
-    static thread_local DeviceInfo cached;
-    int dev = 0;
-    SAM_CUDA(cudaGetDevice(&dev));
-    if (dev != cached_dev) {
-        int sms = 0;
-        SAM_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-        cached.sms = sms;
-        cached_dev = dev;
-    }
-    *out = cached;
-    return SAM_OK;
-}
 
 // ---- optional per-kernel timing (events owned by the library) --------------------------------
 struct Profile {
@@ -66,8 +34,6 @@ inline void prof_mark(int phase, cudaStream_t st) {
 inline void prof_done() {
     if (g_prof.used < g_prof.cap) ++g_prof.used;
 }
-
-inline bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
 int check_verify_args(const void* logits, int64_t stride, int32_t B, int32_t K, int32_t V,
                       const int32_t* drafts, const int32_t* n_draft, int32_t* argmax_out,
