@@ -503,6 +503,7 @@ def sam_launch_count() -> int:
 SAM_CACHE_OUT_OF_PAGES = 1
 SAM_CACHE_TABLE_FULL = 2
 SAM_CACHE_BAD_FORK = 4
+SAM_CACHE_GAVE_UP = 8
 SAM_CACHE_BF16 = 0
 SAM_CACHE_FP16 = 1
 SAM_CACHE_MAX_B = 4096

@@ -6,6 +6,7 @@
 
 #include "sam.h"
 #include "sam_common.h"
+#include "attend_stream.cuh"
 #include "cache_attend.cuh"
 #include "cache_format.cuh"
 #include "cache_io.cuh"
@@ -95,13 +96,27 @@ int launch_read(const CacheView& v, int32_t layer, int32_t B, int32_t Q, const i
     return launched();
 }
 
-template <typename T>
-int launch_attend(const AttendArgs& a, cudaStream_t s) {
-    const int64_t warps = static_cast<int64_t>(a.B) * a.Q * a.H;
-    const unsigned grid = static_cast<unsigned>((warps + 3) / 4);
-    if (a.c.D == 64) attend_rows_kernel<T, 64><<<grid, 128, 0, s>>>(a);
-    else attend_rows_kernel<T, 128><<<grid, 128, 0, s>>>(a);
+// Workspace of sam_cache_attend: arrival counters (zero between calls), then partial results of up to kMaxCtas CTAs.
+constexpr int kMaxCtas = 512;
+constexpr int64_t kCounterBytes = kMaxCtas * 4;
+template <int D>
+constexpr int64_t partial_bytes() {
+    return 2ll * kMaxCtas * 4 * StreamPlan<D, 2>::kPiece;
+}
+
+template <typename T, int D, int NT>
+int launch_stream(const AttendArgs& a, int sms, cudaStream_t s) {
+    using Plan = StreamPlan<D, NT>;
+    SAM_CUDA(cudaFuncSetAttribute(attend_stream_kernel<T, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Plan::kSmem));
+    attend_stream_kernel<T, D, NT><<<std::min(sms * Plan::kCtasPerSm, kMaxCtas), kStreamThreads, Plan::kSmem, s>>>(a);
     return launched();
+}
+
+template <typename T, int D>
+int launch_attend(const AttendArgs& a, cudaStream_t s) {
+    DeviceInfo di;
+    if (int e = device_info(&di)) return e;
+    return static_cast<int64_t>(a.Q) * a.group <= 8 ? launch_stream<T, D, 1>(a, di.sms, s) : launch_stream<T, D, 2>(a, di.sms, s);
 }
 
 }  // namespace
@@ -240,7 +255,7 @@ int64_t sam_cache_attend_workspace_bytes(const sam_cache* c, int32_t B, int32_t 
     if (int e = check_cache(c)) return e;
     if (B < 0 || Q < 0 || H < 1 || H % c->n_kv_heads) return SAM_ERR_INVALID_ARG;
     if (B > SAM_CACHE_MAX_B) return SAM_ERR_TOO_LARGE;
-    return 256;
+    return kCounterBytes + (c->head_dim == 64 ? partial_bytes<64>() : partial_bytes<128>());
 }
 
 int sam_cache_attend(const sam_cache* c, int32_t layer, const void* q, int32_t dtype, int64_t q_row_stride, int64_t q_token_stride,
@@ -275,9 +290,16 @@ int sam_cache_attend(const sam_cache* c, int32_t layer, const void* q, int32_t d
     a.Q = Q;
     a.H = H;
     a.window = window;
+    a.group = H / c->n_kv_heads;
     a.scale = scale;
+    a.q_wide = aligned(q, 16) && (q_row_stride | q_token_stride | q_head_stride) % 8 == 0;
+    a.o_wide = aligned(out, 16) && (out_row_stride | out_token_stride | out_head_stride) % 8 == 0;
+    a.counters = static_cast<int32_t*>(workspace);
+    a.partials = reinterpret_cast<float*>(static_cast<char*>(workspace) + kCounterBytes);
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-    return dtype == SAM_CACHE_BF16 ? launch_attend<__nv_bfloat16>(a, s) : launch_attend<__half>(a, s);
+    const bool bf16 = dtype == SAM_CACHE_BF16;
+    if (c->head_dim == 64) return bf16 ? launch_attend<__nv_bfloat16, 64>(a, s) : launch_attend<__half, 64>(a, s);
+    return bf16 ? launch_attend<__nv_bfloat16, 128>(a, s) : launch_attend<__half, 128>(a, s);
 }
 
 }  // extern "C"
