@@ -7,6 +7,7 @@
 #include "sam.h"
 #include "sam_common.h"
 #include "attend_stream.cuh"
+#include "attend_wide.cuh"
 #include "cache_attend.cuh"
 #include "cache_format.cuh"
 #include "cache_io.cuh"
@@ -99,9 +100,12 @@ int launch_read(const CacheView& v, int32_t layer, int32_t B, int32_t Q, const i
 // Workspace of sam_cache_attend: arrival counters (zero between calls), then partial results of up to kMaxCtas CTAs.
 constexpr int kMaxCtas = 512;
 constexpr int64_t kCounterBytes = kMaxCtas * 4;
+constexpr int64_t kNarrowRows = 16;   // query rows per key/value head up to which the streaming kernel is used
+
 template <int D>
-constexpr int64_t partial_bytes() {
-    return 2ll * kMaxCtas * 4 * StreamPlan<D, 2>::kPiece;
+int64_t partial_bytes(int64_t rows) {
+    if (rows <= kNarrowRows) return 2ll * kMaxCtas * 4 * StreamPlan<D, 2>::kPiece;
+    return 2ll * kWideMaxCtas * 4 * (rows <= 128 ? WidePlan<D, false>::kPart : WidePlan<D, true>::kPart);
 }
 
 template <typename T, int D, int NT>
@@ -112,11 +116,22 @@ int launch_stream(const AttendArgs& a, int sms, cudaStream_t s) {
     return launched();
 }
 
+template <typename T, int D, bool kPair>
+int launch_wide(const AttendArgs& a, int sms, cudaStream_t s) {
+    using Plan = WidePlan<D, kPair>;
+    SAM_CUDA(cudaFuncSetAttribute(attend_wide_kernel<T, D, kPair>, cudaFuncAttributeMaxDynamicSharedMemorySize, Plan::kSmem));
+    attend_wide_kernel<T, D, kPair><<<std::min(sms, kWideMaxCtas), kWideThreads, Plan::kSmem, s>>>(a);
+    return launched();
+}
+
 template <typename T, int D>
 int launch_attend(const AttendArgs& a, cudaStream_t s) {
     DeviceInfo di;
     if (int e = device_info(&di)) return e;
-    return static_cast<int64_t>(a.Q) * a.group <= 8 ? launch_stream<T, D, 1>(a, di.sms, s) : launch_stream<T, D, 2>(a, di.sms, s);
+    const int64_t rows = static_cast<int64_t>(a.Q) * a.group;
+    if (rows <= 8) return launch_stream<T, D, 1>(a, di.sms, s);
+    if (rows <= kNarrowRows) return launch_stream<T, D, 2>(a, di.sms, s);
+    return rows <= 128 ? launch_wide<T, D, false>(a, di.sms, s) : launch_wide<T, D, true>(a, di.sms, s);
 }
 
 }  // namespace
@@ -255,7 +270,8 @@ int64_t sam_cache_attend_workspace_bytes(const sam_cache* c, int32_t B, int32_t 
     if (int e = check_cache(c)) return e;
     if (B < 0 || Q < 0 || H < 1 || H % c->n_kv_heads) return SAM_ERR_INVALID_ARG;
     if (B > SAM_CACHE_MAX_B) return SAM_ERR_TOO_LARGE;
-    return kCounterBytes + (c->head_dim == 64 ? partial_bytes<64>() : partial_bytes<128>());
+    const int64_t rows = static_cast<int64_t>(Q) * (H / c->n_kv_heads);
+    return kCounterBytes + (c->head_dim == 64 ? partial_bytes<64>(rows) : partial_bytes<128>(rows));
 }
 
 int sam_cache_attend(const sam_cache* c, int32_t layer, const void* q, int32_t dtype, int64_t q_row_stride, int64_t q_token_stride,
