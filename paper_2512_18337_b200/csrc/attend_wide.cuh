@@ -19,9 +19,8 @@
 namespace samb200 {
 
 constexpr int kWideUnit = 128;                     // tokens of a step
-constexpr int kWideThreads = 13 * 32;              // two softmax groups of four warps, four expanding warps, one issuing warp
+constexpr int kWideWarps = 20, kWideThreads = kWideWarps * 32;   // two softmax groups and two expanding groups of four warps, one issuing and one filling warp (and two that idle)
 constexpr int kWideMaxCtas = 160;
-constexpr int kWidePrefetch = 4;                   // steps that the tiles are brought into L2 ahead
 
 template <int D, bool kPair>
 struct WidePlan {
@@ -29,7 +28,9 @@ struct WidePlan {
     static constexpr int kTileBytes = 128 * D * 2;                      // a [128][D] fp16 operand
     static constexpr int kChunkBytes = 128 * 128;                       // 64 channels of it
     static constexpr int kQ = 0, kK = (kPair ? 2 : 1) * kTileBytes, kV = kK + 2 * kTileBytes;
-    static constexpr int kSmem = kV + 2 * kTileBytes + 1024;            // and room to start on a 1024-byte boundary
+    static constexpr int kRaw = kV + 2 * kTileBytes;                    // ring of 4-bit halves: eight tiles' keys or values
+    static constexpr int kRawSlots = kPair && D == 128 ? 3 : 6, kRawHalf = 72 * D;
+    static constexpr int kSmem = kRaw + kRawSlots * kRawHalf + 1024;    // and room to start on a 1024-byte boundary
     static constexpr int kPartTile = 128 * D + 2 * 128;                 // floats of a row tile's partial result
     static constexpr int kPart = (kPair ? 2 : 1) * kPartTile;
 };
@@ -144,9 +145,10 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
     using Plan = WidePlan<D, kPair>;
     constexpr int kRows = Plan::kRows;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t bars[16];
+    __shared__ uint64_t bars[14], raw_bars[2][Plan::kRawSlots];
+    __shared__ uint32_t raw_there[Plan::kRawSlots];    // which of a half's eight tiles are there
     __shared__ uint32_t tmem_base;
-    __shared__ int64_t scan[13], start_e, start_begin;
+    __shared__ int64_t scan[kWideWarps], start_e, start_begin;
     __shared__ float2 stats[2][128];
     __shared__ uint32_t stat_nan[2][128];
     __shared__ alignas(4) uint8_t tile_there[4][4];    // per step (mod 4) and expanding warp: which of its two tiles are there
@@ -167,6 +169,8 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
     auto v_full = [&](int s) { return bar + 64 + 8 * s; };
     auto v_empty = [&](int s) { return bar + 80 + 8 * s; };
     const uint32_t query_bar = bar + 96, both_bar = bar + 104;
+    auto raw_full = [&](int s) { return shared_addr(&raw_bars[0][0]) + 8 * s; };
+    auto raw_empty = [&](int s) { return shared_addr(&raw_bars[1][0]) + 8 * s; };
     auto wait = [&](uint32_t b, uint32_t parity) {     // false: give up (here or elsewhere in the CTA)
         for (uint32_t i = 0; i < kCachePolls; ++i) {
             if (barrier_try(b, parity)) return true;
@@ -187,6 +191,10 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
         }
         barrier_init(query_bar, 8);
         barrier_init(both_bar, 8);
+        for (int k = 0; k < Plan::kRawSlots; ++k) {
+            barrier_init(raw_full(k), 1);
+            barrier_init(raw_empty(k), 4);
+        }
         abort_flag = 0;
     }
     barrier_init_fence();
@@ -205,7 +213,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
         if (lane == 31) scan[warp] = y;
         __syncthreads();
         int64_t all = 0, first = 0;
-        for (int w = 0; w < 13; ++w) {
+        for (int w = 0; w < kWideWarps; ++w) {
             if (w == warp) first = all;
             all += scan[w];
         }
@@ -244,7 +252,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
     }
     clear_unused_rows<T, D>(a, cta, gridDim.x);
     if (!busy) return;
-    if (warp == 12) tmem_alloc(shared_addr(&tmem_base), 512);
+    if (warp == 16) tmem_alloc(shared_addr(&tmem_base), 512);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -279,181 +287,14 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
         return t0 + kWideUnit - 1 <= g.first_pos && (a.window == 0 || t0 > g.last_pos - a.window);
     };
 
-    if (warp >= 8 && warp < 12) {
-        // ================= expanding warps: 4-bit tiles -> fp16 operands
-        // Keys of step n + 1 come before the values of step n: that is the order in which the products need them.  A warp takes two
-        // tiles of a step, a thread a quarter of the channels of tokens lane % 8 and + 8: eight threads in turn then write eight
-        // different 16-byte columns of the swizzled rows.
-        const int w = warp - 8, tok = lane & 7, quarter = lane >> 3;
-        constexpr int QB = D / 8;                          // bytes of codes of a quarter
-        constexpr int QW = D / 32;                         // words
-        struct Half {
-            uint32_t codes[4][QW];                         // tile 0: tokens tok, tok + 8; tile 1
-            uint32_t scales[4];                            // D = 128: two bytes, D = 64: one
-            uint32_t nans;                                 // among the values of the same tokens, when asked for
-            uint32_t there;                                // which of the two tiles are there
-        };
-        // Pages of this warp's two tiles of sixteen steps from page_base on: lane = 2 * (step - page_base) + tile.
-        int page_base = -1, page_of = -1;
-        auto load = [&](const WideSegment& g, int step, bool values, bool look, Half& h) {
-            if (page_base < 0 || step - page_base >= 16) {
-                page_base = max(step - 1, 0);              // the values of the step before are still to come
-                const int t = g.ri.lo + (page_base + (lane >> 1)) * kWideUnit + (w * 2 + (lane & 1)) * 16;
-                page_of = t < g.ri.hi && t >= 0 ? c.page_at(g.ri.s, t >> c.log_p) : -1;
-            }
-            const int t0 = g.ri.lo + step * kWideUnit + w * 32;
-            h.nans = 0;
-            h.there = 0;
-            if (!values && lane >= 2 * (kWidePrefetch + step - page_base) && lane < 2 * (kWidePrefetch + 1 + step - page_base) && page_of >= 0)
-                l2_prefetch(c.tile(page_of, a.layer, g.head, (t0 + kWidePrefetch * kWideUnit + (lane & 1) * 16) & (c.page_tokens() - 1)), 18 * D);
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const int t = t0 + x * 16, page = __shfl_sync(0xffffffffu, page_of, 2 * (step - page_base) + x);
-                const uint8_t* tile = page >= 0 ? c.tile(page, a.layer, g.head, t & (c.page_tokens() - 1)) : nullptr;
-                h.there |= static_cast<uint32_t>(page >= 0) << x;
-#pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                    const int tk = tok + 8 * y;
-                    uint32_t(&cd)[QW] = h.codes[x * 2 + y];
-                    if (tile) {
-                        const uint8_t* p = tile + (values ? 8 * D : 0) + tk * (D / 2) + quarter * QB;
-                        if constexpr (D == 128) {
-                            const uint4 v = __ldg(reinterpret_cast<const uint4*>(p));
-                            cd[0] = v.x, cd[1] = v.y, cd[2] = v.z, cd[3] = v.w;
-                            h.scales[x * 2 + y] = __ldg(reinterpret_cast<const uint16_t*>(tile + (values ? 17 : 16) * D + tk * 8 + quarter * 2));
-                        } else {
-                            const uint2 v = __ldg(reinterpret_cast<const uint2*>(p));
-                            cd[0] = v.x, cd[1] = v.y;
-                            h.scales[x * 2 + y] = __ldg(tile + (values ? 17 : 16) * D + tk * 4 + quarter);
-                        }
-                        if (look && t + tk < g.ri.hi) {
-                            uint32_t s = D == 128 ? __ldg(reinterpret_cast<const uint16_t*>(tile + 17 * D + tk * 8 + quarter * 2))
-                                                  : __ldg(tile + 17 * D + tk * 4 + quarter);
-                            if ((s & 0x7f) == 0x7f) h.nans |= 1u << (2 * (x * 2 + y));
-                            if (D == 128 && (s & 0x7f00) == 0x7f00) h.nans |= 2u << (2 * (x * 2 + y));
-                        }
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < QW; ++k) cd[k] = 0;
-                        h.scales[x * 2 + y] = 0;
-                    }
-                }
-            }
-        };
-        auto expand = [&](const WideSegment& g, int step, bool values, const Half& h, uint32_t base) {
-            const int t0 = g.ri.lo + step * kWideUnit;
-            const bool all = seen_by_all(g, t0);
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const int row = (w * 2 + (x >> 1)) * 16 + tok + 8 * (x & 1);
-                uint32_t s = h.scales[x];
-                if (values && !all) {   // what is masked must not be multiplied with
-                    if (t0 + row >= g.ri.hi) s = 0;
-                    if ((s & 0x7f) == 0x7f) s &= 0xff00;
-                    if ((s & 0x7f00) == 0x7f00) s &= 0x00ff;
-                }
-                const uint32_t f = e4m3x2_to_half2(D == 128 ? s : s * 0x0101u);
-                const uint32_t f0 = D == 128 ? __byte_perm(f, f, 0x1010) : f, f1 = D == 128 ? __byte_perm(f, f, 0x3232) : f;
-#pragma unroll
-                for (int k = 0; k < QW; ++k) {
-                    uint32_t y[4];
-                    e2m1x8_to_half2(h.codes[x][k], y);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) y[i] = mul_half2(y[i], k < QW / 2 ? f0 : f1);
-                    // 16-byte column of the 64-channel chunk
-                    const int col = quarter * QW + k, chunk = col >> 3;
-                    const uint32_t at = base + chunk * Plan::kChunkBytes + row * 128 + (((col & 7) ^ (row & 7)) << 4);
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3]) : "memory");
-                }
-            }
-        };
-        uint32_t kt = 0, vt = 0;    // keys, values expanded so far
-        auto put = [&](const WideSegment& g, int step, bool values, const Half& h) -> bool {
-            uint32_t& n = values ? vt : kt;
-            const int stage = n & 1;
-            if (n >= 2 && !wait(values ? v_empty(stage) : k_empty(stage), ((n >> 1) - 1) & 1)) return false;
-            expand(g, step, values, h, sm + (values ? Plan::kV : Plan::kK) + stage * Plan::kTileBytes);
-            if (!values) {
-                const int ring = n & 3;
-                const uint32_t flagged = __ballot_sync(0xffffffffu, h.nans != 0);
-                if (flagged) {
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        // blocks of a quarter: two at 128 channels, one at 64
-                        uint32_t m = D == 128 ? ((h.nans >> (2 * x)) & 3) << (2 * quarter) : ((h.nans >> (2 * x)) & 1) << quarter;
-                        m |= __shfl_xor_sync(0xffffffffu, m, 8);
-                        m |= __shfl_xor_sync(0xffffffffu, m, 16);
-                        if (quarter == 0) nan_block[ring][(w * 2 + (x >> 1)) * 16 + tok + 8 * (x & 1)] = static_cast<uint8_t>(m);
-                    }
-                }
-                if (lane == 0) {
-                    nan_flag[ring][w] = flagged;
-                    tile_there[ring][w] = static_cast<uint8_t>(h.there);
-                }
-            }
-            async_proxy_fence();
-            __syncwarp();
-            if (lane == 0) barrier_arrive(values ? v_full(stage) : k_full(stage));
-            ++n;
-            return true;
-        };
-        for_pieces([&](const WideSegment& g, int s0, int count) {
-            // each half is loaded as soon as the registers of the one before it are free, most of a step ahead of its use
-            Half hk, hv;
-            page_base = -1;
-            load(g, s0, false, !seen_by_all(g, g.ri.lo + s0 * kWideUnit), hk);
-            for (int k = 0; k < count; ++k) {
-                if (!put(g, s0 + k, false, hk)) return false;
-                if (k + 1 < count) load(g, s0 + k + 1, false, !seen_by_all(g, g.ri.lo + (s0 + k + 1) * kWideUnit), hk);
-                if (k > 0 && !put(g, s0 + k - 1, true, hv)) return false;
-                load(g, s0 + k, true, false, hv);
-            }
-            return put(g, s0 + count - 1, true, hv);
-        });
-    } else if (warp == 12) {
-        // ================= issuing warp
-        if (lane == 0) {
-            constexpr uint32_t kScoreDesc = product_desc(128, 128, false), kSumDesc = product_desc(128, D, true);
-            uint32_t kt = 0, vt = 0, n_query = 0, n_weight[2] = {0, 0};
-            for_pieces([&](const WideSegment&, int, int count) {
-                const int jobs = kPair ? 2 * count : count;
-                if (!wait(query_bar, n_query++ & 1)) return false;
-                tc_fence_after();
-                auto scores = [&](int n) -> bool {      // S of job n
-                    const int g = n & 1, tile = kPair ? n >> 1 : n, stage = (kt + tile) & 1;
-                    if ((!kPair || g == 0) && !wait(k_full(stage), ((kt + tile) >> 1) & 1)) return false;
-                    tc_fence_after();
-                    const uint32_t q = sm + Plan::kQ + (kPair ? g : 0) * Plan::kTileBytes, k = sm + Plan::kK + stage * Plan::kTileBytes;
-#pragma unroll
-                    for (int i = 0; i < D / 16; ++i) {
-                        const uint32_t off = (i >> 2) * Plan::kChunkBytes + (i & 3) * 32;
-                        tc_mma_ss(tmem + g * 128, operand_desc(q + off, 16, 1024), operand_desc(k + off, 16, 1024), kScoreDesc, i > 0);
-                    }
-                    tc_commit(score_bar(g));
-                    if (!kPair || g == 1) tc_commit(k_empty(stage));
-                    return true;
-                };
-                if (!scores(0)) return false;
-                for (int n = 0; n < jobs; ++n) {
-                    if (n + 1 < jobs && !scores(n + 1)) return false;
-                    const int g = n & 1, tile = kPair ? n >> 1 : n, stage = (vt + tile) & 1;
-                    if ((!kPair || g == 0) && !wait(v_full(stage), ((vt + tile) >> 1) & 1)) return false;
-                    if (!wait(weight_bar(g), n_weight[g]++ & 1)) return false;
-                    tc_fence_after();
-                    const uint32_t v = sm + Plan::kV + stage * Plan::kTileBytes;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        tc_mma_ts(tmem + 256 + g * 128, tmem + g * 128 + i * 8, operand_desc(v + i * 2048, Plan::kChunkBytes, 1024), kSumDesc, n > 1 || i > 0);
-                    if (!kPair || g == 1) tc_commit(v_empty(stage));
-                    if (n + 2 >= jobs) tc_commit(score_bar(g));   // the group's last: its sums are complete
-                }
-                kt += count;
-                vt += count;
-                return true;
-            });
-        }
-        __syncwarp();
-    } else {
+    // Registers go where they are needed: 2 x 128 threads x 136, 2 x 128 x 72, 128 x 64, of 640 x 96 at launch.
+    // Halves (the keys or the values of a step) come in the order in which the products need them: K0, K1, V0, K2, V1, ..., and go
+    // through a ring of 4-bit tiles.  Number of a half within a piece of `count` steps:
+    auto key_index = [](int k) { return k == 0 ? 0 : 2 * k - 1; };
+    auto value_index = [](int k, int count) { return k == count - 1 ? 2 * count - 1 : 2 * k + 2; };
+
+    if (warp < 8) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 136;");
         // ================= softmax groups
         const int g = warp >> 2, row = tid & 127, quarter_lane = (warp & 3) << 21;   // lane quarter in the tensor-memory address
         const uint32_t s_at = tmem + quarter_lane + g * 128, o_at = tmem + quarter_lane + 256 + g * 128;
@@ -541,13 +382,16 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                 uint32_t x[2][32];
                 if (full) {
                     tmem_load32(s_at, x[0]);
+#pragma unroll 1
+                    for (int q = 0; q < 128; q += 64) {
+                        tmem_load_wait(x[0]);
+                        tmem_load32(s_at + q + 32, x[1]);
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        uint32_t(&s)[32] = x[q & 1];
-                        tmem_load_wait(s);
-                        tmem_load32(s_at + ((q + 1) & 3) * 32, x[(q + 1) & 1]);   // the last one is the first of the second pass
+                        for (int i = 0; i < 32; i += 2) top = fmaxf(fmaxf(top, __uint_as_float(x[0][i])), __uint_as_float(x[0][i + 1]));
+                        tmem_load_wait(x[1]);
+                        tmem_load32(s_at + (q ^ 64), x[0]);          // the last one is the first of the second pass
 #pragma unroll
-                        for (int i = 0; i < 32; i += 2) top = fmaxf(fmaxf(top, __uint_as_float(s[i])), __uint_as_float(s[i + 1]));
+                        for (int i = 0; i < 32; i += 2) top = fmaxf(fmaxf(top, __uint_as_float(x[1][i])), __uint_as_float(x[1][i + 1]));
                     }
                 } else {
 #pragma unroll 1
@@ -579,11 +423,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                 const float ref = m == -INFINITY ? 0.f : m;
                 float2 total = make_float2(0.f, 0.f);
                 if (full) {
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        uint32_t(&s)[32] = x[q & 1];
-                        tmem_load_wait(s);
-                        if (q < 3) tmem_load32(s_at + (q + 1) * 32, x[(q + 1) & 1]);
+                    auto weights = [&](const uint32_t (&s)[32], int at) {
                         uint32_t p[16];
 #pragma unroll
                         for (int i = 0; i < 32; i += 2) {
@@ -593,7 +433,16 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                             total = add2(total, y);
                             p[i / 2] = pack_half2(y.x, y.y);
                         }
-                        tmem_store16(s_at + q * 16, p);  // behind the scores that are still to be read
+                        tmem_store16(s_at + at, p);                  // behind the scores that are still to be read
+                    };
+#pragma unroll 1
+                    for (int q = 0; q < 128; q += 64) {
+                        tmem_load_wait(x[0]);
+                        tmem_load32(s_at + q + 32, x[1]);
+                        weights(x[0], q / 2);
+                        tmem_load_wait(x[1]);
+                        if (q == 0) tmem_load32(s_at + 64, x[0]);
+                        weights(x[1], q / 2 + 16);
                     }
                 } else {
 #pragma unroll 1
@@ -742,11 +591,215 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
             tc_fence_before();
             return both();
         });
+    } else if (warp < 16) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        // ================= expanding warps: 4-bit tiles -> fp16 operands; four warps for the keys, four for the values
+        // A warp takes two tiles of a half, a thread a quarter of the channels of tokens lane / 4 and + 8: its reads are contiguous
+        // over the warp, and with the words of the upper two quarters swapped its writes fall into eight different 16-byte columns of
+        // the swizzled rows.
+        const bool values = warp >= 12;
+        const int w = warp & 3, tok = lane >> 2, quarter = lane & 3;
+        constexpr int QB = D / 8;                          // bytes of codes of a quarter
+        constexpr int QW = D / 32;                         // words
+        const bool swap = D == 128 && quarter >= 2;
+        uint32_t column[QW];                               // where the thread's 16-byte columns go, in a warp's share of a stage
+#pragma unroll
+        for (int k = 0; k < QW; ++k) {
+            const int col = quarter * QW + (swap ? k ^ 2 : k);
+            column[k] = sm + (values ? Plan::kV : Plan::kK) + (col >> 3) * Plan::kChunkBytes + (w * 32 + tok) * 128 + (((col & 7) ^ tok) << 4);
+        }
+        const uint32_t raw = sm + Plan::kRaw + w * (18 * D);
+        const uint32_t codes_at = raw + tok * (D / 2) + quarter * QB, scales_at = raw + 8 * D + (D == 128 ? tok * 8 + quarter * 2 : tok * 4 + quarter);
+        uint32_t n = 0, halves = 0;                        // halves of this kind, and of both kinds in earlier pieces
+        for_pieces([&](const WideSegment& g, int s0, int count) {
+#pragma unroll 1
+            for (int k = 0; k < count; ++k, ++n) {
+                const uint32_t index = halves + (values ? value_index(k, count) : key_index(k));
+                const int slot = index % Plan::kRawSlots, stage = n & 1;
+                if (!wait(raw_full(slot), (index / Plan::kRawSlots) & 1)) return false;
+                const uint32_t there = raw_there[slot] >> (2 * w);
+                uint32_t codes[4][QW], scales[4];
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const uint32_t at = slot * Plan::kRawHalf + (x >> 1) * (9 * D);
+                    lds_words<QW>(at + codes_at + (x & 1) * 8 * (D / 2), codes[x]);
+                    if constexpr (D == 128) {
+                        uint16_t y;
+                        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(y) : "r"(at + scales_at + (x & 1) * 64));
+                        scales[x] = y;
+                    } else {
+                        scales[x] = lds8(at + scales_at + (x & 1) * 32);
+                    }
+                }
+                if (n >= 2 && !wait(values ? v_empty(stage) : k_empty(stage), ((n >> 1) - 1) & 1)) return false;
+                const int t0 = g.ri.lo + (s0 + k) * kWideUnit + w * 32;
+                const bool all = seen_by_all(g, g.ri.lo + (s0 + k) * kWideUnit);
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    uint32_t s = (there >> (x >> 1)) & 1 ? scales[x] : 0;
+                    if (values && !all) {   // what is masked must not be multiplied with
+                        if (t0 + x * 8 + tok >= g.ri.hi) s = 0;
+                        if ((s & 0x7f) == 0x7f) s &= 0xff00;
+                        if ((s & 0x7f00) == 0x7f00) s &= 0x00ff;
+                    }
+                    const uint32_t f = e4m3x2_to_half2(D == 128 ? s : s * 0x0101u);
+                    const uint32_t f0 = D == 128 ? __byte_perm(f, f, swap ? 0x3232 : 0x1010) : f, f1 = D == 128 ? __byte_perm(f, f, swap ? 0x1010 : 0x3232) : f;
+#pragma unroll
+                    for (int q = 0; q < QW; ++q) {
+                        uint32_t y[4];
+                        e2m1x8_to_half2(D == 128 && swap ? codes[x][q ^ (QW / 2)] : codes[x][q], y);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) y[i] = mul_half2(y[i], q < QW / 2 ? f0 : f1);
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
+                                     ::"r"(column[q] + stage * Plan::kTileBytes + x * 1024), "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3]) : "memory");
+                    }
+                }
+                if (!values) {
+                    const int ring = n & 3;
+                    uint32_t flagged = 0;
+                    if (!all) {
+                        // NaN among the values of these tokens, for the rows that do see them
+                        uint32_t nans = 0;
+#pragma unroll 1
+                        for (int x = 0; x < 4; ++x) {
+                            const int t = t0 + x * 8 + tok;
+                            if (!((there >> (x >> 1)) & 1) || t >= g.ri.hi) continue;
+                            const uint8_t* z = c.tile(c.page_at(g.ri.s, t >> c.log_p), a.layer, g.head, t & (c.page_tokens() - 1)) + 17 * D +
+                                               ((x & 1) * 8 + tok) * (D / 16) + (D == 128 ? quarter * 2 : quarter);
+                            const uint32_t s = D == 128 ? __ldg(reinterpret_cast<const uint16_t*>(z)) : __ldg(z);
+                            if ((s & 0x7f) == 0x7f) nans |= 1u << (2 * x);
+                            if (D == 128 && (s & 0x7f00) == 0x7f00) nans |= 2u << (2 * x);
+                        }
+                        flagged = __ballot_sync(0xffffffffu, nans != 0);
+                        if (flagged) {
+#pragma unroll 1
+                            for (int x = 0; x < 4; ++x) {
+                                // blocks of a quarter: two at 128 channels, one at 64
+                                uint32_t m = D == 128 ? ((nans >> (2 * x)) & 3) << (2 * quarter) : ((nans >> (2 * x)) & 1) << quarter;
+                                m |= __shfl_xor_sync(0xffffffffu, m, 1);
+                                m |= __shfl_xor_sync(0xffffffffu, m, 2);
+                                if (quarter == 0) nan_block[ring][w * 32 + x * 8 + tok] = static_cast<uint8_t>(m);
+                            }
+                        }
+                    }
+                    if (lane == 0) {
+                        nan_flag[ring][w] = flagged;
+                        tile_there[ring][w] = static_cast<uint8_t>(there & 3);
+                    }
+                }
+                async_proxy_fence();
+                __syncwarp();
+                if (lane == 0) {
+                    barrier_arrive(raw_empty(slot));
+                    barrier_arrive(values ? v_full(stage) : k_full(stage));
+                }
+            }
+            halves += 2 * count;
+            return true;
+        });
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        if (warp == 17) {
+        // ================= filling warp: a bulk copy of codes and one of scales per tile, lane = 2 * tile + which
+        const int tile_no = (lane >> 1) & 7, scales = lane & 1;
+        uint32_t filled = 0;
+        for_pieces([&](const WideSegment& g, int s0, int count) {
+            const uint8_t* const head = c.head_tiles(0, a.layer, g.head);
+            // pages of four steps: lane = 8 * step + tile; the next four have been read already and are brought into L2 meanwhile
+            auto pages_of = [&](int step) {
+                const int t = g.ri.lo + (step + (lane >> 3)) * kWideUnit + (lane & 7) * 16;
+                return t < g.ri.hi && t >= 0 ? c.page_at(g.ri.s, t >> c.log_p) : -1;
+            };
+            auto tile_of = [&](int page, int t) { return head + page * c.page_bytes + ((t & (c.page_tokens() - 1)) >> 4) * (18 * D); };
+            int base = s0, pages = pages_of(s0), ahead = pages_of(s0 + 4), later = pages_of(s0 + 8);
+            int k = 0, v = 0;
+#pragma unroll 1
+            for (int i = 0; i < 2 * count; ++i, ++filled) {
+                const bool values = !(k < count && k - v < 2);
+                const int step = s0 + (values ? v++ : k++);
+                if (!values && step - base >= 5) {         // the values of the step before are still to come
+                    base += 4;
+                    pages = ahead;
+                    ahead = later;
+                    later = pages_of(base + 8);
+                    const int t = g.ri.lo + (base + 4 + (lane >> 3)) * kWideUnit + (lane & 7) * 16;
+                    if (ahead >= 0 && base + 4 + (lane >> 3) < s0 + count) l2_prefetch(tile_of(ahead, t), 18 * D);
+                }
+                const int off = (step - base) * 8 + tile_no;
+                const int page = off < 32 ? __shfl_sync(0xffffffffu, pages, off & 31) : __shfl_sync(0xffffffffu, ahead, off & 31);
+                const int slot = filled % Plan::kRawSlots;
+                if (filled >= Plan::kRawSlots && !wait(raw_empty(slot), (filled / Plan::kRawSlots - 1) & 1)) return false;
+                const bool on = page >= 0 && lane < 16;
+                const uint32_t there = __ballot_sync(0xffffffffu, on && !scales);
+                if (lane == 0) {
+                    // the even bits, one per tile
+                    uint32_t m = there & 0x5555;
+                    m = (m | m >> 1) & 0x3333;
+                    m = (m | m >> 2) & 0x0f0f;
+                    m = (m | m >> 4) & 0xff;
+                    raw_there[slot] = m;
+                    barrier_expect(raw_full(slot), __popc(there) * (9 * D));
+                }
+                __syncwarp();
+                if (on) {
+                    const uint8_t* tile = tile_of(page, g.ri.lo + step * kWideUnit + tile_no * 16);
+                    const uint32_t dst = sm + Plan::kRaw + slot * Plan::kRawHalf + tile_no * (9 * D);
+                    if (scales) bulk_load(dst + 8 * D, tile + (values ? 17 * D : 16 * D), D, raw_full(slot));
+                    else bulk_load(dst, tile + (values ? 8 * D : 0), 8 * D, raw_full(slot));
+                }
+                __syncwarp();
+            }
+            return true;
+        });
+        } else if (warp == 16) {
+        // ================= issuing warp
+        if (lane == 0) {
+            constexpr uint32_t kScoreDesc = product_desc(128, 128, false), kSumDesc = product_desc(128, D, true);
+            uint32_t kt = 0, vt = 0, n_query = 0, n_weight[2] = {0, 0};
+            for_pieces([&](const WideSegment&, int, int count) {
+                const int jobs = kPair ? 2 * count : count;
+                if (!wait(query_bar, n_query++ & 1)) return false;
+                tc_fence_after();
+                auto scores = [&](int n) -> bool {      // S of job n
+                    const int g = n & 1, tile = kPair ? n >> 1 : n, stage = (kt + tile) & 1;
+                    if ((!kPair || g == 0) && !wait(k_full(stage), ((kt + tile) >> 1) & 1)) return false;
+                    tc_fence_after();
+                    const uint32_t q = sm + Plan::kQ + (kPair ? g : 0) * Plan::kTileBytes, k = sm + Plan::kK + stage * Plan::kTileBytes;
+#pragma unroll
+                    for (int i = 0; i < D / 16; ++i) {
+                        const uint32_t off = (i >> 2) * Plan::kChunkBytes + (i & 3) * 32;
+                        tc_mma_ss(tmem + g * 128, operand_desc(q + off, 16, 1024), operand_desc(k + off, 16, 1024), kScoreDesc, i > 0);
+                    }
+                    tc_commit(score_bar(g));
+                    if (!kPair || g == 1) tc_commit(k_empty(stage));
+                    return true;
+                };
+                if (!scores(0)) return false;
+                for (int n = 0; n < jobs; ++n) {
+                    if (n + 1 < jobs && !scores(n + 1)) return false;
+                    const int g = n & 1, tile = kPair ? n >> 1 : n, stage = (vt + tile) & 1;
+                    if ((!kPair || g == 0) && !wait(v_full(stage), ((vt + tile) >> 1) & 1)) return false;
+                    if (!wait(weight_bar(g), n_weight[g]++ & 1)) return false;
+                    tc_fence_after();
+                    const uint32_t v = sm + Plan::kV + stage * Plan::kTileBytes;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        tc_mma_ts(tmem + 256 + g * 128, tmem + g * 128 + i * 8, operand_desc(v + i * 2048, Plan::kChunkBytes, 1024), kSumDesc, n > 1 || i > 0);
+                    if (!kPair || g == 1) tc_commit(v_empty(stage));
+                    if (n + 2 >= jobs) tc_commit(score_bar(g));   // the group's last: its sums are complete
+                }
+                kt += count;
+                vt += count;
+                return true;
+            });
+        }
+        __syncwarp();
+        }
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == 12) tmem_free(tmem, 512);
+    if (warp == 16) tmem_free(tmem, 512);
     if (tid == 0 && abort_flag && c.meta) atomicOr(&c.meta[1], kStatusGaveUp);
 }
 
