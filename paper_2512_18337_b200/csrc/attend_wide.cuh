@@ -19,7 +19,7 @@
 namespace samb200 {
 
 constexpr int kWideUnit = 128;                     // tokens of a step
-constexpr int kWideWarps = 20, kWideThreads = kWideWarps * 32;   // two softmax groups and two expanding groups of four warps, one issuing and one filling warp (and two that idle)
+constexpr int kWideWarps = 20, kWideThreads = kWideWarps * 32;   // two softmax groups and two expanding groups of four warps, one issuing warp (and three that idle)
 constexpr int kWideMaxCtas = 160;
 
 template <int D, bool kPair>
@@ -28,9 +28,9 @@ struct WidePlan {
     static constexpr int kTileBytes = 128 * D * 2;                      // a [128][D] fp16 operand
     static constexpr int kChunkBytes = 128 * 128;                       // 64 channels of it
     static constexpr int kQ = 0, kK = (kPair ? 2 : 1) * kTileBytes, kV = kK + 2 * kTileBytes;
-    static constexpr int kRaw = kV + 2 * kTileBytes;                    // ring of 4-bit halves: eight tiles' keys or values
-    static constexpr int kRawSlots = kPair && D == 128 ? 3 : 6, kRawHalf = 72 * D;
-    static constexpr int kSmem = kRaw + kRawSlots * kRawHalf + 1024;    // and room to start on a 1024-byte boundary
+    static constexpr int kRaw = kV + 2 * kTileBytes;                    // slots of the expanding warps: two tiles' keys or values each
+    static constexpr int kRawSlots = kPair && D == 128 ? 1 : 3, kRawHalf = 18 * D;
+    static constexpr int kSmem = kRaw + 8 * kRawSlots * kRawHalf + 1024;   // and room to start on a 1024-byte boundary
     static constexpr int kPartTile = 128 * D + 2 * 128;                 // floats of a row tile's partial result
     static constexpr int kPart = (kPair ? 2 : 1) * kPartTile;
 };
@@ -85,8 +85,8 @@ __device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t (&x)[16
 __device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 #undef SAM_R8
 #undef SAM_S8
-__device__ __forceinline__ void l2_prefetch(const void* p, uint32_t bytes) {
-    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
+__device__ __forceinline__ void async_copy16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void async_proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
@@ -145,8 +145,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
     using Plan = WidePlan<D, kPair>;
     constexpr int kRows = Plan::kRows;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t bars[14], raw_bars[2][Plan::kRawSlots];
-    __shared__ uint32_t raw_there[Plan::kRawSlots];    // which of a half's eight tiles are there
+    __shared__ uint64_t bars[14];
     __shared__ uint32_t tmem_base;
     __shared__ int64_t scan[kWideWarps], start_e, start_begin;
     __shared__ float2 stats[2][128];
@@ -169,8 +168,6 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
     auto v_full = [&](int s) { return bar + 64 + 8 * s; };
     auto v_empty = [&](int s) { return bar + 80 + 8 * s; };
     const uint32_t query_bar = bar + 96, both_bar = bar + 104;
-    auto raw_full = [&](int s) { return shared_addr(&raw_bars[0][0]) + 8 * s; };
-    auto raw_empty = [&](int s) { return shared_addr(&raw_bars[1][0]) + 8 * s; };
     auto wait = [&](uint32_t b, uint32_t parity) {     // false: give up (here or elsewhere in the CTA)
         for (uint32_t i = 0; i < kCachePolls; ++i) {
             if (barrier_try(b, parity)) return true;
@@ -191,10 +188,6 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
         }
         barrier_init(query_bar, 8);
         barrier_init(both_bar, 8);
-        for (int k = 0; k < Plan::kRawSlots; ++k) {
-            barrier_init(raw_full(k), 1);
-            barrier_init(raw_empty(k), 4);
-        }
         abort_flag = 0;
     }
     barrier_init_fence();
@@ -288,11 +281,6 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
     };
 
     // Registers go where they are needed: 2 x 128 threads x 136, 2 x 128 x 72, 128 x 64, of 640 x 96 at launch.
-    // Halves (the keys or the values of a step) come in the order in which the products need them: K0, K1, V0, K2, V1, ..., and go
-    // through a ring of 4-bit tiles.  Number of a half within a piece of `count` steps:
-    auto key_index = [](int k) { return k == 0 ? 0 : 2 * k - 1; };
-    auto value_index = [](int k, int count) { return k == count - 1 ? 2 * count - 1 : 2 * k + 2; };
-
     if (warp < 8) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 136;");
         // ================= softmax groups
@@ -594,13 +582,15 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
     } else if (warp < 16) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         // ================= expanding warps: 4-bit tiles -> fp16 operands; four warps for the keys, four for the values
-        // A warp takes two tiles of a half, a thread a quarter of the channels of tokens lane / 4 and + 8: its reads are contiguous
-        // over the warp, and with the words of the upper two quarters swapped its writes fall into eight different 16-byte columns of
-        // the swizzled rows.
+        // A warp takes two tiles of a step and brings them itself, a few steps ahead, into slots of its own (sixteen bytes a thread and
+        // copy: a bulk copy costs some 100 clocks to issue, however small).  A thread expands a quarter of the channels of tokens
+        // lane / 4 and + 8: its reads are contiguous over the warp, and with the words of the upper two quarters swapped its writes
+        // fall into eight different 16-byte columns of the swizzled rows.
         const bool values = warp >= 12;
         const int w = warp & 3, tok = lane >> 2, quarter = lane & 3;
         constexpr int QB = D / 8;                          // bytes of codes of a quarter
         constexpr int QW = D / 32;                         // words
+        constexpr int R = Plan::kRawSlots;
         const bool swap = D == 128 && quarter >= 2;
         uint32_t column[QW];                               // where the thread's 16-byte columns go, in a warp's share of a stage
 #pragma unroll
@@ -608,16 +598,49 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
             const int col = quarter * QW + (swap ? k ^ 2 : k);
             column[k] = sm + (values ? Plan::kV : Plan::kK) + (col >> 3) * Plan::kChunkBytes + (w * 32 + tok) * 128 + (((col & 7) ^ tok) << 4);
         }
-        const uint32_t raw = sm + Plan::kRaw + w * (18 * D);
+        const uint32_t raw = sm + Plan::kRaw + (warp - 8) * R * Plan::kRawHalf;
         const uint32_t codes_at = raw + tok * (D / 2) + quarter * QB, scales_at = raw + 8 * D + (D == 128 ? tok * 8 + quarter * 2 : tok * 4 + quarter);
-        uint32_t n = 0, halves = 0;                        // halves of this kind, and of both kinds in earlier pieces
+        constexpr int kCodeParts = 8 * D / 512;            // warp-wide copies of a tile's codes
+        constexpr int kScaleLanes = D / 16;                // sixteen-byte parts of a tile's scales
+        uint32_t n = 0;                                    // halves expanded so far
         for_pieces([&](const WideSegment& g, int s0, int count) {
+            const uint8_t* const head = c.head_tiles(0, a.layer, g.head) + (values ? 8 * D : 0);
+            // pages of the warp's tiles of sixteen steps: lane = 2 * (step - page_base) + tile
+            int page_base = s0, page_of = -1, slot = 0;
+            uint32_t present = 0;                          // two bits per slot
+            auto fill = [&](int step) {                    // the step's tiles into the slot, if it is one of ours
+                if (step < s0 + count) {
+                    if (step - page_base >= 16 || step == s0) {
+                        page_base = step;
+                        const int t = g.ri.lo + (step + (lane >> 1)) * kWideUnit + (w * 2 + (lane & 1)) * 16;
+                        page_of = t < g.ri.hi && t >= 0 ? c.page_at(g.ri.s, t >> c.log_p) : -1;
+                    }
+                    const int t0 = g.ri.lo + step * kWideUnit + w * 32;
+                    const uint32_t dst = raw + slot * Plan::kRawHalf + lane * 16;
+                    present &= ~(3u << (2 * slot));
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const int page = __shfl_sync(0xffffffffu, page_of, 2 * (step - page_base) + x);
+                        if (page < 0) continue;
+                        present |= 1u << (2 * slot + x);
+                        const uint8_t* src = head + page * c.page_bytes + (((t0 + x * 16) & (c.page_tokens() - 1)) >> 4) * (18 * D) + lane * 16;
+#pragma unroll
+                        for (int y = 0; y < kCodeParts; ++y) async_copy16(dst + x * (9 * D) + y * 512, src + y * 512);
+                        // scales: D bytes, 8 D (values) or 15 D further on for keys
+                        if (lane < kScaleLanes) async_copy16(dst + x * (9 * D) + 8 * D, src + (values ? 9 * D : 16 * D));
+                    }
+                }
+                asm volatile("cp.async.commit_group;" ::: "memory");
+            };
+#pragma unroll 1
+            for (int k = 0; k < R; ++k, ++slot) fill(s0 + k);
+            slot = 0;
 #pragma unroll 1
             for (int k = 0; k < count; ++k, ++n) {
-                const uint32_t index = halves + (values ? value_index(k, count) : key_index(k));
-                const int slot = index % Plan::kRawSlots, stage = n & 1;
-                if (!wait(raw_full(slot), (index / Plan::kRawSlots) & 1)) return false;
-                const uint32_t there = raw_there[slot] >> (2 * w);
+                asm volatile("cp.async.wait_group %0;" ::"n"(R - 1) : "memory");
+                __syncwarp();
+                const int stage = n & 1;
+                const uint32_t there = present >> (2 * slot);
                 uint32_t codes[4][QW], scales[4];
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
@@ -631,6 +654,9 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                         scales[x] = lds8(at + scales_at + (x & 1) * 32);
                     }
                 }
+                __syncwarp();
+                fill(s0 + k + R);
+                if (++slot == R) slot = 0;
                 if (n >= 2 && !wait(values ? v_empty(stage) : k_empty(stage), ((n >> 1) - 1) & 1)) return false;
                 const int t0 = g.ri.lo + (s0 + k) * kWideUnit + w * 32;
                 const bool all = seen_by_all(g, g.ri.lo + (s0 + k) * kWideUnit);
@@ -689,72 +715,18 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                 }
                 async_proxy_fence();
                 __syncwarp();
-                if (lane == 0) {
-                    barrier_arrive(raw_empty(slot));
-                    barrier_arrive(values ? v_full(stage) : k_full(stage));
-                }
+                if (lane == 0) barrier_arrive(values ? v_full(stage) : k_full(stage));
             }
-            halves += 2 * count;
             return true;
         });
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-        if (warp == 17) {
-        // ================= filling warp: a bulk copy of codes and one of scales per tile, lane = 2 * tile + which
-        const int tile_no = (lane >> 1) & 7, scales = lane & 1;
-        uint32_t filled = 0;
-        for_pieces([&](const WideSegment& g, int s0, int count) {
-            const uint8_t* const head = c.head_tiles(0, a.layer, g.head);
-            // pages of four steps: lane = 8 * step + tile; the next four have been read already and are brought into L2 meanwhile
-            auto pages_of = [&](int step) {
-                const int t = g.ri.lo + (step + (lane >> 3)) * kWideUnit + (lane & 7) * 16;
-                return t < g.ri.hi && t >= 0 ? c.page_at(g.ri.s, t >> c.log_p) : -1;
-            };
-            auto tile_of = [&](int page, int t) { return head + page * c.page_bytes + ((t & (c.page_tokens() - 1)) >> 4) * (18 * D); };
-            int base = s0, pages = pages_of(s0), ahead = pages_of(s0 + 4), later = pages_of(s0 + 8);
-            int k = 0, v = 0;
-#pragma unroll 1
-            for (int i = 0; i < 2 * count; ++i, ++filled) {
-                const bool values = !(k < count && k - v < 2);
-                const int step = s0 + (values ? v++ : k++);
-                if (!values && step - base >= 5) {         // the values of the step before are still to come
-                    base += 4;
-                    pages = ahead;
-                    ahead = later;
-                    later = pages_of(base + 8);
-                    const int t = g.ri.lo + (base + 4 + (lane >> 3)) * kWideUnit + (lane & 7) * 16;
-                    if (ahead >= 0 && base + 4 + (lane >> 3) < s0 + count) l2_prefetch(tile_of(ahead, t), 18 * D);
-                }
-                const int off = (step - base) * 8 + tile_no;
-                const int page = off < 32 ? __shfl_sync(0xffffffffu, pages, off & 31) : __shfl_sync(0xffffffffu, ahead, off & 31);
-                const int slot = filled % Plan::kRawSlots;
-                if (filled >= Plan::kRawSlots && !wait(raw_empty(slot), (filled / Plan::kRawSlots - 1) & 1)) return false;
-                const bool on = page >= 0 && lane < 16;
-                const uint32_t there = __ballot_sync(0xffffffffu, on && !scales);
-                if (lane == 0) {
-                    // the even bits, one per tile
-                    uint32_t m = there & 0x5555;
-                    m = (m | m >> 1) & 0x3333;
-                    m = (m | m >> 2) & 0x0f0f;
-                    m = (m | m >> 4) & 0xff;
-                    raw_there[slot] = m;
-                    barrier_expect(raw_full(slot), __popc(there) * (9 * D));
-                }
-                __syncwarp();
-                if (on) {
-                    const uint8_t* tile = tile_of(page, g.ri.lo + step * kWideUnit + tile_no * 16);
-                    const uint32_t dst = sm + Plan::kRaw + slot * Plan::kRawHalf + tile_no * (9 * D);
-                    if (scales) bulk_load(dst + 8 * D, tile + (values ? 17 * D : 16 * D), D, raw_full(slot));
-                    else bulk_load(dst, tile + (values ? 8 * D : 0), 8 * D, raw_full(slot));
-                }
-                __syncwarp();
-            }
-            return true;
-        });
-        } else if (warp == 16) {
+        if (warp == 16) {
         // ================= issuing warp
         if (lane == 0) {
             constexpr uint32_t kScoreDesc = product_desc(128, 128, false), kSumDesc = product_desc(128, D, true);
+            const uint64_t q_desc = operand_desc(sm + Plan::kQ, 16, 1024), k_desc = operand_desc(sm + Plan::kK, 16, 1024);
+            const uint64_t v_desc = operand_desc(sm + Plan::kV, Plan::kChunkBytes, 1024);
             uint32_t kt = 0, vt = 0, n_query = 0, n_weight[2] = {0, 0};
             for_pieces([&](const WideSegment&, int, int count) {
                 const int jobs = kPair ? 2 * count : count;
@@ -764,11 +736,11 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                     const int g = n & 1, tile = kPair ? n >> 1 : n, stage = (kt + tile) & 1;
                     if ((!kPair || g == 0) && !wait(k_full(stage), ((kt + tile) >> 1) & 1)) return false;
                     tc_fence_after();
-                    const uint32_t q = sm + Plan::kQ + (kPair ? g : 0) * Plan::kTileBytes, k = sm + Plan::kK + stage * Plan::kTileBytes;
+                    const uint64_t q = q_desc + (kPair ? g : 0) * (Plan::kTileBytes >> 4), k = k_desc + stage * (Plan::kTileBytes >> 4);
 #pragma unroll
                     for (int i = 0; i < D / 16; ++i) {
-                        const uint32_t off = (i >> 2) * Plan::kChunkBytes + (i & 3) * 32;
-                        tc_mma_ss(tmem + g * 128, operand_desc(q + off, 16, 1024), operand_desc(k + off, 16, 1024), kScoreDesc, i > 0);
+                        const uint32_t off = ((i >> 2) * Plan::kChunkBytes + (i & 3) * 32) >> 4;
+                        tc_mma_ss(tmem + g * 128, q + off, k + off, kScoreDesc, i > 0);
                     }
                     tc_commit(score_bar(g));
                     if (!kPair || g == 1) tc_commit(k_empty(stage));
@@ -781,10 +753,9 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                     if ((!kPair || g == 0) && !wait(v_full(stage), ((vt + tile) >> 1) & 1)) return false;
                     if (!wait(weight_bar(g), n_weight[g]++ & 1)) return false;
                     tc_fence_after();
-                    const uint32_t v = sm + Plan::kV + stage * Plan::kTileBytes;
+                    const uint64_t v = v_desc + stage * (Plan::kTileBytes >> 4);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        tc_mma_ts(tmem + 256 + g * 128, tmem + g * 128 + i * 8, operand_desc(v + i * 2048, Plan::kChunkBytes, 1024), kSumDesc, n > 1 || i > 0);
+                    for (int i = 0; i < 8; ++i) tc_mma_ts(tmem + 256 + g * 128, tmem + g * 128 + i * 8, v + i * (2048 >> 4), kSumDesc, n > 1 || i > 0);
                     if (!kPair || g == 1) tc_commit(v_empty(stage));
                     if (n + 2 >= jobs) tc_commit(score_bar(g));   // the group's last: its sums are complete
                 }
