@@ -1,17 +1,24 @@
 // Attention for many query rows per key/value head (proposals of several heads, prompt chunks): tcgen05 products.
 //
-// S = Q K^T and O += P V on 128-row tiles, with 128 tokens a step.  Four warps expand the 4-bit tiles into two stages of fp16
-// keys and two of fp16 values in shared memory (exact: a value has six significant bits); Q lies there too, S and O in tensor
-// memory.  A thread of a softmax group owns one query row, so its maximum and its sum need no exchange; it writes P as fp16
-// over S, from where the second product takes it.  Two groups alternate, so that one group's exponentials run under the other's
-// products: with more than 128 query rows they hold two row tiles that share the expanded keys and values (kPair), otherwise
-// they take the steps of one row tile in turn and are joined at the end of the segment.
+// S = Q K^T and O += P V on a tile of 128 query rows, with 128 tokens a step.  Sixteen warps expand the 4-bit tiles into two stages
+// of fp16 keys and two of fp16 values in shared memory (exact: a value has six significant bits).  Q, two tiles of scores and the
+// sums O lie in tensor memory.  A thread of the four softmax warps owns one query row, so its maximum and its sum need no exchange;
+// it writes P as fp16 over S, from where the second product takes it.  While it works on one step's scores, the products of the
+// step before and of the step after run.
+//
+// Q is read from tensor memory, not from shared memory, because a 128 x 128 product with both operands in shared memory takes all of
+// its bandwidth: the expanding warps and every barrier then stand still (a store gets through at a tenth of its rate, a load at a
+// thirtieth).  With one operand there the products take half of it.
 //
 // Keys and values have the same layout in shared memory, [token][64 channels] in 128-byte rows with the 128-byte swizzle: for
 // the first product it is read with the channels (the summed index) innermost, for the second with the channels as the N side.
 //
-// The reference of the weights follows the rule of attend_stream.cuh: a row's sums are rescaled only when a score lies 15
-// (powers of two) above it.
+// Weights are 2^(score - reference), with a reference that lies 8 below the largest score when it is set.  It is raised, and the
+// row's sums rescaled, only when the weights of a step add up to more than 2^15: as long as they do not, each of them is within
+// fp16, and the maximum of a step need not be known.  Weights down to 2^-22 of the largest keep all 11 bits.
+//
+// What the warps of an SM run has to stay within the instruction caches: the roles are small loops, and masked steps have code of
+// their own.
 #pragma once
 
 #include "attend_stream.cuh"
@@ -19,20 +26,22 @@
 namespace samb200 {
 
 constexpr int kWideUnit = 128;                     // tokens of a step
-constexpr int kWideWarps = 20, kWideThreads = kWideWarps * 32;   // two softmax groups and two expanding groups of four warps, one issuing warp (and three that idle)
+constexpr int kWideRows = 128;                     // query rows of a segment
+constexpr int kWideWarps = 24, kWideThreads = kWideWarps * 32;   // four softmax warps, sixteen expanding ones, an issuing one (and three that idle)
 constexpr int kWideMaxCtas = 160;
+constexpr float kWideAbove = 8.f, kTotalMax = 32768.f;   // 128 weights of 2^8 add up to no more
+// columns of tensor memory
+constexpr uint32_t kColQ = 0, kColS = 64, kColO = 320;
 
-template <int D, bool kPair>
+template <int D>
 struct WidePlan {
-    static constexpr int kRows = kPair ? 256 : 128;                     // query rows of a segment
     static constexpr int kTileBytes = 128 * D * 2;                      // a [128][D] fp16 operand
     static constexpr int kChunkBytes = 128 * 128;                       // 64 channels of it
-    static constexpr int kQ = 0, kK = (kPair ? 2 : 1) * kTileBytes, kV = kK + 2 * kTileBytes;
-    static constexpr int kRaw = kV + 2 * kTileBytes;                    // slots of the expanding warps: two tiles' keys or values each
-    static constexpr int kRawSlots = kPair && D == 128 ? 1 : 3, kRawHalf = 18 * D;
-    static constexpr int kSmem = kRaw + 8 * kRawSlots * kRawHalf + 1024;   // and room to start on a 1024-byte boundary
-    static constexpr int kPartTile = 128 * D + 2 * 128;                 // floats of a row tile's partial result
-    static constexpr int kPart = (kPair ? 2 : 1) * kPartTile;
+    static constexpr int kK = 0, kV = 2 * kTileBytes;
+    static constexpr int kRaw = kV + 2 * kTileBytes;                    // slots of the expanding warps: a tile's keys or values each
+    static constexpr int kRawSlots = 3, kRawHalf = 9 * D;
+    static constexpr int kSmem = kRaw + 16 * kRawSlots * kRawHalf + 1024;   // and room to start on a 1024-byte boundary
+    static constexpr int kPart = 128 * D + 2 * 128;                     // floats of a partial result
 };
 
 // ---- tensor memory and tcgen05
@@ -115,7 +124,7 @@ __device__ __forceinline__ float2 add2(float2 x, float2 y) {
     return w;
 }
 
-// A segment: one row of the batch, one row tile (kRows query rows), one key/value head; its steps cover the tokens that some
+// A segment: one row of the batch, one tile of kWideRows query rows, one key/value head; its steps cover the tokens that some
 // query row of it sees.  Segments are numbered by row, row tile, head.
 struct WideSegment {
     RowInfo ri;          // lo, hi: of this row tile
@@ -124,15 +133,14 @@ struct WideSegment {
     int first_pos, last_pos;
     int64_t begin;       // number of its first unit
 };
-template <int kRows>
 __device__ __forceinline__ void wide_tile(const AttendArgs& a, int tiles, int64_t e, WideSegment& g) {   // e = b * tiles + rt
     g.b = static_cast<int>(e / tiles);
     g.rt = static_cast<int>(e % tiles);
     g.ri = row_info<kWideUnit>(a, g.b);
-    g.rows = min(g.ri.n * a.group - g.rt * kRows, kRows);
+    g.rows = min(g.ri.n * a.group - g.rt * kWideRows, kWideRows);
     g.steps = 0;
     if (g.rows <= 0) return;
-    const int i0 = g.rt * kRows / a.group, i1 = (g.rt * kRows + g.rows - 1) / a.group, cap = a.c.capacity();
+    const int i0 = g.rt * kWideRows / a.group, i1 = (g.rt * kWideRows + g.rows - 1) / a.group, cap = a.c.capacity();
     g.first_pos = g.ri.len + i0;
     g.last_pos = g.ri.len + i1;
     g.ri.hi = static_cast<int>(min(static_cast<int64_t>(g.ri.len) + i1 + 1, static_cast<int64_t>(cap)));
@@ -140,18 +148,15 @@ __device__ __forceinline__ void wide_tile(const AttendArgs& a, int tiles, int64_
     g.steps = max((g.ri.hi - g.ri.lo + kWideUnit - 1) / kWideUnit, 1);
 }
 
-template <typename T, int D, bool kPair>
+template <typename T, int D>
 __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __grid_constant__ AttendArgs a) {
-    using Plan = WidePlan<D, kPair>;
-    constexpr int kRows = Plan::kRows;
+    using Plan = WidePlan<D>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t bars[14];
     __shared__ uint32_t tmem_base;
     __shared__ int64_t scan[kWideWarps], start_e, start_begin;
-    __shared__ float2 stats[2][128];
-    __shared__ uint32_t stat_nan[2][128];
-    __shared__ alignas(4) uint8_t tile_there[4][4];    // per step (mod 4) and expanding warp: which of its two tiles are there
-    __shared__ uint32_t nan_flag[4][4];                // per step and expanding warp: NaN among the values of its tokens
+    __shared__ alignas(8) uint8_t tile_there[4][8];    // per step (mod 4): which of its eight tiles are there
+    __shared__ alignas(8) uint8_t nan_flag[4][8];      // NaN among the values of a tile's tokens (written where there are masks)
     __shared__ uint8_t nan_block[4][128];              // which 16-channel blocks of a token's values are NaN
     __shared__ int last_here;
     __shared__ volatile int abort_flag;
@@ -160,14 +165,13 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const uint32_t sm = shared_addr(smem), bar = shared_addr(bars);
-    // barriers: scores ready / weights ready per group, keys and values full / empty per stage, queries ready, both groups
-    auto score_bar = [&](int g) { return bar + 8 * g; };
-    auto weight_bar = [&](int g) { return bar + 16 + 8 * g; };
-    auto k_full = [&](int s) { return bar + 32 + 8 * s; };
-    auto k_empty = [&](int s) { return bar + 48 + 8 * s; };
-    auto v_full = [&](int s) { return bar + 64 + 8 * s; };
-    auto v_empty = [&](int s) { return bar + 80 + 8 * s; };
-    const uint32_t query_bar = bar + 96, both_bar = bar + 104;
+    // barriers: scores ready, keys and values full / empty (two each), weights ready, product done, queries ready, softmax warps
+    auto score_bar = [&](int i) { return bar + 8 * i; };
+    auto k_full = [&](int i) { return bar + 16 + 8 * i; };
+    auto k_empty = [&](int i) { return bar + 32 + 8 * i; };
+    auto v_full = [&](int i) { return bar + 48 + 8 * i; };
+    auto v_empty = [&](int i) { return bar + 64 + 8 * i; };
+    const uint32_t weight_bar = bar + 80, product_bar = bar + 88, query_bar = bar + 96, group_bar = bar + 104;
     auto wait = [&](uint32_t b, uint32_t parity) {     // false: give up (here or elsewhere in the CTA)
         for (uint32_t i = 0; i < kCachePolls; ++i) {
             if (barrier_try(b, parity)) return true;
@@ -178,22 +182,23 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
     };
 
     if (tid == 0) {
-        for (int g = 0; g < 2; ++g) {
-            barrier_init(score_bar(g), 1);
-            barrier_init(weight_bar(g), 4);
-            barrier_init(k_full(g), 4);
-            barrier_init(k_empty(g), 1);
-            barrier_init(v_full(g), 4);
-            barrier_init(v_empty(g), 1);
+        for (int i = 0; i < 2; ++i) {
+            barrier_init(score_bar(i), 1);
+            barrier_init(k_full(i), 8);
+            barrier_init(k_empty(i), 1);
+            barrier_init(v_full(i), 8);
+            barrier_init(v_empty(i), 1);
         }
-        barrier_init(query_bar, 8);
-        barrier_init(both_bar, 8);
+        barrier_init(weight_bar, 4);
+        barrier_init(product_bar, 1);
+        barrier_init(query_bar, 4);
+        barrier_init(group_bar, 4);
         abort_flag = 0;
     }
     barrier_init_fence();
 
     // ---- how many units there are, and where our share begins
-    const int tiles = static_cast<int>((static_cast<int64_t>(a.Q) * a.group + kRows - 1) / kRows);
+    const int tiles = static_cast<int>((static_cast<int64_t>(a.Q) * a.group + kWideRows - 1) / kWideRows);
     const int64_t n_tiles = static_cast<int64_t>(a.B) * tiles;
     auto block_sum = [&](int64_t x, int64_t* before) -> int64_t {
         int64_t y = x;
@@ -216,7 +221,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
     auto units_of = [&](int64_t e) -> int64_t {
         if (e >= n_tiles) return 0;
         WideSegment g;
-        wide_tile<kRows>(a, tiles, e, g);
+        wide_tile(a, tiles, e, g);
         return static_cast<int64_t>(g.steps) * c.n_kv;
     };
     int64_t units = 0, mine = 0, before = 0;
@@ -245,7 +250,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
     }
     clear_unused_rows<T, D>(a, cta, gridDim.x);
     if (!busy) return;
-    if (warp == 16) tmem_alloc(shared_addr(&tmem_base), 512);
+    if (warp == 20) tmem_alloc(shared_addr(&tmem_base), 512);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -255,7 +260,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
     auto for_pieces = [&](auto f) {
         WideSegment g;
         int64_t e = start_e;
-        wide_tile<kRows>(a, tiles, e, g);
+        wide_tile(a, tiles, e, g);
         const int64_t rel = u0 - start_begin;
         g.head = static_cast<int>(rel / g.steps);
         g.begin = start_begin + static_cast<int64_t>(g.head) * g.steps;
@@ -270,7 +275,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
             if (++g.head == c.n_kv) {
                 g.head = 0;
                 const int64_t next = g.begin;
-                do wide_tile<kRows>(a, tiles, ++e, g);
+                do wide_tile(a, tiles, ++e, g);
                 while (g.steps == 0 && e + 1 < n_tiles);
                 g.begin = next;
             }
@@ -280,66 +285,66 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
         return t0 + kWideUnit - 1 <= g.first_pos && (a.window == 0 || t0 > g.last_pos - a.window);
     };
 
-    // Registers go where they are needed: 2 x 128 threads x 136, 2 x 128 x 72, 128 x 64, of 640 x 96 at launch.
-    if (warp < 8) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 136;");
-        // ================= softmax groups
-        const int g = warp >> 2, row = tid & 127, quarter_lane = (warp & 3) << 21;   // lane quarter in the tensor-memory address
-        const uint32_t s_at = tmem + quarter_lane + g * 128, o_at = tmem + quarter_lane + 256 + g * 128;
-        uint32_t n_score = 0, n_both = 0, kt = 0;
-        auto both = [&]() -> bool {                     // meets the other group
+    // Registers go where they are needed: 128 threads x 168, 512 x 56, 128 x 72, of 768 x 80 at launch.
+    if (warp < 4) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
+        // ================= softmax warps
+        const int row = tid;
+        const uint32_t lanes = tmem + (static_cast<uint32_t>(warp) << 21);   // the warp's quarter of the lanes
+        uint32_t n = 0, n_group = 0;                    // steps so far; meetings of the four warps
+        auto meet = [&]() -> bool {
             __syncwarp();
-            if (lane == 0) barrier_arrive(both_bar);
-            return wait(both_bar, n_both++ & 1);
+            if (lane == 0) barrier_arrive(group_bar);
+            return wait(group_bar, n_group++ & 1);
+        };
+        uint32_t n_product = 0;                         // products known to be complete: each is waited for in turn, a parity tells two apart
+        auto products = [&](uint32_t upto) -> bool {
+            while (n_product < upto)
+                if (!wait(product_bar, n_product++ & 1)) return false;
+            tc_fence_after();
+            return true;
         };
         for_pieces([&](const WideSegment& seg, int s0, int count) {
-            // ---- queries into shared memory
-            const int rho_tile = seg.rt * kRows + (kPair ? g * 128 : 0);     // first query row of this group's tile
-            const bool mine = (kPair ? g * 128 : 0) + row < seg.rows;
-            const int rho = rho_tile + row, qi = rho / a.group, qh = seg.head * a.group + rho % a.group;
+            // ---- queries into tensor memory
+            const bool mine = row < seg.rows;
+            const int rho = seg.rt * kWideRows + row, qi = rho / a.group, qh = seg.head * a.group + rho % a.group;
             float factor;
             {
-                // without a pair both groups hold the same rows and write half the channels each
-                constexpr int kPart = kPair ? D : D / 2;
                 const T* q = static_cast<const T*>(a.q) + seg.b * a.q_row + static_cast<int64_t>(qi) * a.q_token + static_cast<int64_t>(qh) * a.q_head;
-                int e = 0;
-                float up = 1.f;
-                if constexpr (!std::is_same<T, __half>::value) {
-                    float big = 0.f;
-                    if (mine)
-                        for (int d = 0; d < D; d += 8) {
-                            alignas(16) T x[8];
-                            if (a.q_wide) *reinterpret_cast<uint4*>(x) = __ldg(reinterpret_cast<const uint4*>(q + d));
-                            else
-                                for (int i = 0; i < 8; ++i) x[i] = q[d + i];
+                uint32_t x[D / 2];
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) big = fmaxf(big, fabsf(Elem<T>::to_float(x[i])));
-                        }
-                    e = big > 0.f ? min(14 - (static_cast<int>(__float_as_uint(big) >> 23) - 127), 126) : 0;
-                    up = pow2(e);
-                }
-                if (a.scale < 0.f) up = -up;                 // so that the largest score is the largest product
-                factor = scale_pow2(fabsf(a.scale) * 1.4426950408889634f, c.k_exp - e);
-                const uint32_t base = sm + Plan::kQ + (kPair ? g : 0) * Plan::kTileBytes + row * 128;
-                const int d0 = kPair ? 0 : g * kPart;
-#pragma unroll 4
-                for (int d = d0; d < d0 + kPart; d += 8) {
-                    uint32_t y[4] = {0, 0, 0, 0};
-                    if (mine) {
-                        alignas(16) T x[8];
-                        if (a.q_wide) *reinterpret_cast<uint4*>(x) = __ldg(reinterpret_cast<const uint4*>(q + d));
-                        else
-                            for (int i = 0; i < 8; ++i) x[i] = q[d + i];
+                for (int d = 0; d < D; d += 8) {
+                    alignas(16) T y[8];
+                    if (mine && a.q_wide) {
+                        *reinterpret_cast<uint4*>(y) = __ldg(reinterpret_cast<const uint4*>(q + d));
+                    } else {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            if constexpr (std::is_same<T, __half>::value) y[i] = reinterpret_cast<const uint32_t*>(x)[i] ^ (up < 0.f ? 0x80008000u : 0u);
-                            else y[i] = pack_half2(Elem<T>::to_float(x[2 * i]) * up, Elem<T>::to_float(x[2 * i + 1]) * up);
-                        }
+                        for (int i = 0; i < 8; ++i) y[i] = mine ? q[d + i] : Elem<T>::from_float(0.f);
                     }
-                    const uint32_t at = base + (d >> 6) * Plan::kChunkBytes + ((((d & 63) >> 3) ^ (row & 7)) << 4);
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3]) : "memory");
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[d / 2 + i] = reinterpret_cast<const uint32_t*>(y)[i];
                 }
-                async_proxy_fence();
+                int e = 0;
+                if constexpr (!std::is_same<T, __half>::value) {
+                    auto lo = [](uint32_t w) { return __uint_as_float(w << 16); };
+                    auto hi = [](uint32_t w) { return __uint_as_float(w & 0xffff0000u); };
+                    float big = 0.f;
+#pragma unroll
+                    for (int i = 0; i < D / 2; ++i) big = fmaxf(big, fmaxf(fabsf(lo(x[i])), fabsf(hi(x[i]))));
+                    e = big > 0.f ? min(14 - (static_cast<int>(__float_as_uint(big) >> 23) - 127), 126) : 0;
+                    const float up = pow2(e);
+#pragma unroll
+                    for (int i = 0; i < D / 2; ++i) x[i] = pack_half2(lo(x[i]) * up, hi(x[i]) * up);
+                }
+                if (a.scale < 0.f) {                    // so that the largest score is the largest product
+#pragma unroll
+                    for (int i = 0; i < D / 2; ++i) x[i] ^= 0x80008000u;
+                }
+                factor = scale_pow2(fabsf(a.scale) * 1.4426950408889634f, c.k_exp - e);
+#pragma unroll
+                for (int i = 0; i < D / 2; i += 16) tmem_store16(lanes + kColQ + i, reinterpret_cast<const uint32_t(&)[16]>(x[i]));
+                tmem_store_wait();
+                tc_fence_before();
                 __syncwarp();
                 if (lane == 0) barrier_arrive(query_bar);
             }
@@ -348,158 +353,130 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
             uint32_t nan_blocks = 0;
 
             // ---- steps
-            const int first = kPair ? 0 : g, by = kPair ? 1 : 2;
-            for (int k = first; k < count; k += by) {
-                if (!wait(score_bar(g), n_score++ & 1)) return false;
+#pragma unroll 1
+            for (int k = 0; k < count; ++k, ++n) {
+                const uint32_t s_at = lanes + kColS + (n & 1) * 128;
+                if (!wait(score_bar(n & 1), (n >> 1) & 1)) return false;
                 tc_fence_after();
-                const int t0 = seg.ri.lo + (s0 + k) * kWideUnit, ring = (kt + k) & 3;
-                uint32_t on = *reinterpret_cast<volatile uint32_t*>(tile_there[ring]);
-                on = (on & 3) | (on >> 6 & 0xc) | (on >> 12 & 0x30) | (on >> 18 & 0xc0);
+                const int t0 = seg.ri.lo + (s0 + k) * kWideUnit, ring = n & 3;
+                const uint64_t on8 = *reinterpret_cast<volatile uint64_t*>(tile_there[ring]);
+                const uint32_t on = static_cast<uint32_t>(on8 * 0x0102040810204080ull >> 56);   // bytes of 0 or 1 -> bits
                 const bool all = seen_by_all(seg, t0);
                 const bool full = all && on == 0xff;
-                if (!all) {
-                    volatile uint32_t* flags = nan_flag[ring];
-                    if (flags[0] | flags[1] | flags[2] | flags[3])
+                // Weights with the reference at hand, in one pass: a sum of at most kTotalMax means that each of them is within fp16.
+                // Where that fails, and where there are masks, the step is done in two passes, the largest score first.
+                bool done = false;
+                if (full) {
+                    float2 total = make_float2(0.f, 0.f);
+                    uint32_t x[2][16], p[4][16];
+                    tmem_load16(s_at, x[0]);
+                    if (__any_sync(0xffffffffu, m == -INFINITY)) {   // a first reference from the first sixteen scores
+                        tmem_load_wait(x[0]);
+                        float top = -INFINITY;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) top = fmaxf(top, __uint_as_float(x[0][i]));
+                        if (m == -INFINITY) m = top * factor - kWideAbove;
+                    }
+                    const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) {
+                        uint32_t(&y)[16] = x[q & 1];
+                        tmem_load_wait(y);
+                        if (q < 7) tmem_load16(s_at + (q + 1) * 16, x[(q + 1) & 1]);
+#pragma unroll
+                        for (int i = 0; i < 16; i += 2) {
+                            float2 z = fma2(make_float2(__uint_as_float(y[i]), __uint_as_float(y[i + 1])), make_float2(factor, factor), make_float2(-ref, -ref));
+                            z.x = exp2_fast(z.x);
+                            z.y = exp2_fast(z.y);
+                            total = add2(total, z);
+                            p[q >> 1][(q & 1) * 8 + i / 2] = pack_half2(z.x, z.y);
+                        }
+                    }
+                    const float sum = total.x + total.y;
+                    done = !__any_sync(0xffffffffu, sum > kTotalMax);
+                    if (done) {
+                        l += sum;
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) tmem_store16(s_at + q * 16, p[q]);
+                    }
+                }
+                if (!done) {
+                    if (!all && *reinterpret_cast<volatile uint64_t*>(nan_flag[ring])) {
                         for (int t = 0; t < kWideUnit; ++t)
-                            if (flags[t >> 5] && t0 + t <= pos && (a.window == 0 || t0 + t > pos - a.window)) nan_blocks |= static_cast<volatile uint8_t*>(nan_block[ring])[t];
-                }
-                // Both passes over the scores (their largest; their weights) exist twice: without masks in one straight run, with the
-                // next 32 columns on the way, and with masks as a small loop - a run of masked code does not fit the instruction cache.
-                auto seen = [&](int t) { return ((on >> (t >> 4)) & 1) && t0 + t <= pos && (a.window == 0 || t0 + t > pos - a.window); };
-                float top = -INFINITY;
-                uint32_t x[2][32];
-                if (full) {
-                    tmem_load32(s_at, x[0]);
-#pragma unroll 1
-                    for (int q = 0; q < 128; q += 64) {
-                        tmem_load_wait(x[0]);
-                        tmem_load32(s_at + q + 32, x[1]);
-#pragma unroll
-                        for (int i = 0; i < 32; i += 2) top = fmaxf(fmaxf(top, __uint_as_float(x[0][i])), __uint_as_float(x[0][i + 1]));
-                        tmem_load_wait(x[1]);
-                        tmem_load32(s_at + (q ^ 64), x[0]);          // the last one is the first of the second pass
-#pragma unroll
-                        for (int i = 0; i < 32; i += 2) top = fmaxf(fmaxf(top, __uint_as_float(x[1][i])), __uint_as_float(x[1][i + 1]));
+                            if (static_cast<volatile uint8_t*>(nan_flag[ring])[t >> 4] && t0 + t <= pos && (a.window == 0 || t0 + t > pos - a.window))
+                                nan_blocks |= static_cast<volatile uint8_t*>(nan_block[ring])[t];
                     }
-                } else {
-#pragma unroll 1
-                    for (int q = 0; q < 4; ++q) {
-                        tmem_load32(s_at + q * 32, x[0]);
-                        tmem_load_wait(x[0]);
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) top = fmaxf(top, seen(q * 32 + i) ? __uint_as_float(x[0][i]) : -INFINITY);
-                    }
-                }
-                top *= factor;
-                if (__any_sync(0xffffffffu, top > m + kRaiseAt)) {
-                    const float to = top > m + kRaiseAt ? top - kAbove : m;
-                    const float keep = m == -INFINITY ? 0.f : exp2_fast(m - to);
-                    if (k >= first + by) {               // the sums so far; the group's last product is complete (it came before these scores)
-#pragma unroll 1
-                        for (int q = 0; q < D / 16; ++q) {
-                            uint32_t o[16];
-                            tmem_load16(o_at + q * 16, o);
-                            tmem_load_wait(o);
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * keep);
-                            tmem_store16(o_at + q * 16, o);
-                        }
-                    }
-                    l *= keep;
-                    m = to;
-                }
-                const float ref = m == -INFINITY ? 0.f : m;
-                float2 total = make_float2(0.f, 0.f);
-                if (full) {
-                    auto weights = [&](const uint32_t (&s)[32], int at) {
-                        uint32_t p[16];
-#pragma unroll
-                        for (int i = 0; i < 32; i += 2) {
-                            float2 y = fma2(make_float2(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), make_float2(factor, factor), make_float2(-ref, -ref));
-                            y.x = exp2_fast(y.x);
-                            y.y = exp2_fast(y.y);
-                            total = add2(total, y);
-                            p[i / 2] = pack_half2(y.x, y.y);
-                        }
-                        tmem_store16(s_at + at, p);                  // behind the scores that are still to be read
+                    // which of 32 columns a row sees, as bits
+                    const int from = a.window > 0 ? max(pos - a.window + 1 - t0, 0) : 0, to_col = min(pos - t0, kWideUnit - 1);
+                    auto seen = [&](int q) -> uint32_t {
+                        const int lo = max(from - q * 32, 0), hi = to_col - q * 32;
+                        uint32_t bits = hi < 0 || lo > 31 ? 0u : (0xffffffffu >> (31 - min(hi, 31))) & (0xffffffffu << lo);
+                        if (!((on >> (2 * q)) & 1)) bits &= 0xffff0000u;
+                        if (!((on >> (2 * q)) & 2)) bits &= 0x0000ffffu;
+                        return full ? 0xffffffffu : bits;
                     };
-#pragma unroll 1
-                    for (int q = 0; q < 128; q += 64) {
-                        tmem_load_wait(x[0]);
-                        tmem_load32(s_at + q + 32, x[1]);
-                        weights(x[0], q / 2);
-                        tmem_load_wait(x[1]);
-                        if (q == 0) tmem_load32(s_at + 64, x[0]);
-                        weights(x[1], q / 2 + 16);
-                    }
-                } else {
+                    uint32_t x[32];
+                    float top = -INFINITY;
 #pragma unroll 1
                     for (int q = 0; q < 4; ++q) {
-                        tmem_load32(s_at + q * 32, x[0]);
-                        tmem_load_wait(x[0]);
+                        tmem_load32(s_at + q * 32, x);
+                        tmem_load_wait(x);
+                        const uint32_t bits = seen(q);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) top = fmaxf(top, (bits >> i) & 1 ? __uint_as_float(x[i]) : -INFINITY);
+                    }
+                    top *= factor;
+                    if (__any_sync(0xffffffffu, top > m + kWideAbove)) {
+                        const float to = top > m + kWideAbove ? top - kWideAbove : m;
+                        const float keep = m == -INFINITY ? 0.f : exp2_fast(m - to);
+                        if (k > 0) {                     // the sums so far
+                            if (!products(n)) return false;
+#pragma unroll 1
+                            for (int q = 0; q < D / 16; ++q) {
+                                uint32_t o[16];
+                                tmem_load16(lanes + kColO + q * 16, o);
+                                tmem_load_wait(o);
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * keep);
+                                tmem_store16(lanes + kColO + q * 16, o);
+                            }
+                        }
+                        l *= keep;
+                        m = to;
+                    }
+                    const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll 1
+                    for (int q = 0; q < 4; ++q) {
+                        tmem_load32(s_at + q * 32, x);
+                        tmem_load_wait(x);
+                        const uint32_t bits = seen(q);
                         uint32_t p[16];
 #pragma unroll
                         for (int i = 0; i < 32; i += 2) {
-                            float2 y = make_float2(fmaf(__uint_as_float(x[0][i]), factor, -ref), fmaf(__uint_as_float(x[0][i + 1]), factor, -ref));
-                            y.x = exp2_fast(seen(q * 32 + i) ? y.x : -INFINITY);
-                            y.y = exp2_fast(seen(q * 32 + i + 1) ? y.y : -INFINITY);
-                            total = add2(total, y);
-                            p[i / 2] = pack_half2(y.x, y.y);
+                            const float y0 = fmaf(__uint_as_float(x[i]), factor, -ref), y1 = fmaf(__uint_as_float(x[i + 1]), factor, -ref);
+                            const float e0 = exp2_fast((bits >> i) & 1 ? y0 : -INFINITY), e1 = exp2_fast((bits >> i) & 2 ? y1 : -INFINITY);
+                            l += e0 + e1;
+                            p[i / 2] = pack_half2(e0, e1);
                         }
-                        tmem_store16(s_at + q * 16, p);
+                        tmem_store16(s_at + q * 16, p);      // behind the scores that are still to be read
                     }
                 }
-                l += total.x + total.y;
                 tmem_store_wait();
+                if (!products(n)) return false;          // one at a time is under way; the one before is long done here
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) barrier_arrive(weight_bar(g));
+                if (lane == 0) barrier_arrive(weight_bar);
             }
-            kt += count;
 
             // ---- the piece's result
-            const bool worked = first < count;
-            if (worked) {
-                if (!wait(score_bar(g), n_score++ & 1)) return false;
-                tc_fence_after();
-            }
+            if (!products(n)) return false;
             const bool begins = s0 == 0, ends = s0 + count == seg.steps;
-            float m2 = -INFINITY, w1 = 1.f, w2 = 0.f, top = m, tot = l;
-            bool have1 = true, have2 = false;
-            if (!kPair) {
-                stats[g][row] = make_float2(m, l);
-                stat_nan[g][row] = nan_blocks;
-                if (!both()) return false;
-                tc_fence_after();
-                const float2 s1 = stats[0][row], s2 = stats[1][row];
-                nan_blocks = stat_nan[0][row] | stat_nan[1][row];
-                m2 = s2.x;
-                top = fmaxf(s1.x, m2);
-                w1 = join_weight(s1.x, top);
-                w2 = join_weight(m2, top);
-                tot = w1 * s1.y + w2 * s2.y;
-                have2 = count > 1;
-            }
-            (void)have1;
-            const uint32_t o1 = tmem + quarter_lane + 256 + (kPair ? g * 128 : 0), o2 = tmem + quarter_lane + 256 + 128;
-            constexpr int kCols = kPair ? D : D / 2;
-            const int col0 = kPair ? 0 : g * kCols;
-            // sums of 32 channels
-            auto sums = [&](int col, float (&y)[32]) {
+            auto sums = [&](int col, float (&y)[32]) {  // 32 channels
                 uint32_t x[32];
-                tmem_load32(o1 + col, x);
+                tmem_load32(lanes + kColO + col, x);
                 tmem_load_wait(x);
 #pragma unroll
-                for (int i = 0; i < 32; ++i) y[i] = kPair ? __uint_as_float(x[i]) : __uint_as_float(x[i]) * w1;
-                if (have2) {
-                    tmem_load32(o2 + col, x);
-                    tmem_load_wait(x);
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) y[i] += __uint_as_float(x[i]) * w2;
-                }
-#pragma unroll
-                for (int i = 0; i < 32; ++i)
-                    if ((nan_blocks >> ((col + i) >> 4)) & 1) y[i] = __int_as_float(0x7fffffff);
+                for (int i = 0; i < 32; ++i) y[i] = (nan_blocks >> ((col + i) >> 4)) & 1 ? __int_as_float(0x7fffffff) : __uint_as_float(x[i]);
             };
             auto finish = [&](int col, float (&y)[32], float m_all, float l_all) {
                 const float f = finish_factor(l_all, c.v_exp);
@@ -510,56 +487,52 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
             };
             if (begins && ends) {
 #pragma unroll 1
-                for (int col = col0; col < col0 + kCols; col += 32) {
+                for (int col = 0; col < D; col += 32) {
                     float y[32];
                     sums(col, y);
-                    if (mine) finish(col, y, top, tot);
+                    if (mine) finish(col, y, m, l);
                 }
             } else {
                 // [D / 4][128] float4, then references and totals
-                auto part = [&](int owner, bool first_piece) {
-                    return a.partials + (2ll * owner + first_piece) * Plan::kPart + (kPair ? g * Plan::kPartTile : 0);
-                };
+                auto part = [&](int owner, bool first_piece) { return a.partials + (2ll * owner + first_piece) * Plan::kPart; };
                 float* out = part(cta, begins);
 #pragma unroll 1
-                for (int col = col0; col < col0 + kCols; col += 32) {
+                for (int col = 0; col < D; col += 32) {
                     float y[32];
                     sums(col, y);
 #pragma unroll
                     for (int i = 0; i < 32; i += 4)
                         reinterpret_cast<float4*>(out)[((col + i) >> 2) * 128 + row] = make_float4(y[i], y[i + 1], y[i + 2], y[i + 3]);
                 }
-                if (col0 == 0) {
-                    out[128 * D + row] = top;
-                    out[128 * D + 128 + row] = tot;
-                }
+                out[128 * D + row] = m;
+                out[128 * D + 128 + row] = l;
                 __threadfence();
-                if (!both()) return false;
+                if (!meet()) return false;
                 const int c0 = shares.owner(seg.begin), c1 = shares.owner(seg.begin + seg.steps - 1);
                 if (tid == 0) {
                     last_here = atomicAdd(&a.counters[c0], 1) == c1 - c0;
                     if (last_here) a.counters[c0] = 0;
                     __threadfence();
                 }
-                if (!both()) return false;
+                if (!meet()) return false;
                 if (*static_cast<volatile int*>(&last_here)) {
                     __threadfence();
-                    const int n = c1 - c0 + 1;
+                    const int parts = c1 - c0 + 1;
                     float m_all = -INFINITY, l_all = 0.f;
 #pragma unroll 4
-                    for (int i = 0; i < n; ++i) m_all = fmaxf(m_all, __ldcg(part(c0 + i, i == 0) + 128 * D + row));
+                    for (int i = 0; i < parts; ++i) m_all = fmaxf(m_all, __ldcg(part(c0 + i, i == 0) + 128 * D + row));
 #pragma unroll 4
-                    for (int i = 0; i < n; ++i) {
+                    for (int i = 0; i < parts; ++i) {
                         const float* p = part(c0 + i, i == 0) + 128 * D + row;
                         l_all += join_weight(__ldcg(p), m_all) * __ldcg(p + 128);
                     }
 #pragma unroll 1
-                    for (int col = col0; col < col0 + kCols; col += 32) {
+                    for (int col = 0; col < D; col += 32) {
                         float y[32];
 #pragma unroll
                         for (int i = 0; i < 32; ++i) y[i] = 0.f;
-#pragma unroll 1
-                        for (int i = 0; i < n; ++i) {
+#pragma unroll 2
+                        for (int i = 0; i < parts; ++i) {
                             const float* p = part(c0 + i, i == 0);
                             const float wt = join_weight(__ldcg(p + 128 * D + row), m_all);
 #pragma unroll
@@ -574,20 +547,20 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                         if (mine) finish(col, y, m_all, l_all);
                     }
                 }
+                if (!meet()) return false;                // `last_here` is free again
             }
-            // the next piece writes the queries and the sums anew: both groups are through with these
             tc_fence_before();
-            return both();
+            return true;
         });
-    } else if (warp < 16) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-        // ================= expanding warps: 4-bit tiles -> fp16 operands; four warps for the keys, four for the values
-        // A warp takes two tiles of a step and brings them itself, a few steps ahead, into slots of its own (sixteen bytes a thread and
+    } else if (warp < 20) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        // ================= expanding warps: 4-bit tiles -> fp16 operands; eight warps for the keys, eight for the values
+        // A warp takes one tile of a step and brings it itself, a few steps ahead, into slots of its own (sixteen bytes a thread and
         // copy: a bulk copy costs some 100 clocks to issue, however small).  A thread expands a quarter of the channels of tokens
         // lane / 4 and + 8: its reads are contiguous over the warp, and with the words of the upper two quarters swapped its writes
         // fall into eight different 16-byte columns of the swizzled rows.
         const bool values = warp >= 12;
-        const int w = warp & 3, tok = lane >> 2, quarter = lane & 3;
+        const int w = (warp - 4) & 7, tok = lane >> 2, quarter = lane & 3;
         constexpr int QB = D / 8;                          // bytes of codes of a quarter
         constexpr int QW = D / 32;                         // words
         constexpr int R = Plan::kRawSlots;
@@ -596,38 +569,34 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
 #pragma unroll
         for (int k = 0; k < QW; ++k) {
             const int col = quarter * QW + (swap ? k ^ 2 : k);
-            column[k] = sm + (values ? Plan::kV : Plan::kK) + (col >> 3) * Plan::kChunkBytes + (w * 32 + tok) * 128 + (((col & 7) ^ tok) << 4);
+            column[k] = sm + (values ? Plan::kV : Plan::kK) + (col >> 3) * Plan::kChunkBytes + (w * 16 + tok) * 128 + (((col & 7) ^ tok) << 4);
         }
-        const uint32_t raw = sm + Plan::kRaw + (warp - 8) * R * Plan::kRawHalf;
+        const uint32_t raw = sm + Plan::kRaw + (warp - 4) * R * Plan::kRawHalf;
         const uint32_t codes_at = raw + tok * (D / 2) + quarter * QB, scales_at = raw + 8 * D + (D == 128 ? tok * 8 + quarter * 2 : tok * 4 + quarter);
         constexpr int kCodeParts = 8 * D / 512;            // warp-wide copies of a tile's codes
         constexpr int kScaleLanes = D / 16;                // sixteen-byte parts of a tile's scales
         uint32_t n = 0;                                    // halves expanded so far
         for_pieces([&](const WideSegment& g, int s0, int count) {
             const uint8_t* const head = c.head_tiles(0, a.layer, g.head) + (values ? 8 * D : 0);
-            // pages of the warp's tiles of sixteen steps: lane = 2 * (step - page_base) + tile
-            int page_base = s0, page_of = -1, slot = 0;
-            uint32_t present = 0;                          // two bits per slot
-            auto fill = [&](int step) {                    // the step's tiles into the slot, if it is one of ours
+            int page_base = s0, page_of = -1, slot = 0;    // pages of the warp's tiles of 32 steps: lane = step - page_base
+            uint32_t present = 0;                          // a bit per slot
+            auto fill = [&](int step) {                    // the step's tile into the slot, if it is one of ours
                 if (step < s0 + count) {
-                    if (step - page_base >= 16 || step == s0) {
+                    if (step - page_base >= 32 || step == s0) {
                         page_base = step;
-                        const int t = g.ri.lo + (step + (lane >> 1)) * kWideUnit + (w * 2 + (lane & 1)) * 16;
+                        const int t = g.ri.lo + (step + lane) * kWideUnit + w * 16;
                         page_of = t < g.ri.hi && t >= 0 ? c.page_at(g.ri.s, t >> c.log_p) : -1;
                     }
-                    const int t0 = g.ri.lo + step * kWideUnit + w * 32;
-                    const uint32_t dst = raw + slot * Plan::kRawHalf + lane * 16;
-                    present &= ~(3u << (2 * slot));
+                    const int page = __shfl_sync(0xffffffffu, page_of, step - page_base);
+                    present &= ~(1u << slot);
+                    if (page >= 0) {
+                        present |= 1u << slot;
+                        const int t = g.ri.lo + step * kWideUnit + w * 16;
+                        const uint32_t dst = raw + slot * Plan::kRawHalf + lane * 16;
+                        const uint8_t* src = head + page * c.page_bytes + ((t & (c.page_tokens() - 1)) >> 4) * (18 * D) + lane * 16;
 #pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        const int page = __shfl_sync(0xffffffffu, page_of, 2 * (step - page_base) + x);
-                        if (page < 0) continue;
-                        present |= 1u << (2 * slot + x);
-                        const uint8_t* src = head + page * c.page_bytes + (((t0 + x * 16) & (c.page_tokens() - 1)) >> 4) * (18 * D) + lane * 16;
-#pragma unroll
-                        for (int y = 0; y < kCodeParts; ++y) async_copy16(dst + x * (9 * D) + y * 512, src + y * 512);
-                        // scales: D bytes, 8 D (values) or 15 D further on for keys
-                        if (lane < kScaleLanes) async_copy16(dst + x * (9 * D) + 8 * D, src + (values ? 9 * D : 16 * D));
+                        for (int y = 0; y < kCodeParts; ++y) async_copy16(dst + y * 512, src + y * 512);
+                        if (lane < kScaleLanes) async_copy16(dst + 8 * D, src + (values ? 9 * D : 16 * D));
                     }
                 }
                 asm volatile("cp.async.commit_group;" ::: "memory");
@@ -640,29 +609,29 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                 asm volatile("cp.async.wait_group %0;" ::"n"(R - 1) : "memory");
                 __syncwarp();
                 const int stage = n & 1;
-                const uint32_t there = present >> (2 * slot);
-                uint32_t codes[4][QW], scales[4];
+                const bool there = (present >> slot) & 1;
+                uint32_t codes[2][QW], scales[2];
 #pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    const uint32_t at = slot * Plan::kRawHalf + (x >> 1) * (9 * D);
-                    lds_words<QW>(at + codes_at + (x & 1) * 8 * (D / 2), codes[x]);
+                for (int x = 0; x < 2; ++x) {
+                    const uint32_t at = slot * Plan::kRawHalf;
+                    lds_words<QW>(at + codes_at + x * 8 * (D / 2), codes[x]);
                     if constexpr (D == 128) {
                         uint16_t y;
-                        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(y) : "r"(at + scales_at + (x & 1) * 64));
+                        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(y) : "r"(at + scales_at + x * 64));
                         scales[x] = y;
                     } else {
-                        scales[x] = lds8(at + scales_at + (x & 1) * 32);
+                        scales[x] = lds8(at + scales_at + x * 32);
                     }
                 }
                 __syncwarp();
                 fill(s0 + k + R);
                 if (++slot == R) slot = 0;
                 if (n >= 2 && !wait(values ? v_empty(stage) : k_empty(stage), ((n >> 1) - 1) & 1)) return false;
-                const int t0 = g.ri.lo + (s0 + k) * kWideUnit + w * 32;
+                const int t0 = g.ri.lo + (s0 + k) * kWideUnit + w * 16;
                 const bool all = seen_by_all(g, g.ri.lo + (s0 + k) * kWideUnit);
 #pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    uint32_t s = (there >> (x >> 1)) & 1 ? scales[x] : 0;
+                for (int x = 0; x < 2; ++x) {
+                    uint32_t s = there ? scales[x] : 0;
                     if (values && !all) {   // what is masked must not be multiplied with
                         if (t0 + x * 8 + tok >= g.ri.hi) s = 0;
                         if ((s & 0x7f) == 0x7f) s &= 0xff00;
@@ -682,35 +651,32 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                 }
                 if (!values) {
                     const int ring = n & 3;
-                    uint32_t flagged = 0;
+                    if (lane == 0) tile_there[ring][w] = there;
                     if (!all) {
                         // NaN among the values of these tokens, for the rows that do see them
                         uint32_t nans = 0;
 #pragma unroll 1
-                        for (int x = 0; x < 4; ++x) {
+                        for (int x = 0; x < 2; ++x) {
                             const int t = t0 + x * 8 + tok;
-                            if (!((there >> (x >> 1)) & 1) || t >= g.ri.hi) continue;
+                            if (!there || t >= g.ri.hi) continue;
                             const uint8_t* z = c.tile(c.page_at(g.ri.s, t >> c.log_p), a.layer, g.head, t & (c.page_tokens() - 1)) + 17 * D +
-                                               ((x & 1) * 8 + tok) * (D / 16) + (D == 128 ? quarter * 2 : quarter);
+                                               (x * 8 + tok) * (D / 16) + (D == 128 ? quarter * 2 : quarter);
                             const uint32_t s = D == 128 ? __ldg(reinterpret_cast<const uint16_t*>(z)) : __ldg(z);
                             if ((s & 0x7f) == 0x7f) nans |= 1u << (2 * x);
                             if (D == 128 && (s & 0x7f00) == 0x7f00) nans |= 2u << (2 * x);
                         }
-                        flagged = __ballot_sync(0xffffffffu, nans != 0);
+                        const uint32_t flagged = __ballot_sync(0xffffffffu, nans != 0);
                         if (flagged) {
 #pragma unroll 1
-                            for (int x = 0; x < 4; ++x) {
+                            for (int x = 0; x < 2; ++x) {
                                 // blocks of a quarter: two at 128 channels, one at 64
                                 uint32_t m = D == 128 ? ((nans >> (2 * x)) & 3) << (2 * quarter) : ((nans >> (2 * x)) & 1) << quarter;
                                 m |= __shfl_xor_sync(0xffffffffu, m, 1);
                                 m |= __shfl_xor_sync(0xffffffffu, m, 2);
-                                if (quarter == 0) nan_block[ring][w * 32 + x * 8 + tok] = static_cast<uint8_t>(m);
+                                if (quarter == 0) nan_block[ring][w * 16 + x * 8 + tok] = static_cast<uint8_t>(m);
                             }
                         }
-                    }
-                    if (lane == 0) {
-                        nan_flag[ring][w] = flagged;
-                        tile_there[ring][w] = static_cast<uint8_t>(there & 3);
+                        if (lane == 0) nan_flag[ring][w] = flagged != 0;
                     }
                 }
                 async_proxy_fence();
@@ -720,47 +686,40 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
             return true;
         });
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-        if (warp == 16) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        if (warp == 20) {
         // ================= issuing warp
         if (lane == 0) {
             constexpr uint32_t kScoreDesc = product_desc(128, 128, false), kSumDesc = product_desc(128, D, true);
-            const uint64_t q_desc = operand_desc(sm + Plan::kQ, 16, 1024), k_desc = operand_desc(sm + Plan::kK, 16, 1024);
-            const uint64_t v_desc = operand_desc(sm + Plan::kV, Plan::kChunkBytes, 1024);
-            uint32_t kt = 0, vt = 0, n_query = 0, n_weight[2] = {0, 0};
+            const uint64_t k_desc = operand_desc(sm + Plan::kK, 16, 1024), v_desc = operand_desc(sm + Plan::kV, Plan::kChunkBytes, 1024);
+            uint32_t n = 0, n_query = 0;                 // steps in earlier pieces
             for_pieces([&](const WideSegment&, int, int count) {
-                const int jobs = kPair ? 2 * count : count;
-                if (!wait(query_bar, n_query++ & 1)) return false;
-                tc_fence_after();
-                auto scores = [&](int n) -> bool {      // S of job n
-                    const int g = n & 1, tile = kPair ? n >> 1 : n, stage = (kt + tile) & 1;
-                    if ((!kPair || g == 0) && !wait(k_full(stage), ((kt + tile) >> 1) & 1)) return false;
+                auto scores = [&](uint32_t i) -> bool {  // S of step i
+                    const int stage = i & 1;
+                    if (!wait(k_full(stage), (i >> 1) & 1)) return false;
                     tc_fence_after();
-                    const uint64_t q = q_desc + (kPair ? g : 0) * (Plan::kTileBytes >> 4), k = k_desc + stage * (Plan::kTileBytes >> 4);
+                    const uint64_t k = k_desc + stage * (Plan::kTileBytes >> 4);
 #pragma unroll
-                    for (int i = 0; i < D / 16; ++i) {
-                        const uint32_t off = ((i >> 2) * Plan::kChunkBytes + (i & 3) * 32) >> 4;
-                        tc_mma_ss(tmem + g * 128, q + off, k + off, kScoreDesc, i > 0);
-                    }
-                    tc_commit(score_bar(g));
-                    if (!kPair || g == 1) tc_commit(k_empty(stage));
+                    for (int x = 0; x < D / 16; ++x)
+                        tc_mma_ts(tmem + kColS + stage * 128, tmem + kColQ + x * 8, k + (((x >> 2) * Plan::kChunkBytes + (x & 3) * 32) >> 4), kScoreDesc, x > 0);
+                    tc_commit(score_bar(stage));
+                    tc_commit(k_empty(stage));
                     return true;
                 };
-                if (!scores(0)) return false;
-                for (int n = 0; n < jobs; ++n) {
-                    if (n + 1 < jobs && !scores(n + 1)) return false;
-                    const int g = n & 1, tile = kPair ? n >> 1 : n, stage = (vt + tile) & 1;
-                    if ((!kPair || g == 0) && !wait(v_full(stage), ((vt + tile) >> 1) & 1)) return false;
-                    if (!wait(weight_bar(g), n_weight[g]++ & 1)) return false;
+                if (!wait(query_bar, n_query++ & 1)) return false;
+                if (!scores(n) || (count > 1 && !scores(n + 1))) return false;
+#pragma unroll 1
+                for (int k = 0; k < count; ++k, ++n) {
+                    const int stage = n & 1;
+                    if (!wait(v_full(stage), (n >> 1) & 1) || !wait(weight_bar, n & 1)) return false;
                     tc_fence_after();
                     const uint64_t v = v_desc + stage * (Plan::kTileBytes >> 4);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) tc_mma_ts(tmem + 256 + g * 128, tmem + g * 128 + i * 8, v + i * (2048 >> 4), kSumDesc, n > 1 || i > 0);
-                    if (!kPair || g == 1) tc_commit(v_empty(stage));
-                    if (n + 2 >= jobs) tc_commit(score_bar(g));   // the group's last: its sums are complete
+                    for (int x = 0; x < 8; ++x) tc_mma_ts(tmem + kColO, tmem + kColS + stage * 128 + x * 8, v + x * (2048 >> 4), kSumDesc, k > 0 || x > 0);
+                    tc_commit(v_empty(stage));
+                    tc_commit(product_bar);
+                    if (k + 2 < count && !scores(n + 2)) return false;
                 }
-                kt += count;
-                vt += count;
                 return true;
             });
         }
@@ -770,7 +729,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == 16) tmem_free(tmem, 512);
+    if (warp == 20) tmem_free(tmem, 512);
     if (tid == 0 && abort_flag && c.meta) atomicOr(&c.meta[1], kStatusGaveUp);
 }
 

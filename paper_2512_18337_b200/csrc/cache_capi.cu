@@ -105,7 +105,7 @@ constexpr int64_t kNarrowRows = 16;   // query rows per key/value head up to whi
 template <int D>
 int64_t partial_bytes(int64_t rows) {
     if (rows <= kNarrowRows) return 2ll * kMaxCtas * 4 * StreamPlan<D, 2>::kPiece;
-    return 2ll * kWideMaxCtas * 4 * (rows <= 128 ? WidePlan<D, false>::kPart : WidePlan<D, true>::kPart);
+    return 2ll * kWideMaxCtas * 4 * WidePlan<D>::kPart;
 }
 
 template <typename T, int D, int NT>
@@ -116,11 +116,11 @@ int launch_stream(const AttendArgs& a, int sms, cudaStream_t s) {
     return launched();
 }
 
-template <typename T, int D, bool kPair>
+template <typename T, int D>
 int launch_wide(const AttendArgs& a, int sms, cudaStream_t s) {
-    using Plan = WidePlan<D, kPair>;
-    SAM_CUDA(cudaFuncSetAttribute(attend_wide_kernel<T, D, kPair>, cudaFuncAttributeMaxDynamicSharedMemorySize, Plan::kSmem));
-    attend_wide_kernel<T, D, kPair><<<std::min(sms, kWideMaxCtas), kWideThreads, Plan::kSmem, s>>>(a);
+    using Plan = WidePlan<D>;
+    SAM_CUDA(cudaFuncSetAttribute(attend_wide_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Plan::kSmem));
+    attend_wide_kernel<T, D><<<std::min(sms, kWideMaxCtas), kWideThreads, Plan::kSmem, s>>>(a);
     return launched();
 }
 
@@ -131,7 +131,7 @@ int launch_attend(const AttendArgs& a, cudaStream_t s) {
     const int64_t rows = static_cast<int64_t>(a.Q) * a.group;
     if (rows <= 8) return launch_stream<T, D, 1>(a, di.sms, s);
     if (rows <= kNarrowRows) return launch_stream<T, D, 2>(a, di.sms, s);
-    return rows <= 128 ? launch_wide<T, D, false>(a, di.sms, s) : launch_wide<T, D, true>(a, di.sms, s);
+    return launch_wide<T, D>(a, di.sms, s);
 }
 
 }  // namespace
