@@ -1,6 +1,6 @@
 // Attention for many query rows per key/value head (proposals of several heads, prompt chunks): tcgen05 products.
 //
-// S = Q K^T and O += P V on a tile of 128 query rows, with 128 tokens a step.  Sixteen warps expand the 4-bit tiles into two stages
+// S = Q K^T and O += P V on a tile of 128 query rows, with 128 tokens a step.  Eight warps expand the 4-bit tiles into two stages
 // of fp16 keys and two of fp16 values in shared memory (exact: a value has six significant bits).  Q, two tiles of scores and the
 // sums O lie in tensor memory.  A thread of the four softmax warps owns one query row, so its maximum and its sum need no exchange;
 // it writes P as fp16 over S, from where the second product takes it.  While it works on one step's scores, the products of the
@@ -27,7 +27,7 @@ namespace samb200 {
 
 constexpr int kWideUnit = 128;                     // tokens of a step
 constexpr int kWideRows = 128;                     // query rows of a segment
-constexpr int kWideWarps = 24, kWideThreads = kWideWarps * 32;   // four softmax warps, sixteen expanding ones, an issuing one (and three that idle)
+constexpr int kWideWarps = 16, kWideThreads = kWideWarps * 32;   // four softmax warps, eight expanding ones, an issuing one (and three that idle)
 constexpr int kWideMaxCtas = 160;
 constexpr float kWideAbove = 8.f, kTotalMax = 32768.f;   // 128 weights of 2^8 add up to no more
 // columns of tensor memory
@@ -38,9 +38,9 @@ struct WidePlan {
     static constexpr int kTileBytes = 128 * D * 2;                      // a [128][D] fp16 operand
     static constexpr int kChunkBytes = 128 * 128;                       // 64 channels of it
     static constexpr int kK = 0, kV = 2 * kTileBytes;
-    static constexpr int kRaw = kV + 2 * kTileBytes;                    // slots of the expanding warps: a tile's keys or values each
-    static constexpr int kRawSlots = 3, kRawHalf = 9 * D;
-    static constexpr int kSmem = kRaw + 16 * kRawSlots * kRawHalf + 1024;   // and room to start on a 1024-byte boundary
+    static constexpr int kRaw = kV + 2 * kTileBytes;                    // slots of the expanding warps: two tiles' keys or values each
+    static constexpr int kRawSlots = 3, kRawHalf = 18 * D;
+    static constexpr int kSmem = kRaw + 8 * kRawSlots * kRawHalf + 1024;   // and room to start on a 1024-byte boundary
     static constexpr int kPart = 128 * D + 2 * 128;                     // floats of a partial result
 };
 
@@ -155,8 +155,8 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
     __shared__ uint64_t bars[14];
     __shared__ uint32_t tmem_base;
     __shared__ int64_t scan[kWideWarps], start_e, start_begin;
-    __shared__ alignas(8) uint8_t tile_there[4][8];    // per step (mod 4): which of its eight tiles are there
-    __shared__ alignas(8) uint8_t nan_flag[4][8];      // NaN among the values of a tile's tokens (written where there are masks)
+    __shared__ alignas(4) uint8_t tile_there[4][4];    // per step (mod 4) and expanding warp: which of its two tiles are there
+    __shared__ alignas(4) uint8_t nan_flag[4][4];      // NaN among the values of the warp's tokens (written where there are masks)
     __shared__ uint8_t nan_block[4][128];              // which 16-channel blocks of a token's values are NaN
     __shared__ int last_here;
     __shared__ volatile int abort_flag;
@@ -184,9 +184,9 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
             barrier_init(score_bar(i), 1);
-            barrier_init(k_full(i), 8);
+            barrier_init(k_full(i), 4);
             barrier_init(k_empty(i), 1);
-            barrier_init(v_full(i), 8);
+            barrier_init(v_full(i), 4);
             barrier_init(v_empty(i), 1);
         }
         barrier_init(weight_bar, 4);
@@ -250,7 +250,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
     }
     clear_unused_rows<T, D>(a, cta, gridDim.x);
     if (!busy) return;
-    if (warp == 20) tmem_alloc(shared_addr(&tmem_base), 512);
+    if (warp == 12) tmem_alloc(shared_addr(&tmem_base), 512);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -285,9 +285,9 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
         return t0 + kWideUnit - 1 <= g.first_pos && (a.window == 0 || t0 > g.last_pos - a.window);
     };
 
-    // Registers go where they are needed: 128 threads x 168, 512 x 56, 128 x 72, of 768 x 80 at launch.
+    // Registers go where they are needed: 128 threads x 200, 256 x 88, 128 x 72, of 512 x 128 at launch.
     if (warp < 4) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         // ================= softmax warps
         const int row = tid;
         const uint32_t lanes = tmem + (static_cast<uint32_t>(warp) << 21);   // the warp's quarter of the lanes
@@ -359,8 +359,8 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                 if (!wait(score_bar(n & 1), (n >> 1) & 1)) return false;
                 tc_fence_after();
                 const int t0 = seg.ri.lo + (s0 + k) * kWideUnit, ring = n & 3;
-                const uint64_t on8 = *reinterpret_cast<volatile uint64_t*>(tile_there[ring]);
-                const uint32_t on = static_cast<uint32_t>(on8 * 0x0102040810204080ull >> 56);   // bytes of 0 or 1 -> bits
+                uint32_t on = *reinterpret_cast<volatile uint32_t*>(tile_there[ring]);
+                on = (on * 0x01041040u) >> 24;            // two bits of each byte, side by side
                 const bool all = seen_by_all(seg, t0);
                 const bool full = all && on == 0xff;
                 // Weights with the reference at hand, in one pass: a sum of at most kTotalMax means that each of them is within fp16.
@@ -401,9 +401,9 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                     }
                 }
                 if (!done) {
-                    if (!all && *reinterpret_cast<volatile uint64_t*>(nan_flag[ring])) {
+                    if (!all && *reinterpret_cast<volatile uint32_t*>(nan_flag[ring])) {
                         for (int t = 0; t < kWideUnit; ++t)
-                            if (static_cast<volatile uint8_t*>(nan_flag[ring])[t >> 4] && t0 + t <= pos && (a.window == 0 || t0 + t > pos - a.window))
+                            if (static_cast<volatile uint8_t*>(nan_flag[ring])[t >> 5] && t0 + t <= pos && (a.window == 0 || t0 + t > pos - a.window))
                                 nan_blocks |= static_cast<volatile uint8_t*>(nan_block[ring])[t];
                     }
                     // which of 32 columns a row sees, as bits
@@ -552,115 +552,131 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
             tc_fence_before();
             return true;
         });
-    } else if (warp < 20) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-        // ================= expanding warps: 4-bit tiles -> fp16 operands; eight warps for the keys, eight for the values
-        // A warp takes one tile of a step and brings it itself, a few steps ahead, into slots of its own (sixteen bytes a thread and
+    } else if (warp < 12) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        // ================= expanding warps: 4-bit tiles -> fp16 operands; four warps for the keys, four for the values
+        // A warp takes two tiles of a step and brings them itself, a few steps ahead, into slots of its own (sixteen bytes a thread and
         // copy: a bulk copy costs some 100 clocks to issue, however small).  A thread expands a quarter of the channels of tokens
-        // lane / 4 and + 8: its reads are contiguous over the warp, and with the words of the upper two quarters swapped its writes
+        // lane / 4 and + 8: its reads are contiguous over the warp, and with the halves of the upper two quarters swapped its writes
         // fall into eight different 16-byte columns of the swizzled rows.
-        const bool values = warp >= 12;
-        const int w = (warp - 4) & 7, tok = lane >> 2, quarter = lane & 3;
+        const bool values = warp >= 8;
+        const int w = warp & 3, tok = lane >> 2, quarter = lane & 3;
         constexpr int QB = D / 8;                          // bytes of codes of a quarter
-        constexpr int QW = D / 32;                         // words
+        constexpr int QW = D / 32, HW = QW / 2;            // words of it, and of half of it
         constexpr int R = Plan::kRawSlots;
-        const bool swap = D == 128 && quarter >= 2;
+        const int swap = D == 128 && quarter >= 2;
         uint32_t column[QW];                               // where the thread's 16-byte columns go, in a warp's share of a stage
 #pragma unroll
         for (int k = 0; k < QW; ++k) {
-            const int col = quarter * QW + (swap ? k ^ 2 : k);
-            column[k] = sm + (values ? Plan::kV : Plan::kK) + (col >> 3) * Plan::kChunkBytes + (w * 16 + tok) * 128 + (((col & 7) ^ tok) << 4);
+            const int col = quarter * QW + (swap ? k ^ HW : k);
+            column[k] = sm + (values ? Plan::kV : Plan::kK) + (col >> 3) * Plan::kChunkBytes + (w * 32 + tok) * 128 + (((col & 7) ^ tok) << 4);
         }
         const uint32_t raw = sm + Plan::kRaw + (warp - 4) * R * Plan::kRawHalf;
         const uint32_t codes_at = raw + tok * (D / 2) + quarter * QB, scales_at = raw + 8 * D + (D == 128 ? tok * 8 + quarter * 2 : tok * 4 + quarter);
+        const uint32_t half0 = codes_at + (swap ? QB / 2 : 0), half1 = codes_at + (swap ? 0 : QB / 2);
+        const uint32_t sel0 = D == 64 || !swap ? 0x1010 : 0x3232, sel1 = D == 64 || swap ? 0x1010 : 0x3232;
         constexpr int kCodeParts = 8 * D / 512;            // warp-wide copies of a tile's codes
         constexpr int kScaleLanes = D / 16;                // sixteen-byte parts of a tile's scales
+        const uint32_t full_bar = values ? v_full(0) : k_full(0), empty_bar = values ? v_empty(0) : k_empty(0);
+        const int tile_mask = (c.page_tokens() >> 4) - 1;
+        const uint32_t page_bytes = static_cast<uint32_t>(c.page_bytes >> 7);   // pages are multiples of 128 bytes
         uint32_t n = 0;                                    // halves expanded so far
         for_pieces([&](const WideSegment& g, int s0, int count) {
-            const uint8_t* const head = c.head_tiles(0, a.layer, g.head) + (values ? 8 * D : 0);
-            int page_base = s0, page_of = -1, slot = 0;    // pages of the warp's tiles of 32 steps: lane = step - page_base
-            uint32_t present = 0;                          // a bit per slot
-            auto fill = [&](int step) {                    // the step's tile into the slot, if it is one of ours
+            const uint8_t* const head = c.head_tiles(0, a.layer, g.head) + (values ? 8 * D : 0) + lane * 16;
+            const int tile0 = (g.ri.lo >> 4) + w * 2;      // number of the warp's first tile of step 0
+            int page_base = s0, page_of = -1;              // pages of the warp's tiles of sixteen steps: lane = 2 * (step - page_base) + tile
+            uint32_t present = 0;                          // two bits per slot
+            auto fill = [&](int step, int slot) {          // the step's tiles into the slot, if it is one of ours
                 if (step < s0 + count) {
-                    if (step - page_base >= 32 || step == s0) {
+                    if (step - page_base >= 16 || step == s0) {
                         page_base = step;
-                        const int t = g.ri.lo + (step + lane) * kWideUnit + w * 16;
+                        const int t = g.ri.lo + (step + (lane >> 1)) * kWideUnit + (w * 2 + (lane & 1)) * 16;
                         page_of = t < g.ri.hi && t >= 0 ? c.page_at(g.ri.s, t >> c.log_p) : -1;
                     }
-                    const int page = __shfl_sync(0xffffffffu, page_of, step - page_base);
-                    present &= ~(1u << slot);
-                    if (page >= 0) {
-                        present |= 1u << slot;
-                        const int t = g.ri.lo + step * kWideUnit + w * 16;
-                        const uint32_t dst = raw + slot * Plan::kRawHalf + lane * 16;
-                        const uint8_t* src = head + page * c.page_bytes + ((t & (c.page_tokens() - 1)) >> 4) * (18 * D) + lane * 16;
+                    const uint32_t dst = raw + slot * Plan::kRawHalf + lane * 16;
+                    uint32_t on = 0;
 #pragma unroll
-                        for (int y = 0; y < kCodeParts; ++y) async_copy16(dst + y * 512, src + y * 512);
-                        if (lane < kScaleLanes) async_copy16(dst + 8 * D, src + (values ? 9 * D : 16 * D));
+                    for (int x = 0; x < 2; ++x) {
+                        const int page = __shfl_sync(0xffffffffu, page_of, 2 * (step - page_base) + x);
+                        const int tile = (tile0 + step * 8 + x) & tile_mask;
+                        if (page >= 0) {
+                            on |= 1u << x;
+                            const uint8_t* src = head + static_cast<uint64_t>(page) * page_bytes * 128 + tile * (18 * D);
+#pragma unroll
+                            for (int y = 0; y < kCodeParts; ++y) async_copy16(dst + x * (9 * D) + y * 512, src + y * 512);
+                            if (lane < kScaleLanes) async_copy16(dst + x * (9 * D) + 8 * D, src + (values ? 9 * D : 16 * D));
+                        }
                     }
+                    present = (present & ~(3u << (2 * slot))) | on << (2 * slot);
                 }
                 asm volatile("cp.async.commit_group;" ::: "memory");
             };
 #pragma unroll 1
-            for (int k = 0; k < R; ++k, ++slot) fill(s0 + k);
-            slot = 0;
+            for (int k = 0; k < R; ++k) fill(s0 + k, k);
+            int slot = 0;
 #pragma unroll 1
             for (int k = 0; k < count; ++k, ++n) {
                 asm volatile("cp.async.wait_group %0;" ::"n"(R - 1) : "memory");
                 __syncwarp();
-                const int stage = n & 1;
-                const bool there = (present >> slot) & 1;
-                uint32_t codes[2][QW], scales[2];
+                const uint32_t there = (present >> (2 * slot)) & 3, from = slot * Plan::kRawHalf;
+                uint32_t codes[4][2][HW], scales[4];
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const uint32_t at = slot * Plan::kRawHalf;
-                    lds_words<QW>(at + codes_at + x * 8 * (D / 2), codes[x]);
+                for (int x = 0; x < 4; ++x) {
+                    const uint32_t at = from + (x >> 1) * (9 * D);
+                    lds_words<HW>(at + half0 + (x & 1) * 8 * (D / 2), codes[x][0]);
+                    lds_words<HW>(at + half1 + (x & 1) * 8 * (D / 2), codes[x][1]);
                     if constexpr (D == 128) {
                         uint16_t y;
-                        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(y) : "r"(at + scales_at + x * 64));
+                        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(y) : "r"(at + scales_at + (x & 1) * 64));
                         scales[x] = y;
                     } else {
-                        scales[x] = lds8(at + scales_at + x * 32);
+                        scales[x] = lds8(at + scales_at + (x & 1) * 32) * 0x0101u;
                     }
                 }
                 __syncwarp();
-                fill(s0 + k + R);
+                fill(s0 + k + R, slot);
                 if (++slot == R) slot = 0;
-                if (n >= 2 && !wait(values ? v_empty(stage) : k_empty(stage), ((n >> 1) - 1) & 1)) return false;
-                const int t0 = g.ri.lo + (s0 + k) * kWideUnit + w * 16;
+                const uint32_t stage = n & 1;
                 const bool all = seen_by_all(g, g.ri.lo + (s0 + k) * kWideUnit);
+                const int t0 = g.ri.lo + (s0 + k) * kWideUnit + w * 32;
+                if (!all || there != 3) {                  // what is absent or masked must not be multiplied with
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    uint32_t s = there ? scales[x] : 0;
-                    if (values && !all) {   // what is masked must not be multiplied with
-                        if (t0 + x * 8 + tok >= g.ri.hi) s = 0;
-                        if ((s & 0x7f) == 0x7f) s &= 0xff00;
-                        if ((s & 0x7f00) == 0x7f00) s &= 0x00ff;
+                    for (int x = 0; x < 4; ++x) {
+                        if (!((there >> (x >> 1)) & 1) || (values && t0 + x * 8 + tok >= g.ri.hi)) scales[x] = 0;
+                        if (values && !all) {
+                            if ((scales[x] & 0x7f) == 0x7f) scales[x] &= 0xff00;
+                            if ((scales[x] & 0x7f00) == 0x7f00) scales[x] &= 0x00ff;
+                        }
                     }
-                    const uint32_t f = e4m3x2_to_half2(D == 128 ? s : s * 0x0101u);
-                    const uint32_t f0 = D == 128 ? __byte_perm(f, f, swap ? 0x3232 : 0x1010) : f, f1 = D == 128 ? __byte_perm(f, f, swap ? 0x1010 : 0x3232) : f;
+                }
+                if (n >= 2 && !wait(empty_bar + 8 * stage, ((n >> 1) - 1) & 1)) return false;
+                const uint32_t into = stage * Plan::kTileBytes;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const uint32_t f = e4m3x2_to_half2(scales[x]);
+                    const uint32_t f0 = __byte_perm(f, f, sel0), f1 = __byte_perm(f, f, sel1);
 #pragma unroll
                     for (int q = 0; q < QW; ++q) {
                         uint32_t y[4];
-                        e2m1x8_to_half2(D == 128 && swap ? codes[x][q ^ (QW / 2)] : codes[x][q], y);
+                        e2m1x8_to_half2(codes[x][q / HW][q % HW], y);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) y[i] = mul_half2(y[i], q < QW / 2 ? f0 : f1);
+                        for (int i = 0; i < 4; ++i) y[i] = mul_half2(y[i], q < HW ? f0 : f1);
                         asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
-                                     ::"r"(column[q] + stage * Plan::kTileBytes + x * 1024), "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3]) : "memory");
+                                     ::"r"(column[q] + into + x * 1024), "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3]) : "memory");
                     }
                 }
                 if (!values) {
                     const int ring = n & 3;
-                    if (lane == 0) tile_there[ring][w] = there;
+                    if (lane == 0) tile_there[ring][w] = static_cast<uint8_t>(there);
                     if (!all) {
                         // NaN among the values of these tokens, for the rows that do see them
                         uint32_t nans = 0;
 #pragma unroll 1
-                        for (int x = 0; x < 2; ++x) {
+                        for (int x = 0; x < 4; ++x) {
                             const int t = t0 + x * 8 + tok;
-                            if (!there || t >= g.ri.hi) continue;
+                            if (!((there >> (x >> 1)) & 1) || t >= g.ri.hi) continue;
                             const uint8_t* z = c.tile(c.page_at(g.ri.s, t >> c.log_p), a.layer, g.head, t & (c.page_tokens() - 1)) + 17 * D +
-                                               (x * 8 + tok) * (D / 16) + (D == 128 ? quarter * 2 : quarter);
+                                               ((x & 1) * 8 + tok) * (D / 16) + (D == 128 ? quarter * 2 : quarter);
                             const uint32_t s = D == 128 ? __ldg(reinterpret_cast<const uint16_t*>(z)) : __ldg(z);
                             if ((s & 0x7f) == 0x7f) nans |= 1u << (2 * x);
                             if (D == 128 && (s & 0x7f00) == 0x7f00) nans |= 2u << (2 * x);
@@ -668,12 +684,12 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                         const uint32_t flagged = __ballot_sync(0xffffffffu, nans != 0);
                         if (flagged) {
 #pragma unroll 1
-                            for (int x = 0; x < 2; ++x) {
+                            for (int x = 0; x < 4; ++x) {
                                 // blocks of a quarter: two at 128 channels, one at 64
                                 uint32_t m = D == 128 ? ((nans >> (2 * x)) & 3) << (2 * quarter) : ((nans >> (2 * x)) & 1) << quarter;
                                 m |= __shfl_xor_sync(0xffffffffu, m, 1);
                                 m |= __shfl_xor_sync(0xffffffffu, m, 2);
-                                if (quarter == 0) nan_block[ring][w * 16 + x * 8 + tok] = static_cast<uint8_t>(m);
+                                if (quarter == 0) nan_block[ring][w * 32 + x * 8 + tok] = static_cast<uint8_t>(m);
                             }
                         }
                         if (lane == 0) nan_flag[ring][w] = flagged != 0;
@@ -681,13 +697,13 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                 }
                 async_proxy_fence();
                 __syncwarp();
-                if (lane == 0) barrier_arrive(values ? v_full(stage) : k_full(stage));
+                if (lane == 0) barrier_arrive(full_bar + 8 * stage);
             }
             return true;
         });
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-        if (warp == 20) {
+        if (warp == 12) {
         // ================= issuing warp
         if (lane == 0) {
             constexpr uint32_t kScoreDesc = product_desc(128, 128, false), kSumDesc = product_desc(128, D, true);
@@ -729,7 +745,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == 20) tmem_free(tmem, 512);
+    if (warp == 12) tmem_free(tmem, 512);
     if (tid == 0 && abort_flag && c.meta) atomicOr(&c.meta[1], kStatusGaveUp);
 }
 
