@@ -2,9 +2,10 @@
 //
 // S = Q K^T and O += P V on a tile of 128 query rows, with 128 tokens a step.  Eight warps expand the 4-bit tiles into two stages
 // of fp16 keys and two of fp16 values in shared memory (exact: a value has six significant bits).  Q, two tiles of scores and the
-// sums O lie in tensor memory.  A thread of the four softmax warps owns one query row, so its maximum and its sum need no exchange;
-// it writes P as fp16 over S, from where the second product takes it.  While it works on one step's scores, the products of the
-// step before and of the step after run.
+// sums O lie in tensor memory.  Two threads of the eight softmax warps share a query row, each with
+// half of a step's tokens; they write P as fp16 over S, from where the second product takes it.  While they work on one step's
+// scores, the products of the step before and of the step after run.  (One warp per scheduler, with whole rows, took 2,470 clocks
+// a step: it waits for itself most of the time.)
 //
 // Q is read from tensor memory, not from shared memory, because a 128 x 128 product with both operands in shared memory takes all of
 // its bandwidth: the expanding warps and every barrier then stand still (a store gets through at a tenth of its rate, a load at a
@@ -27,7 +28,7 @@ namespace samb200 {
 
 constexpr int kWideUnit = 128;                     // tokens of a step
 constexpr int kWideRows = 128;                     // query rows of a segment
-constexpr int kWideWarps = 16, kWideThreads = kWideWarps * 32;   // four softmax warps, eight expanding ones, an issuing one (and three that idle)
+constexpr int kWideWarps = 20, kWideThreads = kWideWarps * 32;   // eight softmax warps, eight expanding ones, an issuing one (and three that idle)
 constexpr int kWideMaxCtas = 160;
 constexpr float kWideAbove = 8.f, kTotalMax = 32768.f;   // 128 weights of 2^8 add up to no more
 // columns of tensor memory
@@ -152,12 +153,14 @@ template <typename T, int D>
 __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __grid_constant__ AttendArgs a) {
     using Plan = WidePlan<D>;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t bars[14];
+    __shared__ uint64_t bars[18];
     __shared__ uint32_t tmem_base;
     __shared__ int64_t scan[kWideWarps], start_e, start_begin;
     __shared__ alignas(4) uint8_t tile_there[4][4];    // per step (mod 4) and expanding warp: which of its two tiles are there
     __shared__ alignas(4) uint8_t nan_flag[4][4];      // NaN among the values of the warp's tokens (written where there are masks)
     __shared__ uint8_t nan_block[4][128];              // which 16-channel blocks of a token's values are NaN
+    __shared__ float shared_row[2][128];               // what the two threads of a query row tell each other
+    __shared__ uint32_t again[4];                      // last step (+ 1) that a pair of softmax warps had to do again
     __shared__ int last_here;
     __shared__ volatile int abort_flag;
 
@@ -165,13 +168,15 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const uint32_t sm = shared_addr(smem), bar = shared_addr(bars);
-    // barriers: scores ready, keys and values full / empty (two each), weights ready, product done, queries ready, softmax warps
+    // barriers: scores ready, keys and values full / empty (two each), weights ready, product done, queries ready, all softmax
+    // warps, the two that share rows
     auto score_bar = [&](int i) { return bar + 8 * i; };
     auto k_full = [&](int i) { return bar + 16 + 8 * i; };
     auto k_empty = [&](int i) { return bar + 32 + 8 * i; };
     auto v_full = [&](int i) { return bar + 48 + 8 * i; };
     auto v_empty = [&](int i) { return bar + 64 + 8 * i; };
     const uint32_t weight_bar = bar + 80, product_bar = bar + 88, query_bar = bar + 96, group_bar = bar + 104;
+    auto pair_bar = [&](int i) { return bar + 112 + 8 * i; };
     auto wait = [&](uint32_t b, uint32_t parity) {     // false: give up (here or elsewhere in the CTA)
         for (uint32_t i = 0; i < kCachePolls; ++i) {
             if (barrier_try(b, parity)) return true;
@@ -189,11 +194,13 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
             barrier_init(v_full(i), 4);
             barrier_init(v_empty(i), 1);
         }
-        barrier_init(weight_bar, 4);
+        barrier_init(weight_bar, 8);
         barrier_init(product_bar, 1);
-        barrier_init(query_bar, 4);
-        barrier_init(group_bar, 4);
+        barrier_init(query_bar, 8);
+        barrier_init(group_bar, 8);
+        for (int i = 0; i < 4; ++i) barrier_init(pair_bar(i), 2);
         abort_flag = 0;
+        for (int i = 0; i < 4; ++i) again[i] = 0;
     }
     barrier_init_fence();
 
@@ -250,7 +257,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
     }
     clear_unused_rows<T, D>(a, cta, gridDim.x);
     if (!busy) return;
-    if (warp == 12) tmem_alloc(shared_addr(&tmem_base), 512);
+    if (warp == 16) tmem_alloc(shared_addr(&tmem_base), 512);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -285,13 +292,26 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
         return t0 + kWideUnit - 1 <= g.first_pos && (a.window == 0 || t0 > g.last_pos - a.window);
     };
 
-    // Registers go where they are needed: 128 threads x 200, 256 x 88, 128 x 72, of 512 x 128 at launch.
-    if (warp < 4) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+    // Registers go where they are needed: 256 threads x 112, 256 x 88, 128 x 72, of 640 x 96 at launch.
+    if (warp < 8) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 112;");
         // ================= softmax warps
-        const int row = tid;
-        const uint32_t lanes = tmem + (static_cast<uint32_t>(warp) << 21);   // the warp's quarter of the lanes
-        uint32_t n = 0, n_group = 0;                    // steps so far; meetings of the four warps
+        const int row = tid & 127, part_no = warp >> 2, pair = warp & 3;     // tokens 64 part_no ... of a step
+        const uint32_t lanes = tmem + (static_cast<uint32_t>(pair) << 21);   // the warp's quarter of the lanes
+        uint32_t n = 0, n_group = 0, n_pair = 0;        // steps so far; meetings of all warps, of the pair
+        auto meet_pair = [&]() -> bool {
+            __syncwarp();
+            if (lane == 0) barrier_arrive(pair_bar(pair));
+            return wait(pair_bar(pair), n_pair++ & 1);
+        };
+        // The larger of the two threads' values (ok: whether the other warp came in time).
+        auto larger = [&](float x, bool& ok) -> float {
+            shared_row[part_no][row] = x;
+            ok = meet_pair();
+            const float y = static_cast<volatile float*>(shared_row[part_no ^ 1])[row];
+            ok = ok && meet_pair();                     // the places are free again
+            return fmaxf(x, y);
+        };
         auto meet = [&]() -> bool {
             __syncwarp();
             if (lane == 0) barrier_arrive(group_bar);
@@ -311,9 +331,9 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
             float factor;
             {
                 const T* q = static_cast<const T*>(a.q) + seg.b * a.q_row + static_cast<int64_t>(qi) * a.q_token + static_cast<int64_t>(qh) * a.q_head;
-                uint32_t x[D / 2];
-#pragma unroll
-                for (int d = 0; d < D; d += 8) {
+                constexpr int kHalf = D / 2;            // channels of a thread; the size of the row is taken over all of them
+                uint32_t x[kHalf / 2];
+                auto load8 = [&](int d, uint32_t (&w)[4]) {
                     alignas(16) T y[8];
                     if (mine && a.q_wide) {
                         *reinterpret_cast<uint4*>(y) = __ldg(reinterpret_cast<const uint4*>(q + d));
@@ -322,27 +342,32 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                         for (int i = 0; i < 8; ++i) y[i] = mine ? q[d + i] : Elem<T>::from_float(0.f);
                     }
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) x[d / 2 + i] = reinterpret_cast<const uint32_t*>(y)[i];
-                }
+                    for (int i = 0; i < 4; ++i) w[i] = reinterpret_cast<const uint32_t*>(y)[i];
+                };
+#pragma unroll
+                for (int d = 0; d < kHalf; d += 8) load8(part_no * kHalf + d, reinterpret_cast<uint32_t(&)[4]>(x[d / 2]));
                 int e = 0;
                 if constexpr (!std::is_same<T, __half>::value) {
                     auto lo = [](uint32_t w) { return __uint_as_float(w << 16); };
                     auto hi = [](uint32_t w) { return __uint_as_float(w & 0xffff0000u); };
                     float big = 0.f;
 #pragma unroll
-                    for (int i = 0; i < D / 2; ++i) big = fmaxf(big, fmaxf(fabsf(lo(x[i])), fabsf(hi(x[i]))));
+                    for (int i = 0; i < kHalf / 2; ++i) big = fmaxf(big, fmaxf(fabsf(lo(x[i])), fabsf(hi(x[i]))));
+                    bool ok;
+                    big = larger(big, ok);
+                    if (!ok) return false;
                     e = big > 0.f ? min(14 - (static_cast<int>(__float_as_uint(big) >> 23) - 127), 126) : 0;
                     const float up = pow2(e);
 #pragma unroll
-                    for (int i = 0; i < D / 2; ++i) x[i] = pack_half2(lo(x[i]) * up, hi(x[i]) * up);
+                    for (int i = 0; i < kHalf / 2; ++i) x[i] = pack_half2(lo(x[i]) * up, hi(x[i]) * up);
                 }
                 if (a.scale < 0.f) {                    // so that the largest score is the largest product
 #pragma unroll
-                    for (int i = 0; i < D / 2; ++i) x[i] ^= 0x80008000u;
+                    for (int i = 0; i < kHalf / 2; ++i) x[i] ^= 0x80008000u;
                 }
                 factor = scale_pow2(fabsf(a.scale) * 1.4426950408889634f, c.k_exp - e);
 #pragma unroll
-                for (int i = 0; i < D / 2; i += 16) tmem_store16(lanes + kColQ + i, reinterpret_cast<const uint32_t(&)[16]>(x[i]));
+                for (int i = 0; i < kHalf / 2; i += 16) tmem_store16(lanes + kColQ + part_no * (kHalf / 2) + i, reinterpret_cast<const uint32_t(&)[16]>(x[i]));
                 tmem_store_wait();
                 tc_fence_before();
                 __syncwarp();
@@ -355,7 +380,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
             // ---- steps
 #pragma unroll 1
             for (int k = 0; k < count; ++k, ++n) {
-                const uint32_t s_at = lanes + kColS + (n & 1) * 128;
+                const uint32_t s_at = lanes + kColS + (n & 1) * 128 + part_no * 64;
                 if (!wait(score_bar(n & 1), (n >> 1) & 1)) return false;
                 tc_fence_after();
                 const int t0 = seg.ri.lo + (s0 + k) * kWideUnit, ring = n & 3;
@@ -368,21 +393,24 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                 bool done = false;
                 if (full) {
                     float2 total = make_float2(0.f, 0.f);
-                    uint32_t x[2][16], p[4][16];
+                    uint32_t x[2][16], p[2][16];
                     tmem_load16(s_at, x[0]);
-                    if (__any_sync(0xffffffffu, m == -INFINITY)) {   // a first reference from the first sixteen scores
+                    if (__any_sync(0xffffffffu, m == -INFINITY)) {   // a first reference from some of the scores
                         tmem_load_wait(x[0]);
                         float top = -INFINITY;
 #pragma unroll
                         for (int i = 0; i < 16; ++i) top = fmaxf(top, __uint_as_float(x[0][i]));
+                        bool ok;
+                        top = larger(top, ok);
+                        if (!ok) return false;
                         if (m == -INFINITY) m = top * factor - kWideAbove;
                     }
                     const float ref = m == -INFINITY ? 0.f : m;
 #pragma unroll
-                    for (int q = 0; q < 8; ++q) {
+                    for (int q = 0; q < 4; ++q) {
                         uint32_t(&y)[16] = x[q & 1];
                         tmem_load_wait(y);
-                        if (q < 7) tmem_load16(s_at + (q + 1) * 16, x[(q + 1) & 1]);
+                        if (q < 3) tmem_load16(s_at + (q + 1) * 16, x[(q + 1) & 1]);
 #pragma unroll
                         for (int i = 0; i < 16; i += 2) {
                             float2 z = fma2(make_float2(__uint_as_float(y[i]), __uint_as_float(y[i + 1])), make_float2(factor, factor), make_float2(-ref, -ref));
@@ -393,11 +421,13 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                         }
                     }
                     const float sum = total.x + total.y;
-                    done = !__any_sync(0xffffffffu, sum > kTotalMax);
+                    if (__any_sync(0xffffffffu, sum > kTotalMax) && lane == 0) static_cast<volatile uint32_t*>(again)[pair] = n + 1;
+                    if (!meet_pair()) return false;
+                    done = static_cast<volatile uint32_t*>(again)[pair] != n + 1;
                     if (done) {
                         l += sum;
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) tmem_store16(s_at + q * 16, p[q]);
+                        tmem_store16(s_at, p[0]);
+                        tmem_store16(s_at + 16, p[1]);
                     }
                 }
                 if (!done) {
@@ -406,7 +436,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                             if (static_cast<volatile uint8_t*>(nan_flag[ring])[t >> 5] && t0 + t <= pos && (a.window == 0 || t0 + t > pos - a.window))
                                 nan_blocks |= static_cast<volatile uint8_t*>(nan_block[ring])[t];
                     }
-                    // which of 32 columns a row sees, as bits
+                    // which of 32 columns a row sees, as bits; q: 0 .. 3 over the step
                     const int from = a.window > 0 ? max(pos - a.window + 1 - t0, 0) : 0, to_col = min(pos - t0, kWideUnit - 1);
                     auto seen = [&](int q) -> uint32_t {
                         const int lo = max(from - q * 32, 0), hi = to_col - q * 32;
@@ -418,21 +448,23 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                     uint32_t x[32];
                     float top = -INFINITY;
 #pragma unroll 1
-                    for (int q = 0; q < 4; ++q) {
+                    for (int q = 0; q < 2; ++q) {
                         tmem_load32(s_at + q * 32, x);
                         tmem_load_wait(x);
-                        const uint32_t bits = seen(q);
+                        const uint32_t bits = seen(part_no * 2 + q);
 #pragma unroll
                         for (int i = 0; i < 32; ++i) top = fmaxf(top, (bits >> i) & 1 ? __uint_as_float(x[i]) : -INFINITY);
                     }
-                    top *= factor;
+                    bool ok;
+                    top = larger(top, ok) * factor;
+                    if (!ok) return false;
                     if (__any_sync(0xffffffffu, top > m + kWideAbove)) {
                         const float to = top > m + kWideAbove ? top - kWideAbove : m;
                         const float keep = m == -INFINITY ? 0.f : exp2_fast(m - to);
                         if (k > 0) {                     // the sums so far
                             if (!products(n)) return false;
 #pragma unroll 1
-                            for (int q = 0; q < D / 16; ++q) {
+                            for (int q = part_no * (D / 32); q < (part_no + 1) * (D / 32); ++q) {
                                 uint32_t o[16];
                                 tmem_load16(lanes + kColO + q * 16, o);
                                 tmem_load_wait(o);
@@ -446,10 +478,10 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                     }
                     const float ref = m == -INFINITY ? 0.f : m;
 #pragma unroll 1
-                    for (int q = 0; q < 4; ++q) {
+                    for (int q = 0; q < 2; ++q) {
                         tmem_load32(s_at + q * 32, x);
                         tmem_load_wait(x);
-                        const uint32_t bits = seen(q);
+                        const uint32_t bits = seen(part_no * 2 + q);
                         uint32_t p[16];
 #pragma unroll
                         for (int i = 0; i < 32; i += 2) {
@@ -470,7 +502,14 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
 
             // ---- the piece's result
             if (!products(n)) return false;
+            {   // the row's total
+                shared_row[part_no][row] = l;
+                if (!meet_pair()) return false;
+                l = static_cast<volatile float*>(shared_row[0])[row] + static_cast<volatile float*>(shared_row[1])[row];
+                if (!meet_pair()) return false;
+            }
             const bool begins = s0 == 0, ends = s0 + count == seg.steps;
+            const int col0 = part_no * (D / 2), col1 = col0 + D / 2;
             auto sums = [&](int col, float (&y)[32]) {  // 32 channels
                 uint32_t x[32];
                 tmem_load32(lanes + kColO + col, x);
@@ -487,7 +526,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
             };
             if (begins && ends) {
 #pragma unroll 1
-                for (int col = 0; col < D; col += 32) {
+                for (int col = col0; col < col1; col += 32) {
                     float y[32];
                     sums(col, y);
                     if (mine) finish(col, y, m, l);
@@ -497,15 +536,17 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                 auto part = [&](int owner, bool first_piece) { return a.partials + (2ll * owner + first_piece) * Plan::kPart; };
                 float* out = part(cta, begins);
 #pragma unroll 1
-                for (int col = 0; col < D; col += 32) {
+                for (int col = col0; col < col1; col += 32) {
                     float y[32];
                     sums(col, y);
 #pragma unroll
                     for (int i = 0; i < 32; i += 4)
                         reinterpret_cast<float4*>(out)[((col + i) >> 2) * 128 + row] = make_float4(y[i], y[i + 1], y[i + 2], y[i + 3]);
                 }
-                out[128 * D + row] = m;
-                out[128 * D + 128 + row] = l;
+                if (part_no == 0) {
+                    out[128 * D + row] = m;
+                    out[128 * D + 128 + row] = l;
+                }
                 __threadfence();
                 if (!meet()) return false;
                 const int c0 = shares.owner(seg.begin), c1 = shares.owner(seg.begin + seg.steps - 1);
@@ -527,7 +568,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                         l_all += join_weight(__ldcg(p), m_all) * __ldcg(p + 128);
                     }
 #pragma unroll 1
-                    for (int col = 0; col < D; col += 32) {
+                    for (int col = col0; col < col1; col += 32) {
                         float y[32];
 #pragma unroll
                         for (int i = 0; i < 32; ++i) y[i] = 0.f;
@@ -552,14 +593,14 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
             tc_fence_before();
             return true;
         });
-    } else if (warp < 12) {
+    } else if (warp < 16) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
         // ================= expanding warps: 4-bit tiles -> fp16 operands; four warps for the keys, four for the values
         // A warp takes two tiles of a step and brings them itself, a few steps ahead, into slots of its own (sixteen bytes a thread and
         // copy: a bulk copy costs some 100 clocks to issue, however small).  A thread expands a quarter of the channels of tokens
         // lane / 4 and + 8: its reads are contiguous over the warp, and with the halves of the upper two quarters swapped its writes
         // fall into eight different 16-byte columns of the swizzled rows.
-        const bool values = warp >= 8;
+        const bool values = warp >= 12;
         const int w = warp & 3, tok = lane >> 2, quarter = lane & 3;
         constexpr int QB = D / 8;                          // bytes of codes of a quarter
         constexpr int QW = D / 32, HW = QW / 2;            // words of it, and of half of it
@@ -571,7 +612,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
             const int col = quarter * QW + (swap ? k ^ HW : k);
             column[k] = sm + (values ? Plan::kV : Plan::kK) + (col >> 3) * Plan::kChunkBytes + (w * 32 + tok) * 128 + (((col & 7) ^ tok) << 4);
         }
-        const uint32_t raw = sm + Plan::kRaw + (warp - 4) * R * Plan::kRawHalf;
+        const uint32_t raw = sm + Plan::kRaw + (warp - 8) * R * Plan::kRawHalf;
         const uint32_t codes_at = raw + tok * (D / 2) + quarter * QB, scales_at = raw + 8 * D + (D == 128 ? tok * 8 + quarter * 2 : tok * 4 + quarter);
         const uint32_t half0 = codes_at + (swap ? QB / 2 : 0), half1 = codes_at + (swap ? 0 : QB / 2);
         const uint32_t sel0 = D == 64 || !swap ? 0x1010 : 0x3232, sel1 = D == 64 || swap ? 0x1010 : 0x3232;
@@ -703,7 +744,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
         });
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-        if (warp == 12) {
+        if (warp == 16) {
         // ================= issuing warp
         if (lane == 0) {
             constexpr uint32_t kScoreDesc = product_desc(128, 128, false), kSumDesc = product_desc(128, D, true);
@@ -731,7 +772,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                     tc_fence_after();
                     const uint64_t v = v_desc + stage * (Plan::kTileBytes >> 4);
 #pragma unroll
-                    for (int x = 0; x < 8; ++x) tc_mma_ts(tmem + kColO, tmem + kColS + stage * 128 + x * 8, v + x * (2048 >> 4), kSumDesc, k > 0 || x > 0);
+                    for (int x = 0; x < 8; ++x) tc_mma_ts(tmem + kColO, tmem + kColS + stage * 128 + (x >> 2) * 64 + (x & 3) * 8, v + x * (2048 >> 4), kSumDesc, k > 0 || x > 0);
                     tc_commit(v_empty(stage));
                     tc_commit(product_bar);
                     if (k + 2 < count && !scores(n + 2)) return false;
@@ -745,7 +786,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == 12) tmem_free(tmem, 512);
+    if (warp == 16) tmem_free(tmem, 512);
     if (tid == 0 && abort_flag && c.meta) atomicOr(&c.meta[1], kStatusGaveUp);
 }
 
