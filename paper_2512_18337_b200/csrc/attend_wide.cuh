@@ -1,6 +1,6 @@
 // Attention for many query rows per key/value head (proposals of several heads, prompt chunks): tcgen05 products.
 //
-// S = Q K^T and O += P V on a tile of 128 query rows, with 128 tokens a step.  Eight warps expand the 4-bit tiles into two stages
+// S = Q K^T and O += P V on a tile of 128 query rows, with 128 tokens a step.  Sixteen warps expand the 4-bit tiles into two stages
 // of fp16 keys and two of fp16 values in shared memory (exact: a value has six significant bits).  Q, two tiles of scores and the
 // sums O lie in tensor memory.  Two threads of the eight softmax warps share a query row, each with
 // half of a step's tokens; they write P as fp16 over S, from where the second product takes it.  While they work on one step's
@@ -28,7 +28,7 @@ namespace samb200 {
 
 constexpr int kWideUnit = 128;                     // tokens of a step
 constexpr int kWideRows = 128;                     // query rows of a segment
-constexpr int kWideWarps = 20, kWideThreads = kWideWarps * 32;   // eight softmax warps, eight expanding ones, an issuing one (and three that idle)
+constexpr int kWideWarps = 28, kWideThreads = kWideWarps * 32;   // eight softmax warps, sixteen expanding ones, an issuing one (and three that idle)
 constexpr int kWideMaxCtas = 160;
 constexpr float kWideAbove = 8.f, kTotalMax = 32768.f;   // 128 weights of 2^8 add up to no more
 // columns of tensor memory
@@ -40,8 +40,8 @@ struct WidePlan {
     static constexpr int kChunkBytes = 128 * 128;                       // 64 channels of it
     static constexpr int kK = 0, kV = 2 * kTileBytes;
     static constexpr int kRaw = kV + 2 * kTileBytes;                    // slots of the expanding warps: two tiles' keys or values each
-    static constexpr int kRawSlots = 3, kRawHalf = 18 * D;
-    static constexpr int kSmem = kRaw + 8 * kRawSlots * kRawHalf + 1024;   // and room to start on a 1024-byte boundary
+    static constexpr int kRawSlots = 2, kRawHalf = 18 * D;
+    static constexpr int kSmem = kRaw + 16 * kRawSlots * kRawHalf + 1024;   // and room to start on a 1024-byte boundary
     static constexpr int kPart = 128 * D + 2 * 128;                     // floats of a partial result
 };
 
@@ -153,14 +153,13 @@ template <typename T, int D>
 __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __grid_constant__ AttendArgs a) {
     using Plan = WidePlan<D>;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t bars[18];
+    __shared__ uint64_t bars[15];
     __shared__ uint32_t tmem_base;
     __shared__ int64_t scan[kWideWarps], start_e, start_begin;
     __shared__ alignas(4) uint8_t tile_there[4][4];    // per step (mod 4) and expanding warp: which of its two tiles are there
     __shared__ alignas(4) uint8_t nan_flag[4][4];      // NaN among the values of the warp's tokens (written where there are masks)
     __shared__ uint8_t nan_block[4][128];              // which 16-channel blocks of a token's values are NaN
     __shared__ float shared_row[2][128];               // what the two threads of a query row tell each other
-    __shared__ uint32_t again[4];                      // last step (+ 1) that a pair of softmax warps had to do again
     __shared__ int last_here;
     __shared__ volatile int abort_flag;
 
@@ -168,24 +167,25 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const uint32_t sm = shared_addr(smem), bar = shared_addr(bars);
-    // barriers: scores ready, keys and values full / empty (two each), weights ready, product done, queries ready, all softmax
-    // warps, the two that share rows
+    // barriers: scores ready, keys and values full / empty (two each), product done, weights ready, queries
+    // ready
     auto score_bar = [&](int i) { return bar + 8 * i; };
     auto k_full = [&](int i) { return bar + 16 + 8 * i; };
     auto k_empty = [&](int i) { return bar + 32 + 8 * i; };
     auto v_full = [&](int i) { return bar + 48 + 8 * i; };
     auto v_empty = [&](int i) { return bar + 64 + 8 * i; };
-    const uint32_t weight_bar = bar + 80, product_bar = bar + 88, query_bar = bar + 96, group_bar = bar + 104;
-    auto pair_bar = [&](int i) { return bar + 112 + 8 * i; };
-    auto wait = [&](uint32_t b, uint32_t parity) {     // false: give up (here or elsewhere in the CTA)
+    auto product_bar = [&](int i) { return bar + 80 + 8 * i; };
+    auto weight_bar = [&](int i) { return bar + 96 + 8 * i; };   // two: a softmax warp may be a step ahead of another
+    const uint32_t query_bar = bar + 112;
+    // Gives up after kCachePolls polls, and at once when some wait of the CTA has: everybody then runs on without waiting, the
+    // results are not valid, and the status says so.
+    auto wait = [&](uint32_t b, uint32_t parity) {
         for (uint32_t i = 0; i < kCachePolls; ++i) {
-            if (barrier_try(b, parity)) return true;
-            if ((i & 63) == 63 && abort_flag) return false;
+            if (barrier_try(b, parity)) return;
+            if ((i & 15) == 15 && abort_flag) return;
         }
         abort_flag = 1;
-        return false;
     };
-
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
             barrier_init(score_bar(i), 1);
@@ -193,14 +193,11 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
             barrier_init(k_empty(i), 1);
             barrier_init(v_full(i), 4);
             barrier_init(v_empty(i), 1);
+            barrier_init(product_bar(i), 1);
+            barrier_init(weight_bar(i), 8);
         }
-        barrier_init(weight_bar, 8);
-        barrier_init(product_bar, 1);
         barrier_init(query_bar, 8);
-        barrier_init(group_bar, 8);
-        for (int i = 0; i < 4; ++i) barrier_init(pair_bar(i), 2);
         abort_flag = 0;
-        for (int i = 0; i < 4; ++i) again[i] = 0;
     }
     barrier_init_fence();
 
@@ -257,13 +254,13 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
     }
     clear_unused_rows<T, D>(a, cta, gridDim.x);
     if (!busy) return;
-    if (warp == 16) tmem_alloc(shared_addr(&tmem_base), 512);
+    if (warp == 24) tmem_alloc(shared_addr(&tmem_base), 512);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_base;
 
-    // Runs f(segment, first step, steps, index) over the pieces of our share; f returns false to stop.
+    // Runs f(segment, first step, steps) over the pieces of our share.
     auto for_pieces = [&](auto f) {
         WideSegment g;
         int64_t e = start_e;
@@ -272,10 +269,10 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
         g.head = static_cast<int>(rel / g.steps);
         g.begin = start_begin + static_cast<int64_t>(g.head) * g.steps;
         int64_t u = u0;
-        for (int index = 0;; ++index) {
+        for (;;) {
             const int s0 = static_cast<int>(u - g.begin);
             const int count = static_cast<int>(min(u1 - u, static_cast<int64_t>(g.steps - s0)));
-            if (!f(g, s0, count)) return;
+            f(g, s0, count);
             u += count;
             if (u >= u1) return;
             g.begin += g.steps;
@@ -292,37 +289,33 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
         return t0 + kWideUnit - 1 <= g.first_pos && (a.window == 0 || t0 > g.last_pos - a.window);
     };
 
-    // Registers go where they are needed: 256 threads x 112, 256 x 88, 128 x 72, of 640 x 96 at launch.
+    // Registers go where they are needed: 256 threads x 96, 512 x 64, 128 x 48, of 896 x 72 at launch.
     if (warp < 8) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 112;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 96;");
         // ================= softmax warps
         const int row = tid & 127, part_no = warp >> 2, pair = warp & 3;     // tokens 64 part_no ... of a step
         const uint32_t lanes = tmem + (static_cast<uint32_t>(pair) << 21);   // the warp's quarter of the lanes
-        uint32_t n = 0, n_group = 0, n_pair = 0;        // steps so far; meetings of all warps, of the pair
-        auto meet_pair = [&]() -> bool {
-            __syncwarp();
-            if (lane == 0) barrier_arrive(pair_bar(pair));
-            return wait(pair_bar(pair), n_pair++ & 1);
+        uint32_t n = 0;                                 // steps so far
+        auto meet_pair = [&]() { asm volatile("barrier.cta.sync.aligned %0, 64;" ::"r"(1 + pair) : "memory"); };
+        auto any_of_pair = [&](bool x) -> bool {        // true if x is for any of the pair's threads
+            uint32_t y;
+            asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred.aligned q, %2, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                         : "=r"(y) : "r"(static_cast<uint32_t>(x)), "r"(1 + pair) : "memory");
+            return y != 0;
         };
-        // The larger of the two threads' values (ok: whether the other warp came in time).
-        auto larger = [&](float x, bool& ok) -> float {
+        auto meet = [&]() { asm volatile("barrier.cta.sync.aligned 5, 256;" ::: "memory"); };
+        auto larger = [&](float x) -> float {           // the larger of the two threads' values
             shared_row[part_no][row] = x;
-            ok = meet_pair();
+            meet_pair();
             const float y = static_cast<volatile float*>(shared_row[part_no ^ 1])[row];
-            ok = ok && meet_pair();                     // the places are free again
+            meet_pair();                                // the places are free again
             return fmaxf(x, y);
         };
-        auto meet = [&]() -> bool {
-            __syncwarp();
-            if (lane == 0) barrier_arrive(group_bar);
-            return wait(group_bar, n_group++ & 1);
-        };
-        uint32_t n_product = 0;                         // products known to be complete: each is waited for in turn, a parity tells two apart
-        auto products = [&](uint32_t upto) -> bool {
-            while (n_product < upto)
-                if (!wait(product_bar, n_product++ & 1)) return false;
+        // Product n complete.  Asked for when the scores of step n + 1 are there, or none are to come: the product before n has been
+        // complete since, so that the parity of n's barrier tells.
+        auto product = [&](uint32_t i) {
+            wait(product_bar(i & 1), (i >> 1) & 1);
             tc_fence_after();
-            return true;
         };
         for_pieces([&](const WideSegment& seg, int s0, int count) {
             // ---- queries into tensor memory
@@ -353,9 +346,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                     float big = 0.f;
 #pragma unroll
                     for (int i = 0; i < kHalf / 2; ++i) big = fmaxf(big, fmaxf(fabsf(lo(x[i])), fabsf(hi(x[i]))));
-                    bool ok;
-                    big = larger(big, ok);
-                    if (!ok) return false;
+                    big = larger(big);
                     e = big > 0.f ? min(14 - (static_cast<int>(__float_as_uint(big) >> 23) - 127), 126) : 0;
                     const float up = pow2(e);
 #pragma unroll
@@ -381,17 +372,16 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
 #pragma unroll 1
             for (int k = 0; k < count; ++k, ++n) {
                 const uint32_t s_at = lanes + kColS + (n & 1) * 128 + part_no * 64;
-                if (!wait(score_bar(n & 1), (n >> 1) & 1)) return false;
+                wait(score_bar(n & 1), (n >> 1) & 1);
                 tc_fence_after();
                 const int t0 = seg.ri.lo + (s0 + k) * kWideUnit, ring = n & 3;
                 uint32_t on = *reinterpret_cast<volatile uint32_t*>(tile_there[ring]);
                 on = (on * 0x01041040u) >> 24;            // two bits of each byte, side by side
                 const bool all = seen_by_all(seg, t0);
-                const bool full = all && on == 0xff;
                 // Weights with the reference at hand, in one pass: a sum of at most kTotalMax means that each of them is within fp16.
                 // Where that fails, and where there are masks, the step is done in two passes, the largest score first.
                 bool done = false;
-                if (full) {
+                if (all) {                               // that every tile is there is looked at with the sum
                     float2 total = make_float2(0.f, 0.f);
                     uint32_t x[2][16], p[2][16];
                     tmem_load16(s_at, x[0]);
@@ -400,9 +390,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                         float top = -INFINITY;
 #pragma unroll
                         for (int i = 0; i < 16; ++i) top = fmaxf(top, __uint_as_float(x[0][i]));
-                        bool ok;
-                        top = larger(top, ok);
-                        if (!ok) return false;
+                        top = larger(top);
                         if (m == -INFINITY) m = top * factor - kWideAbove;
                     }
                     const float ref = m == -INFINITY ? 0.f : m;
@@ -421,9 +409,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                         }
                     }
                     const float sum = total.x + total.y;
-                    if (__any_sync(0xffffffffu, sum > kTotalMax) && lane == 0) static_cast<volatile uint32_t*>(again)[pair] = n + 1;
-                    if (!meet_pair()) return false;
-                    done = static_cast<volatile uint32_t*>(again)[pair] != n + 1;
+                    done = !any_of_pair(sum > kTotalMax || on != 0xff);
                     if (done) {
                         l += sum;
                         tmem_store16(s_at, p[0]);
@@ -443,7 +429,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                         uint32_t bits = hi < 0 || lo > 31 ? 0u : (0xffffffffu >> (31 - min(hi, 31))) & (0xffffffffu << lo);
                         if (!((on >> (2 * q)) & 1)) bits &= 0xffff0000u;
                         if (!((on >> (2 * q)) & 2)) bits &= 0x0000ffffu;
-                        return full ? 0xffffffffu : bits;
+                        return bits;
                     };
                     uint32_t x[32];
                     float top = -INFINITY;
@@ -455,14 +441,12 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
 #pragma unroll
                         for (int i = 0; i < 32; ++i) top = fmaxf(top, (bits >> i) & 1 ? __uint_as_float(x[i]) : -INFINITY);
                     }
-                    bool ok;
-                    top = larger(top, ok) * factor;
-                    if (!ok) return false;
+                    top = larger(top) * factor;
                     if (__any_sync(0xffffffffu, top > m + kWideAbove)) {
                         const float to = top > m + kWideAbove ? top - kWideAbove : m;
                         const float keep = m == -INFINITY ? 0.f : exp2_fast(m - to);
                         if (k > 0) {                     // the sums so far
-                            if (!products(n)) return false;
+                            product(n - 1);
 #pragma unroll 1
                             for (int q = part_no * (D / 32); q < (part_no + 1) * (D / 32); ++q) {
                                 uint32_t o[16];
@@ -494,19 +478,18 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                     }
                 }
                 tmem_store_wait();
-                if (!products(n)) return false;          // one at a time is under way; the one before is long done here
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) barrier_arrive(weight_bar);
+                if (lane == 0) barrier_arrive(weight_bar(n & 1));
             }
 
             // ---- the piece's result
-            if (!products(n)) return false;
+            product(n - 1);
             {   // the row's total
                 shared_row[part_no][row] = l;
-                if (!meet_pair()) return false;
+                meet_pair();
                 l = static_cast<volatile float*>(shared_row[0])[row] + static_cast<volatile float*>(shared_row[1])[row];
-                if (!meet_pair()) return false;
+                meet_pair();
             }
             const bool begins = s0 == 0, ends = s0 + count == seg.steps;
             const int col0 = part_no * (D / 2), col1 = col0 + D / 2;
@@ -548,14 +531,14 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                     out[128 * D + 128 + row] = l;
                 }
                 __threadfence();
-                if (!meet()) return false;
+                meet();
                 const int c0 = shares.owner(seg.begin), c1 = shares.owner(seg.begin + seg.steps - 1);
                 if (tid == 0) {
                     last_here = atomicAdd(&a.counters[c0], 1) == c1 - c0;
                     if (last_here) a.counters[c0] = 0;
                     __threadfence();
                 }
-                if (!meet()) return false;
+                meet();
                 if (*static_cast<volatile int*>(&last_here)) {
                     __threadfence();
                     const int parts = c1 - c0 + 1;
@@ -588,19 +571,20 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                         if (mine) finish(col, y, m_all, l_all);
                     }
                 }
-                if (!meet()) return false;                // `last_here` is free again
+                meet();                // `last_here` is free again
             }
             tc_fence_before();
-            return true;
         });
-    } else if (warp < 16) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-        // ================= expanding warps: 4-bit tiles -> fp16 operands; four warps for the keys, four for the values
-        // A warp takes two tiles of a step and brings them itself, a few steps ahead, into slots of its own (sixteen bytes a thread and
+    } else if (warp < 24) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        // ================= expanding warps: 4-bit tiles -> fp16 operands; eight warps for the keys, eight for the values
+        // Four of the eight take a step, the other four the next one: half of a warp's time goes into waiting (a round of
+        // barriers and copies takes 1,650 clocks, expanding a tile 320).  A warp takes two tiles and brings them itself, a few steps ahead, into slots of its own (sixteen bytes a thread and
         // copy: a bulk copy costs some 100 clocks to issue, however small).  A thread expands a quarter of the channels of tokens
         // lane / 4 and + 8: its reads are contiguous over the warp, and with the halves of the upper two quarters swapped its writes
         // fall into eight different 16-byte columns of the swizzled rows.
-        const bool values = warp >= 12;
+        const bool values = warp >= 16;
+        const uint32_t stage = (warp >> 2) & 1;            // the steps that this warp takes, and where it puts them
         const int w = warp & 3, tok = lane >> 2, quarter = lane & 3;
         constexpr int QB = D / 8;                          // bytes of codes of a quarter
         constexpr int QW = D / 32, HW = QW / 2;            // words of it, and of half of it
@@ -610,7 +594,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
 #pragma unroll
         for (int k = 0; k < QW; ++k) {
             const int col = quarter * QW + (swap ? k ^ HW : k);
-            column[k] = sm + (values ? Plan::kV : Plan::kK) + (col >> 3) * Plan::kChunkBytes + (w * 32 + tok) * 128 + (((col & 7) ^ tok) << 4);
+            column[k] = sm + (values ? Plan::kV : Plan::kK) + stage * Plan::kTileBytes + (col >> 3) * Plan::kChunkBytes + (w * 32 + tok) * 128 + (((col & 7) ^ tok) << 4);
         }
         const uint32_t raw = sm + Plan::kRaw + (warp - 8) * R * Plan::kRawHalf;
         const uint32_t codes_at = raw + tok * (D / 2) + quarter * QB, scales_at = raw + 8 * D + (D == 128 ? tok * 8 + quarter * 2 : tok * 4 + quarter);
@@ -618,18 +602,19 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
         const uint32_t sel0 = D == 64 || !swap ? 0x1010 : 0x3232, sel1 = D == 64 || swap ? 0x1010 : 0x3232;
         constexpr int kCodeParts = 8 * D / 512;            // warp-wide copies of a tile's codes
         constexpr int kScaleLanes = D / 16;                // sixteen-byte parts of a tile's scales
-        const uint32_t full_bar = values ? v_full(0) : k_full(0), empty_bar = values ? v_empty(0) : k_empty(0);
+        const uint32_t full_bar = (values ? v_full(0) : k_full(0)) + 8 * stage, empty_bar = (values ? v_empty(0) : k_empty(0)) + 8 * stage;
         const int tile_mask = (c.page_tokens() >> 4) - 1;
         const uint32_t page_bytes = static_cast<uint32_t>(c.page_bytes >> 7);   // pages are multiples of 128 bytes
-        uint32_t n = 0;                                    // halves expanded so far
+        uint32_t n = 0;                                    // steps in earlier pieces
         for_pieces([&](const WideSegment& g, int s0, int count) {
             const uint8_t* const head = c.head_tiles(0, a.layer, g.head) + (values ? 8 * D : 0) + lane * 16;
             const int tile0 = (g.ri.lo >> 4) + w * 2;      // number of the warp's first tile of step 0
-            int page_base = s0, page_of = -1;              // pages of the warp's tiles of sixteen steps: lane = 2 * (step - page_base) + tile
+            int page_base = -16, page_of = -1;              // pages of the warp's tiles of sixteen steps: lane = 2 * (step - page_base) + tile
+            const int first = (n ^ stage) & 1;             // our first step of the piece
             uint32_t present = 0;                          // two bits per slot
             auto fill = [&](int step, int slot) {          // the step's tiles into the slot, if it is one of ours
                 if (step < s0 + count) {
-                    if (step - page_base >= 16 || step == s0) {
+                    if (step - page_base >= 16) {
                         page_base = step;
                         const int t = g.ri.lo + (step + (lane >> 1)) * kWideUnit + (w * 2 + (lane & 1)) * 16;
                         page_of = t < g.ri.hi && t >= 0 ? c.page_at(g.ri.s, t >> c.log_p) : -1;
@@ -653,10 +638,10 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                 asm volatile("cp.async.commit_group;" ::: "memory");
             };
 #pragma unroll 1
-            for (int k = 0; k < R; ++k) fill(s0 + k, k);
+            for (int k = 0; k < R; ++k) fill(s0 + first + 2 * k, k);
             int slot = 0;
 #pragma unroll 1
-            for (int k = 0; k < count; ++k, ++n) {
+            for (int k = first; k < count; k += 2) {
                 asm volatile("cp.async.wait_group %0;" ::"n"(R - 1) : "memory");
                 __syncwarp();
                 const uint32_t there = (present >> (2 * slot)) & 3, from = slot * Plan::kRawHalf;
@@ -675,9 +660,8 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                     }
                 }
                 __syncwarp();
-                fill(s0 + k + R, slot);
+                fill(s0 + k + 2 * R, slot);
                 if (++slot == R) slot = 0;
-                const uint32_t stage = n & 1;
                 const bool all = seen_by_all(g, g.ri.lo + (s0 + k) * kWideUnit);
                 const int t0 = g.ri.lo + (s0 + k) * kWideUnit + w * 32;
                 if (!all || there != 3) {                  // what is absent or masked must not be multiplied with
@@ -690,8 +674,8 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                         }
                     }
                 }
-                if (n >= 2 && !wait(empty_bar + 8 * stage, ((n >> 1) - 1) & 1)) return false;
-                const uint32_t into = stage * Plan::kTileBytes;
+                const uint32_t i = n + k;                  // number of the step in this CTA
+                if (i >= 2) wait(empty_bar, ((i >> 1) - 1) & 1);
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
                     const uint32_t f = e4m3x2_to_half2(scales[x]);
@@ -701,13 +685,13 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                         uint32_t y[4];
                         e2m1x8_to_half2(codes[x][q / HW][q % HW], y);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) y[i] = mul_half2(y[i], q < HW ? f0 : f1);
+                        for (int z = 0; z < 4; ++z) y[z] = mul_half2(y[z], q < HW ? f0 : f1);
                         asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
-                                     ::"r"(column[q] + into + x * 1024), "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3]) : "memory");
+                                     ::"r"(column[q] + x * 1024), "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3]) : "memory");
                     }
                 }
                 if (!values) {
-                    const int ring = n & 3;
+                    const int ring = i & 3;
                     if (lane == 0) tile_there[ring][w] = static_cast<uint8_t>(there);
                     if (!all) {
                         // NaN among the values of these tokens, for the rows that do see them
@@ -738,22 +722,22 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                 }
                 async_proxy_fence();
                 __syncwarp();
-                if (lane == 0) barrier_arrive(full_bar + 8 * stage);
+                if (lane == 0) barrier_arrive(full_bar);
             }
-            return true;
+            n += count;
         });
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-        if (warp == 16) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+        if (warp == 24) {
         // ================= issuing warp
         if (lane == 0) {
             constexpr uint32_t kScoreDesc = product_desc(128, 128, false), kSumDesc = product_desc(128, D, true);
             const uint64_t k_desc = operand_desc(sm + Plan::kK, 16, 1024), v_desc = operand_desc(sm + Plan::kV, Plan::kChunkBytes, 1024);
             uint32_t n = 0, n_query = 0;                 // steps in earlier pieces
             for_pieces([&](const WideSegment&, int, int count) {
-                auto scores = [&](uint32_t i) -> bool {  // S of step i
+                auto scores = [&](uint32_t i) {          // S of step i
                     const int stage = i & 1;
-                    if (!wait(k_full(stage), (i >> 1) & 1)) return false;
+                    wait(k_full(stage), (i >> 1) & 1);
                     tc_fence_after();
                     const uint64_t k = k_desc + stage * (Plan::kTileBytes >> 4);
 #pragma unroll
@@ -761,23 +745,23 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                         tc_mma_ts(tmem + kColS + stage * 128, tmem + kColQ + x * 8, k + (((x >> 2) * Plan::kChunkBytes + (x & 3) * 32) >> 4), kScoreDesc, x > 0);
                     tc_commit(score_bar(stage));
                     tc_commit(k_empty(stage));
-                    return true;
                 };
-                if (!wait(query_bar, n_query++ & 1)) return false;
-                if (!scores(n) || (count > 1 && !scores(n + 1))) return false;
+                wait(query_bar, n_query++ & 1);
+                scores(n);
+                if (count > 1) scores(n + 1);
 #pragma unroll 1
                 for (int k = 0; k < count; ++k, ++n) {
                     const int stage = n & 1;
-                    if (!wait(v_full(stage), (n >> 1) & 1) || !wait(weight_bar, n & 1)) return false;
+                    wait(v_full(stage), (n >> 1) & 1);
+                    wait(weight_bar(stage), (n >> 1) & 1);
                     tc_fence_after();
                     const uint64_t v = v_desc + stage * (Plan::kTileBytes >> 4);
 #pragma unroll
                     for (int x = 0; x < 8; ++x) tc_mma_ts(tmem + kColO, tmem + kColS + stage * 128 + (x >> 2) * 64 + (x & 3) * 8, v + x * (2048 >> 4), kSumDesc, k > 0 || x > 0);
                     tc_commit(v_empty(stage));
-                    tc_commit(product_bar);
-                    if (k + 2 < count && !scores(n + 2)) return false;
+                    tc_commit(product_bar(stage));
+                    if (k + 2 < count) scores(n + 2);
                 }
-                return true;
             });
         }
         __syncwarp();
@@ -786,7 +770,8 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == 16) tmem_free(tmem, 512);
+    if (abort_flag) __nanosleep(100000);               // products still under way
+    if (warp == 24) tmem_free(tmem, 512);
     if (tid == 0 && abort_flag && c.meta) atomicOr(&c.meta[1], kStatusGaveUp);
 }
 
