@@ -167,13 +167,11 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const uint32_t sm = shared_addr(smem), bar = shared_addr(bars);
-    // barriers: scores ready, keys and values full / empty (two each), product done, weights ready, queries
+    // barriers: scores ready, keys and values ready, product done (two each), weights ready, queries
     // ready
     auto score_bar = [&](int i) { return bar + 8 * i; };
     auto k_full = [&](int i) { return bar + 16 + 8 * i; };
-    auto k_empty = [&](int i) { return bar + 32 + 8 * i; };
     auto v_full = [&](int i) { return bar + 48 + 8 * i; };
-    auto v_empty = [&](int i) { return bar + 64 + 8 * i; };
     auto product_bar = [&](int i) { return bar + 80 + 8 * i; };
     auto weight_bar = [&](int i) { return bar + 96 + 8 * i; };   // two: a softmax warp may be a step ahead of another
     const uint32_t query_bar = bar + 112;
@@ -190,9 +188,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
         for (int i = 0; i < 2; ++i) {
             barrier_init(score_bar(i), 1);
             barrier_init(k_full(i), 4);
-            barrier_init(k_empty(i), 1);
             barrier_init(v_full(i), 4);
-            barrier_init(v_empty(i), 1);
             barrier_init(product_bar(i), 1);
             barrier_init(weight_bar(i), 8);
         }
@@ -602,7 +598,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
         const uint32_t sel0 = D == 64 || !swap ? 0x1010 : 0x3232, sel1 = D == 64 || swap ? 0x1010 : 0x3232;
         constexpr int kCodeParts = 8 * D / 512;            // warp-wide copies of a tile's codes
         constexpr int kScaleLanes = D / 16;                // sixteen-byte parts of a tile's scales
-        const uint32_t full_bar = (values ? v_full(0) : k_full(0)) + 8 * stage, empty_bar = (values ? v_empty(0) : k_empty(0)) + 8 * stage;
+        const uint32_t full_bar = (values ? v_full(0) : k_full(0)) + 8 * stage, empty_bar = (values ? product_bar(0) : score_bar(0)) + 8 * stage;   // done with: by the products
         const int tile_mask = (c.page_tokens() >> 4) - 1;
         const uint32_t page_bytes = static_cast<uint32_t>(c.page_bytes >> 7);   // pages are multiples of 128 bytes
         uint32_t n = 0;                                    // steps in earlier pieces
@@ -735,30 +731,32 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
             const uint64_t k_desc = operand_desc(sm + Plan::kK, 16, 1024), v_desc = operand_desc(sm + Plan::kV, Plan::kChunkBytes, 1024);
             uint32_t n = 0, n_query = 0;                 // steps in earlier pieces
             for_pieces([&](const WideSegment&, int, int count) {
+                auto keys = [&](uint32_t i) { wait(k_full(i & 1), (i >> 1) & 1); };
                 auto scores = [&](uint32_t i) {          // S of step i
                     const int stage = i & 1;
-                    wait(k_full(stage), (i >> 1) & 1);
-                    tc_fence_after();
                     const uint64_t k = k_desc + stage * (Plan::kTileBytes >> 4);
 #pragma unroll
                     for (int x = 0; x < D / 16; ++x)
                         tc_mma_ts(tmem + kColS + stage * 128, tmem + kColQ + x * 8, k + (((x >> 2) * Plan::kChunkBytes + (x & 3) * 32) >> 4), kScoreDesc, x > 0);
                     tc_commit(score_bar(stage));
-                    tc_commit(k_empty(stage));
                 };
                 wait(query_bar, n_query++ & 1);
-                scores(n);
-                if (count > 1) scores(n + 1);
+                for (int k = 0; k < 2 && k < count; ++k) {
+                    keys(n + k);
+                    tc_fence_after();
+                    scores(n + k);
+                }
 #pragma unroll 1
                 for (int k = 0; k < count; ++k, ++n) {
                     const int stage = n & 1;
+                    if (k + 2 < count) keys(n + 2);      // long there, as the values are: what is waited for is the weights
                     wait(v_full(stage), (n >> 1) & 1);
                     wait(weight_bar(stage), (n >> 1) & 1);
                     tc_fence_after();
                     const uint64_t v = v_desc + stage * (Plan::kTileBytes >> 4);
 #pragma unroll
-                    for (int x = 0; x < 8; ++x) tc_mma_ts(tmem + kColO, tmem + kColS + stage * 128 + (x >> 2) * 64 + (x & 3) * 8, v + x * (2048 >> 4), kSumDesc, k > 0 || x > 0);
-                    tc_commit(v_empty(stage));
+                    for (int x = 0; x < 8; ++x)
+                        tc_mma_ts(tmem + kColO, tmem + kColS + stage * 128 + (x >> 2) * 64 + (x & 3) * 8, v + x * (2048 >> 4), kSumDesc, k > 0 || x > 0);
                     tc_commit(product_bar(stage));
                     if (k + 2 < count) scores(n + 2);
                 }
