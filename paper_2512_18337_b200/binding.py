@@ -158,7 +158,7 @@ def _host(a: Optional[np.ndarray], dtype) -> Optional[int]:
 def _stream(stream) -> Optional[int]:
     if stream is None:
         import torch
-        return torch.cuda.current_stream().cuda_stream or None
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) or None
     if isinstance(stream, int):
         return stream or None
     return stream.cuda_stream or None
@@ -624,6 +624,8 @@ class SamCache:
                                     v_exp)
         self.handle = C.addressof(self._struct)
         self._ws = None
+        self._ws_need = {}      # workspace bytes by (B, Q, H)
+        self._codes = {torch.bfloat16: SAM_CACHE_BF16, torch.float16: SAM_CACHE_FP16}
         if not any(n in given for n in self.BOOKS):
             sam_cache_init(self.handle, stream)
 
@@ -639,25 +641,28 @@ class SamCache:
         with torch.cuda.stream(stream):
             return make(shape, dtype=dtype, device=device)
 
-    @staticmethod
-    def _dtype(t) -> int:
-        import torch
-        if t not in (torch.bfloat16, torch.float16):
+    def _dtype(self, t) -> int:
+        code = self._codes.get(t)
+        if code is None:
             raise ValueError("bfloat16 or float16 is wanted")
-        return SAM_CACHE_BF16 if t == torch.bfloat16 else SAM_CACHE_FP16
+        return code
 
     def _rows(self, t, heads: Optional[int]):
-        if t.dim() != 4 or t.shape[3] != self.head_dim or (heads is not None and t.shape[2] != heads):
+        """(address, strides of row, token and head)."""
+        shape, strides = t.shape, t.stride()
+        if len(shape) != 4 or shape[3] != self.head_dim or (heads is not None and shape[2] != heads):
             raise ValueError("a [B, Q, heads, head_dim] tensor is wanted")
-        if not t.is_cuda or (t.stride(3) != 1 and t.numel()):
+        if not t.is_cuda or (strides[3] != 1 and t.numel()):
             raise ValueError("expected a CUDA tensor with contiguous channels")
-        return t.data_ptr(), t.stride()[:3]
+        return t.data_ptr(), strides[:3]
 
-    @staticmethod
-    def _index(t, B: int):
-        if t is not None and (t.numel() != B or "int32" not in str(t.dtype)):
+    def _index(self, t, B: int):
+        """Address of an int32 vector with one entry per row (or None)."""
+        if t is None:
+            return None
+        if t.dtype != self.page_table.dtype or t.numel() != B:
             raise ValueError("an int32 tensor with one entry per row is wanted")
-        return t
+        return _dev(t)
 
     def reserve(self, n_new, streams=None, stream=None) -> None:
         B = n_new.numel()
@@ -714,16 +719,20 @@ class SamCache:
         B, Q, H = q.shape[:3]
         if out is None:
             out = self._empty(q.shape, q.dtype, q.device, stream)
+        elif out.shape != q.shape or out.dtype != q.dtype:
+            raise ValueError("out like q is wanted")
         if lse is None:
             lse = self._empty((B, Q, H), torch.float32, q.device, stream)
+        elif tuple(lse.shape) != (B, Q, H) or lse.dtype != torch.float32:
+            raise ValueError("a float32 lse [B, Q, H] is wanted")
         po, so = self._rows(out, H)
-        if out.shape != q.shape or out.dtype != q.dtype or tuple(lse.shape) != (B, Q, H) or lse.dtype != torch.float32:
-            raise ValueError("out like q and a float32 lse [B, Q, H] are wanted")
-        need = sam_cache_attend_workspace_bytes(self.handle, B, Q, H)
+        need = self._ws_need.get((B, Q, H))
+        if need is None:
+            need = self._ws_need[B, Q, H] = sam_cache_attend_workspace_bytes(self.handle, B, Q, H)
         if workspace is None:
-            if self._ws is None or self._ws.numel() < need:
-                self._ws = self._empty(need, torch.uint8, q.device, stream, zero=True)
             workspace = self._ws
+            if workspace is None or workspace.numel() < need:
+                workspace = self._ws = self._empty(need, torch.uint8, q.device, stream, zero=True)
         sam_cache_attend(self.handle, layer, pq, self._dtype(q.dtype), sq, B, Q, H, self._index(streams, B),
                          self._index(n_new, B), self.head_dim ** -0.5 if scale is None else scale, window, po, so, lse,
                          workspace, workspace.numel() * workspace.element_size(), stream)

@@ -110,7 +110,7 @@ struct StreamCursor {
         enter<kRows>(a, row);
         base = row_begin;
         const int64_t rel = u - base;
-        const int seg = static_cast<int>(rel / steps);
+        const int seg = static_cast<int>(quotient(rel, steps));
         step = static_cast<int>(rel - static_cast<int64_t>(seg) * steps);
         head = seg / tiles;
         rt = seg % tiles;

@@ -135,8 +135,8 @@ struct WideSegment {
     int64_t begin;       // number of its first unit
 };
 __device__ __forceinline__ void wide_tile(const AttendArgs& a, int tiles, int64_t e, WideSegment& g) {   // e = b * tiles + rt
-    g.b = static_cast<int>(e / tiles);
-    g.rt = static_cast<int>(e % tiles);
+    g.b = static_cast<int>(quotient(e, tiles));
+    g.rt = static_cast<int>(e - static_cast<int64_t>(g.b) * tiles);
     g.ri = row_info<kWideUnit>(a, g.b);
     g.rows = min(g.ri.n * a.group - g.rt * kWideRows, kWideRows);
     g.steps = 0;
@@ -262,7 +262,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
         int64_t e = start_e;
         wide_tile(a, tiles, e, g);
         const int64_t rel = u0 - start_begin;
-        g.head = static_cast<int>(rel / g.steps);
+        g.head = static_cast<int>(quotient(rel, g.steps));
         g.begin = start_begin + static_cast<int64_t>(g.head) * g.steps;
         int64_t u = u0;
         for (;;) {

@@ -51,13 +51,20 @@ __device__ __forceinline__ RowInfo row_info(const AttendArgs& a, int b) {
 template <int kUnit>
 __device__ __forceinline__ int row_steps(const RowInfo& r) { return r.n > 0 ? max((r.hi - r.lo + kUnit - 1) / kUnit, 1) : 0; }
 
+// 64-bit quotients of numbers that nearly always fit 32 bits (a 64-bit division is a subroutine of over a hundred instructions).
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+    if (((a | b) >> 31) == 0) return static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
+    return a / b;
+}
+
 // Shares of T units among W workers: the first T mod W have one more.
 struct Shares {
     int64_t base, rem;
-    __device__ __forceinline__ Shares(int64_t T, int W) : base(T / W), rem(T % W) {}
+    __device__ __forceinline__ Shares(int64_t T, int W) : base(quotient(T, W)), rem(T - base * W) {}
     __device__ __forceinline__ int64_t begin(int w) const { return w * base + min(static_cast<int64_t>(w), rem); }
     __device__ __forceinline__ int owner(int64_t u) const {
-        return static_cast<int>(u < rem * (base + 1) ? u / (base + 1) : rem + (u - rem * (base + 1)) / base);
+        const int64_t first = rem * (base + 1);
+        return static_cast<int>(u < first ? quotient(u, base + 1) : rem + quotient(u - first, base));
     }
 };
 

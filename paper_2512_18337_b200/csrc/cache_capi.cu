@@ -108,10 +108,23 @@ int64_t partial_bytes(int64_t rows) {
     return 2ll * kWideMaxCtas * 4 * WidePlan<D>::kPart;
 }
 
+// Dynamic shared memory above the default has to be asked for once per kernel and device.
+template <typename K>
+int allow_shared(K* kernel, int bytes, uint64_t* asked) {   // asked: the kernel's own, one bit per device
+    int dev = 0;
+    SAM_CUDA(cudaGetDevice(&dev));
+    const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
+    if (*asked & bit) return SAM_OK;
+    SAM_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+    *asked |= bit;
+    return SAM_OK;
+}
+
 template <typename T, int D, int NT>
 int launch_stream(const AttendArgs& a, int sms, cudaStream_t s) {
     using Plan = StreamPlan<D, NT>;
-    SAM_CUDA(cudaFuncSetAttribute(attend_stream_kernel<T, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Plan::kSmem));
+    static thread_local uint64_t asked = 0;
+    if (int e = allow_shared(attend_stream_kernel<T, D, NT>, Plan::kSmem, &asked)) return e;
     attend_stream_kernel<T, D, NT><<<std::min(sms * Plan::kCtasPerSm, kMaxCtas), kStreamThreads, Plan::kSmem, s>>>(a);
     return launched();
 }
@@ -119,7 +132,8 @@ int launch_stream(const AttendArgs& a, int sms, cudaStream_t s) {
 template <typename T, int D>
 int launch_wide(const AttendArgs& a, int sms, cudaStream_t s) {
     using Plan = WidePlan<D>;
-    SAM_CUDA(cudaFuncSetAttribute(attend_wide_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Plan::kSmem));
+    static thread_local uint64_t asked = 0;
+    if (int e = allow_shared(attend_wide_kernel<T, D>, Plan::kSmem, &asked)) return e;
     attend_wide_kernel<T, D><<<std::min(sms, kWideMaxCtas), kWideThreads, Plan::kSmem, s>>>(a);
     return launched();
 }
