@@ -99,15 +99,15 @@ struct StreamCursor {
     int b, steps, tiles, head, rt, step;
 
     template <int kRows>
-    __device__ __forceinline__ void enter(const AttendArgs& a, int row) {
+    __device__ __forceinline__ void enter(const AttendArgs& a, int row, const RowInfo& info) {
         b = row;
-        ri = row_info<kStreamUnit>(a, row);
+        ri = info;
         steps = row_steps<kStreamUnit>(ri);
         tiles = (ri.n * a.group + kRows - 1) / kRows;
     }
     template <int kRows>
-    __device__ __forceinline__ void seek(const AttendArgs& a, int row, int64_t row_begin, int64_t u) {
-        enter<kRows>(a, row);
+    __device__ __forceinline__ void seek(const AttendArgs& a, int row, const RowInfo& info, int64_t row_begin, int64_t u) {
+        enter<kRows>(a, row, info);
         base = row_begin;
         const int64_t rel = u - base;
         const int seg = static_cast<int>(quotient(rel, steps));
@@ -125,7 +125,7 @@ struct StreamCursor {
         if (++head < a.c.n_kv) return;
         head = 0;
         base += static_cast<int64_t>(steps) * tiles * a.c.n_kv;
-        do enter<kRows>(a, b + 1);
+        do enter<kRows>(a, b + 1, row_info<kStreamUnit>(a, b + 1));
         while (steps == 0 && b + 1 < a.B);
     }
 };
@@ -167,6 +167,7 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
     __shared__ uint64_t bars[kStreamWarps][kStages];
     __shared__ int64_t scan[kStreamWarps], row_base[kStreamWarps];
     __shared__ int row_of[kStreamWarps];
+    __shared__ RowInfo row_found[kStreamWarps];
     __shared__ StreamPiece pieces[kStreamWarps][2];
     __shared__ int last_here;
 
@@ -175,9 +176,13 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
     const int r = lane >> 2, j = lane & 3;
 
     // ---- how many units there are, and where our share begins
+    int64_t segments = 0;
+    bool count_segments = true;
+    RowInfo ri{};                                          // of the row that the thread looked at last
     auto units_of = [&](int b) -> int64_t {
-        const RowInfo ri = row_info<kStreamUnit>(a, b);
+        ri = row_info<kStreamUnit>(a, b);
         const int tiles = (ri.n * a.group + kRows - 1) / kRows;
+        if (count_segments) segments += tiles * c.n_kv;
         return static_cast<int64_t>(row_steps<kStreamUnit>(ri)) * tiles * c.n_kv;
     };
     auto block_sum = [&](int64_t x, int64_t* before) -> int64_t {   // the total, and the sum over earlier threads
@@ -202,16 +207,22 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
     if (tid < kStreamWarps * kStages) barrier_init(shared_addr(&bars[0][0]) + tid * 8, 1);
     if (tid < kStreamWarps * 2) pieces[tid >> 1][tid & 1].used = 0;
     barrier_init_fence();
-    int64_t units = 0, mine = 0, before = 0;
+    int64_t units = 0, mine = 0, before = 0, unused;
     for (int b0 = 0; b0 < a.B; b0 += kStreamThreads) {
         mine = b0 + tid < a.B ? units_of(b0 + tid) : 0;
         units += block_sum(mine, &before);
     }
-    // every warp of the numbering has at least one unit, but for the last CTA's
-    const int ctas = static_cast<int>(min((units + kStreamWarps - 1) / kStreamWarps, static_cast<int64_t>(gridDim.x)));
+    count_segments = false;
+    segments = block_sum(segments, &unused);
+    // About a unit a warp at least.  With up to two units a warp in a segment, a CTA
+    // per segment: one more unit costs less than joining results across CTAs (one stream, 333 positions: 16.4 -> 11.6 us).
+    const int64_t wanted = segments <= gridDim.x && units <= segments * kStreamWarps * 2 ? segments : (units + kStreamWarps - 1) / kStreamWarps;
+    const int ctas = static_cast<int>(min(wanted, static_cast<int64_t>(gridDim.x)));
     const int cta = blockIdx.x;
     const bool busy = cta < ctas;
-    const Shares shares(units, max(ctas, 1) * kStreamWarps);
+    const Shares shares(units, max(ctas, 1));              // of the CTAs, and of this one's warps
+    const int64_t cta_begin = busy ? shares.begin(cta) : 0, cta_units = busy ? shares.begin(cta + 1) - cta_begin : 0;
+    const Shares warp_shares(cta_units, kStreamWarps);
     if (busy) {
         const bool once = a.B <= kStreamThreads;
         int64_t sum = 0;
@@ -223,10 +234,11 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
                 sum += all;
             }
             for (int w = 0; w < kStreamWarps; ++w) {
-                const int64_t u = shares.begin(cta * kStreamWarps + w);
+                const int64_t u = cta_begin + warp_shares.begin(w);
                 if (u >= before && u < before + mine) {
                     row_of[w] = b0 + tid;
                     row_base[w] = before;
+                    row_found[w] = ri;
                 }
             }
         }
@@ -235,36 +247,40 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
 
     uint8_t* const own = smem + warp * Plan::kPerWarp;
     const uint32_t ring = shared_addr(own), bar0 = shared_addr(&bars[warp][0]);
-    const int64_t u0 = busy ? shares.begin(cta * kStreamWarps + warp) : 0, u1 = busy ? shares.begin(cta * kStreamWarps + warp + 1) : 0;
+    const int64_t u0 = cta_begin + warp_shares.begin(warp), u1 = cta_begin + warp_shares.begin(warp + 1);
     int64_t left = u1 - u0, to_load = left;
     bool gave_up = false;
 
-    // ---- the filling side of the ring
+    // ---- the filling side of the ring: lane l knows where the tiles of step page_step + l are, and issues their copies
     StreamCursor in{}, cur{};
     uint32_t present = 0;              // two bits per stage: which of the unit's tiles are there
-    int page0 = -1, page1 = -1;        // pages of the tiles of step page_step + lane
+    const uint8_t* from0 = nullptr;    // the two tiles of the lane's step
+    const uint8_t* from1 = nullptr;
+    uint32_t have0 = 0, have1 = 0;     // bit l: lane l has them
     int page_step = -1;
     auto fill = [&](int stage) {
         if (to_load == 0) return;
         if (page_step < 0 || in.step - page_step >= 32) {
             page_step = in.step;
-            const int t = in.ri.lo + (page_step + lane) * kStreamUnit, i = t >> c.log_p;
-            page0 = t < in.ri.hi && t >= 0 ? c.page_at(in.ri.s, i) : -1;
-            page1 = c.log_p > 4 ? page0 : t + 16 < in.ri.hi && t >= 0 ? c.page_at(in.ri.s, i + 1) : -1;
+            const int t = in.ri.lo + (page_step + lane) * kStreamUnit, i = t >> c.log_p, slot = t & (c.page_tokens() - 1);
+            const int page0 = t < in.ri.hi && t >= 0 ? c.page_at(in.ri.s, i) : -1;
+            const int page1 = t + 16 >= in.ri.hi || t < 0 ? -1 : c.log_p > 4 ? page0 : c.page_at(in.ri.s, i + 1);
+            from0 = c.tile(max(page0, 0), a.layer, in.head, slot);
+            from1 = c.tile(max(page1, 0), a.layer, in.head, c.log_p > 4 ? slot + 16 : 0);
+            have0 = __ballot_sync(0xffffffffu, page0 >= 0);
+            have1 = __ballot_sync(0xffffffffu, page1 >= 0);
         }
-        const int p0 = __shfl_sync(0xffffffffu, page0, in.step - page_step), p1 = __shfl_sync(0xffffffffu, page1, in.step - page_step);
-        const int t = in.ri.lo + in.step * kStreamUnit;
-        const bool on0 = p0 >= 0, on1 = p1 >= 0 && t + 16 < in.ri.hi;
-        present = (present & ~(3u << (2 * stage))) | (static_cast<uint32_t>(on0) | static_cast<uint32_t>(on1) << 1) << (2 * stage);
-        if (lane == 0) {
+        const int l = in.step - page_step;
+        const uint32_t on = ((have0 >> l) & 1) | ((have1 >> l) & 1) << 1;
+        present = (present & ~(3u << (2 * stage))) | on << (2 * stage);
+        if (lane == l) {
             const uint32_t dst = ring + stage * Plan::kUnitBytes, bar = bar0 + stage * 8;
-            barrier_expect(bar, (static_cast<uint32_t>(on0) + on1) * Plan::kTile);
-            const int slot = t & (c.page_tokens() - 1);
-            if (on0 && on1 && c.log_p > 4) {
-                bulk_load(dst, c.tile(p0, a.layer, in.head, slot), Plan::kUnitBytes, bar);
+            barrier_expect(bar, __popc(on) * Plan::kTile);
+            if (on == 3 && c.log_p > 4) {
+                bulk_load(dst, from0, Plan::kUnitBytes, bar);
             } else {
-                if (on0) bulk_load(dst, c.tile(p0, a.layer, in.head, slot), Plan::kTile, bar);
-                if (on1) bulk_load(dst + Plan::kTile, c.tile(p1, a.layer, in.head, (t + 16) & (c.page_tokens() - 1)), Plan::kTile, bar);
+                if (on & 1) bulk_load(dst, from0, Plan::kTile, bar);
+                if (on & 2) bulk_load(dst + Plan::kTile, from1, Plan::kTile, bar);
             }
         }
         --to_load;
@@ -274,7 +290,7 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
         }
     };
     if (left > 0) {
-        in.seek<kRows>(a, row_of[warp], row_base[warp], u0);
+        in.seek<kRows>(a, row_of[warp], row_found[warp], row_base[warp], u0);
         cur = in;
         for (int s = 0; s < kStages; ++s) fill(s);
     }
@@ -290,7 +306,7 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
         const int count = static_cast<int>(min(left, static_cast<int64_t>(cur.steps - s0)));
         const int rows = cur.ri.n * a.group - cur.rt * kRows;   // query rows of the segment (more than kRows: kRows)
         uint32_t qf[NT][KW][4];
-        float factor[NT][2], m[NT][2], l[NT][2], o[MT][NT][4];
+        float factor[NT][2], m[NT][2], limit[NT][2], l[NT][2], o[MT][NT][4];   // limit: m + kRaiseAt
         int pos[NT][2];
         int first_pos, last_pos;
         {
@@ -326,7 +342,7 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
                 big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
                 e_row = big > 0.f ? 14 - (static_cast<int>(__float_as_uint(big) >> 23) - 127) : 0;
                 e_row = min(e_row, 126);
-                e_scale = pow2(e_row);
+                e_scale = a.scale < 0.f ? -pow2(e_row) : pow2(e_row);   // so that the largest score is the largest product
 #pragma unroll
                 for (int w = 0; w < KW; ++w)
 #pragma unroll
@@ -336,15 +352,15 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
 #pragma unroll
                 for (int w = 0; w < KW; ++w)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) qf[nt][w][k] = reinterpret_cast<const uint32_t*>(x)[w * 4 + k];
+                    for (int k = 0; k < 4; ++k) qf[nt][w][k] = reinterpret_cast<const uint32_t*>(x)[w * 4 + k] ^ (a.scale < 0.f ? 0x80008000u : 0u);
             }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int e_col = __shfl_sync(0xffffffffu, e_row, (2 * j + h) * 4);
-                factor[nt][h] = scale_pow2(a.scale * 1.4426950408889634f, c.k_exp - e_col);
+                factor[nt][h] = scale_pow2(fabsf(a.scale) * 1.4426950408889634f, c.k_exp - e_col);
                 const int col = nt * 8 + 2 * j + h;
                 pos[nt][h] = col < rows ? cur.ri.len + (cur.rt * kRows + col) / a.group : -1;
-                m[nt][h] = -INFINITY;
+                m[nt][h] = limit[nt][h] = -INFINITY;
                 l[nt][h] = 0.f;
             }
 #pragma unroll
@@ -404,33 +420,40 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
                 }
             }
             // ---- softmax over the tokens of the unit
+            if (!full) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            const int t = t0 + h * 16 + tok + (x >> 1) * 8, p = pos[nt][x & 1];
+                            const bool seen = ((here >> h) & 1) && t <= p && (a.window == 0 || t > p - a.window);
+                            s[h][nt][x] = seen ? s[h][nt][x] : -INFINITY;
+                        }
+            }
+            // the largest score of the thread's two columns, against what the reference allows
             bool raise = false;
+            float top[NT][2];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        float y = s[h][nt][x] * factor[nt][x & 1];
-                        if (!full) {
-                            const int t = t0 + h * 16 + tok + (x >> 1) * 8, p = pos[nt][x & 1];
-                            const bool seen = ((here >> h) & 1) && t <= p && (a.window == 0 || t > p - a.window);
-                            y = seen ? y : -INFINITY;
-                        }
-                        s[h][nt][x] = y;
-                        raise |= y > m[nt][x & 1] + kRaiseAt;
-                    }
+                for (int x = 0; x < 2; ++x) {
+                    top[nt][x] = fmaxf(fmaxf(s[0][nt][x], s[0][nt][x + 2]), fmaxf(s[1][nt][x], s[1][nt][x + 2])) * factor[nt][x];
+                    raise |= top[nt][x] > limit[nt][x];
+                }
             if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
-                        float top = fmaxf(fmaxf(s[0][nt][x], s[0][nt][x + 2]), fmaxf(s[1][nt][x], s[1][nt][x + 2]));
+                        float y = top[nt][x];
 #pragma unroll
-                        for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-                        top = fmaxf(top - kAbove, m[nt][x]);
-                        const float keep = m[nt][x] == -INFINITY ? 0.f : exp2_fast(m[nt][x] - top);
-                        m[nt][x] = top;
+                        for (int d = 4; d < 32; d <<= 1) y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, d));
+                        y = fmaxf(y - kAbove, m[nt][x]);
+                        const float keep = m[nt][x] == -INFINITY ? 0.f : exp2_fast(m[nt][x] - y);
+                        m[nt][x] = y;
+                        limit[nt][x] = y + kRaiseAt;
                         l[nt][x] *= keep;
 #pragma unroll
                         for (int mt = 0; mt < MT; ++mt) {
@@ -442,11 +465,11 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
             uint32_t p[2][NT][2];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                const float z0 = m[nt][0] == -INFINITY ? 0.f : m[nt][0], z1 = m[nt][1] == -INFINITY ? 0.f : m[nt][1];
+                const float z0 = m[nt][0] == -INFINITY ? 0.f : -m[nt][0], z1 = m[nt][1] == -INFINITY ? 0.f : -m[nt][1];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const float e0 = exp2_fast(s[h][nt][0] - z0), e1 = exp2_fast(s[h][nt][1] - z1);
-                    const float e2 = exp2_fast(s[h][nt][2] - z0), e3 = exp2_fast(s[h][nt][3] - z1);
+                    const float e0 = exp2_fast(fmaf(s[h][nt][0], factor[nt][0], z0)), e1 = exp2_fast(fmaf(s[h][nt][1], factor[nt][1], z1));
+                    const float e2 = exp2_fast(fmaf(s[h][nt][2], factor[nt][0], z0)), e3 = exp2_fast(fmaf(s[h][nt][3], factor[nt][1], z1));
                     l[nt][0] += e0 + e2;
                     l[nt][1] += e1 + e3;
                     p[h][nt][0] = transpose_8x8(pack_half2(e0, e1));
@@ -614,7 +637,7 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
             const StreamPiece& d = pieces[w0][slot];
             int w1 = w0;
             bool open = d.open;
-            while (open && w1 + 1 < kStreamWarps) open = pieces[++w1][0].open;
+            while (open && w1 + 1 < kStreamWarps && pieces[w1 + 1][0].used) open = pieces[++w1][0].open;
             auto get = [&](int k) {
                 return reinterpret_cast<const float*>(smem + (w0 + k) * Plan::kPerWarp + (k == 0 && slot == 1 ? 0 : Plan::kRing));
             };
@@ -636,7 +659,7 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
         const int at = k ? crossing2 : crossing;
         if (at < 0) break;
         const StreamPiece& d = pieces[at >> 1][at & 1];
-        const int c0 = shares.owner(d.seg_begin) / kStreamWarps, c1 = shares.owner(d.seg_begin + d.steps - 1) / kStreamWarps;
+        const int c0 = shares.owner(d.seg_begin), c1 = shares.owner(d.seg_begin + d.steps - 1);
         __threadfence();
         __syncthreads();
         if (tid == 0) last_here = atomicAdd(&a.counters[c0], 1) == c1 - c0;

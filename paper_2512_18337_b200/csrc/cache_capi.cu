@@ -100,7 +100,7 @@ int launch_read(const CacheView& v, int32_t layer, int32_t B, int32_t Q, const i
 // Workspace of sam_cache_attend: arrival counters (zero between calls), then partial results of up to kMaxCtas CTAs.
 constexpr int kMaxCtas = 512;
 constexpr int64_t kCounterBytes = kMaxCtas * 4;
-constexpr int64_t kNarrowRows = 16;   // query rows per key/value head up to which the streaming kernel is used
+constexpr int64_t kNarrowRows = 32;   // query rows per key/value head up to which the streaming kernel is used
 
 template <int D>
 int64_t partial_bytes(int64_t rows) {
