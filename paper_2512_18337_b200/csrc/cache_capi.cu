@@ -78,22 +78,30 @@ int copy_grid(int64_t pages, int64_t page_bytes, int* grid) {
     return SAM_OK;
 }
 
+// Grid of append and read, and the multiplier that divides by the blocks of a token.
+dim3 io_grid(const CacheView& v, int32_t B, int32_t Q, uint32_t* magic) {
+    const int64_t per_token = static_cast<int64_t>(v.n_kv) * (v.D / 16);
+    *magic = static_cast<uint32_t>(((int64_t(1) << 32) + per_token - 1) / per_token);
+    const int64_t blocks = (Q * per_token + kIoThreads * kIoBlocks - 1) / (kIoThreads * kIoBlocks);
+    return dim3(static_cast<unsigned>(blocks), B, 2);
+}
+
 template <typename T>
 int launch_append(const CacheView& v, int32_t layer, const void* k, const void* vv, KvStrides st, int32_t B, int32_t Q,
                   const int32_t* streams, const int32_t* n_new, cudaStream_t s) {
     const bool wide = aligned(k, 16) && aligned(vv, 16) && st.row % 8 == 0 && st.token % 8 == 0 && st.head % 8 == 0;
-    const int64_t blocks = (static_cast<int64_t>(Q) * v.n_kv * (v.D / 16) * 2 + 255) / 256;
-    append_kernel<T><<<dim3(static_cast<unsigned>(std::min<int64_t>(blocks, 1 << 20)), B), 256, 0, s>>>(
-        v, layer, static_cast<const T*>(k), static_cast<const T*>(vv), st, wide, Q, streams, n_new);
+    uint32_t magic;
+    const dim3 grid = io_grid(v, B, Q, &magic);
+    append_kernel<T><<<grid, kIoThreads, 0, s>>>(v, layer, static_cast<const T*>(k), static_cast<const T*>(vv), st, wide, Q, magic, streams, n_new);
     return launched();
 }
 
 template <typename T>
 int launch_read(const CacheView& v, int32_t layer, int32_t B, int32_t Q, const int32_t* streams, const int32_t* first,
                 const int32_t* n, void* k, void* vv, cudaStream_t s) {
-    const int64_t blocks = (static_cast<int64_t>(Q) * v.n_kv * (v.D / 16) * 2 + 255) / 256;
-    read_kernel<T><<<dim3(static_cast<unsigned>(std::min<int64_t>(blocks, 1 << 20)), B), 256, 0, s>>>(
-        v, layer, Q, streams, first, n, static_cast<T*>(k), static_cast<T*>(vv));
+    uint32_t magic;
+    const dim3 grid = io_grid(v, B, Q, &magic);
+    read_kernel<T><<<grid, kIoThreads, 0, s>>>(v, layer, Q, magic, streams, first, n, static_cast<T*>(k), static_cast<T*>(vv));
     return launched();
 }
 
@@ -260,6 +268,7 @@ int sam_cache_append(const sam_cache* c, int32_t layer, const void* k, const voi
     if (layer < 0 || layer >= c->n_layers || B < 0 || Q < 0 || (dtype != SAM_CACHE_BF16 && dtype != SAM_CACHE_FP16)) return SAM_ERR_INVALID_ARG;
     if (B > SAM_CACHE_MAX_B) return SAM_ERR_TOO_LARGE;
     if (B == 0 || Q == 0) return SAM_OK;
+    if (static_cast<int64_t>(Q) * c->n_kv_heads >= (int64_t(1) << 31)) return SAM_ERR_TOO_LARGE;
     if (!k || !v || !aligned(k, 2) || !aligned(v, 2) || (!streams && B > c->n_streams)) return SAM_ERR_INVALID_ARG;
     const KvStrides st{row_stride, token_stride, head_stride};
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
@@ -274,6 +283,7 @@ int sam_cache_read(const sam_cache* c, int32_t layer, int32_t B, int32_t Q, cons
     if (layer < 0 || layer >= c->n_layers || B < 0 || Q < 0 || (dtype != SAM_CACHE_BF16 && dtype != SAM_CACHE_FP16)) return SAM_ERR_INVALID_ARG;
     if (B > SAM_CACHE_MAX_B) return SAM_ERR_TOO_LARGE;
     if (B == 0 || Q == 0) return SAM_OK;
+    if (static_cast<int64_t>(Q) * c->n_kv_heads >= (int64_t(1) << 31)) return SAM_ERR_TOO_LARGE;
     if (!k_out || !v_out || !aligned(k_out, 16) || !aligned(v_out, 16) || (!streams && B > c->n_streams)) return SAM_ERR_INVALID_ARG;
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     return dtype == SAM_CACHE_BF16 ? launch_read<__nv_bfloat16>(view(c), layer, B, Q, streams, first, n, k_out, v_out, s)
