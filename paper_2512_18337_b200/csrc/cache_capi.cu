@@ -212,7 +212,7 @@ int sam_cache_commit(const sam_cache* c, int32_t B, const int32_t* streams, cons
     if (B > SAM_CACHE_MAX_B) return SAM_ERR_TOO_LARGE;
     if (B == 0) return SAM_OK;
     if (B > c->n_streams || !n_keep) return SAM_ERR_INVALID_ARG;
-    commit_kernel<<<1, kPageThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(view(c), B, streams, n_keep);
+    commit_kernel<<<1, kPageThreads, (B + 1) * 4, static_cast<cudaStream_t>(cuda_stream)>>>(view(c), B, streams, n_keep);
     return launched();
 }
 

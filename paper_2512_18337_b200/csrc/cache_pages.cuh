@@ -65,6 +65,16 @@ __device__ __forceinline__ int block_scan(int x, int* total) {
     return y - x + (warp ? sums[warp - 1] : 0);
 }
 
+// Sum over the block, known to all threads.
+__device__ __forceinline__ int block_sum(int x) {
+    __shared__ int sums[32];
+    x = __reduce_add_sync(0xffffffffu, x);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = x;
+    __syncthreads();
+    return __reduce_add_sync(0xffffffffu, (threadIdx.x & 31) < (blockDim.x >> 5) ? sums[threadIdx.x & 31] : 0);
+}
+
 __global__ void cache_init_kernel(CacheView c) {
     const int64_t i0 = blockIdx.x * static_cast<int64_t>(blockDim.x) + threadIdx.x, step = static_cast<int64_t>(gridDim.x) * blockDim.x;
     for (int64_t i = i0; i < static_cast<int64_t>(c.n_streams) * c.max_pages; i += step) c.table[i] = -1;
@@ -93,51 +103,55 @@ __device__ __forceinline__ RowNeed row_need(const CacheView& c, const int32_t* s
     return r;
 }
 
-// One block.  Row state kept in scratch between the phases: row_a = the page to be copied (or -1), row_b = 1 when this
-// row keeps a page whose count the phases have taken to zero.
+// One block; a thread looks after up to four rows and keeps them in registers.  What a step costs is the chain of dependent
+// loads (stream, length, table, counts), so each of them is made once.
+constexpr int kRowsPerThread = 4;   // SAM_CACHE_MAX_B / kPageThreads
 __global__ void __launch_bounds__(kPageThreads) reserve_kernel(CacheView c, int B, const int32_t* streams, const int32_t* n_new) {
     const PageScratch sc = page_scratch(c);
     __shared__ int bad, copies;
     if (threadIdx.x == 0) bad = copies = 0;
     __syncthreads();
-    // writers of a page leave it: a count of zero means that all its holders write
-    for (int b = threadIdx.x; b < B; b += kPageThreads) {
-        const RowNeed r = row_need(c, streams, n_new, b);
-        if (r.want > c.max_pages) bad = 1;
-        if (r.page0 >= 0) atomicSub(&c.ref[r.page0], 1);
-        sc.row_a[b] = r.page0;
-    }
-    __syncthreads();
-    for (int b = threadIdx.x; b < B; b += kPageThreads) sc.row_b[b] = sc.row_a[b] >= 0 && __ldcg(&c.ref[sc.row_a[b]]) == 0;
-    __syncthreads();
-    for (int b = threadIdx.x; b < B; b += kPageThreads)
-        if (sc.row_b[b]) atomicMax(&c.ref[sc.row_a[b]], b + 1);
-    __syncthreads();
-    for (int b = threadIdx.x; b < B; b += kPageThreads)
-        if (sc.row_b[b]) sc.row_b[b] = __ldcg(&c.ref[sc.row_a[b]]) == b + 1 ? 2 : 1;   // 2: the last of them, which keeps the page
-    __syncthreads();
-    int need_all = 0;
-    for (int b0 = 0; b0 < B; b0 += kPageThreads) {
-        const int b = b0 + threadIdx.x;
-        int need = 0;
-        if (b < B) {
-            const RowNeed r = row_need(c, streams, n_new, b);
-            need = r.page0 >= 0 && sc.row_b[b] != 2;
-            for (int i = r.first; i < min(r.want, c.max_pages); ++i) need += c.page_at(r.s, i) < 0;
-        }
-        int total;
-        block_scan(need, &total);
-        need_all += total;
-    }
     const int n_free = c.meta[0];
-    const bool ok = !bad && need_all <= n_free;
+    RowNeed r[kRowsPerThread];
+    int need[kRowsPerThread];
+    bool sole[kRowsPerThread], keeper[kRowsPerThread];
+    // writers of a page leave it: a count of zero means that all its holders write
+#pragma unroll
+    for (int u = 0; u < kRowsPerThread; ++u) {
+        const int b = u * kPageThreads + threadIdx.x;
+        r[u].s = r[u].page0 = -1;
+        r[u].first = r[u].want = need[u] = 0;
+        if (b >= B) continue;
+        r[u] = row_need(c, streams, n_new, b);
+        if (r[u].want > c.max_pages) bad = 1;
+        if (r[u].page0 >= 0) atomicSub(&c.ref[r[u].page0], 1);
+        for (int i = r[u].first; i < min(r[u].want, c.max_pages); ++i) need[u] += c.page_at(r[u].s, i) < 0;
+    }
     __syncthreads();
-    if (!ok) {   // put the counts back
-        for (int b = threadIdx.x; b < B; b += kPageThreads)
-            if (sc.row_b[b] == 2) c.ref[sc.row_a[b]] = 0;
+#pragma unroll
+    for (int u = 0; u < kRowsPerThread; ++u) sole[u] = r[u].page0 >= 0 && __ldcg(&c.ref[r[u].page0]) == 0;
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kRowsPerThread; ++u)
+        if (sole[u]) atomicMax(&c.ref[r[u].page0], u * kPageThreads + threadIdx.x + 1);
+    __syncthreads();
+    int mine = 0;
+#pragma unroll
+    for (int u = 0; u < kRowsPerThread; ++u) {
+        // the last of the rows that write keeps the page
+        keeper[u] = sole[u] && __ldcg(&c.ref[r[u].page0]) == static_cast<int>(u * kPageThreads + threadIdx.x + 1);
+        need[u] += r[u].page0 >= 0 && !keeper[u];
+        mine += need[u];
+    }
+    const int need_all = block_sum(mine);
+    if (bad || need_all > n_free) {   // put the counts back
+#pragma unroll
+        for (int u = 0; u < kRowsPerThread; ++u)
+            if (keeper[u]) c.ref[r[u].page0] = 0;
         __syncthreads();
-        for (int b = threadIdx.x; b < B; b += kPageThreads)
-            if (sc.row_a[b] >= 0) atomicAdd(&c.ref[sc.row_a[b]], 1);
+#pragma unroll
+        for (int u = 0; u < kRowsPerThread; ++u)
+            if (r[u].page0 >= 0) atomicAdd(&c.ref[r[u].page0], 1);
         if (threadIdx.x == 0) {
             c.meta[1] |= bad ? kStatusTableFull : kStatusOutOfPages;
             *sc.count = 0;
@@ -145,33 +159,25 @@ __global__ void __launch_bounds__(kPageThreads) reserve_kernel(CacheView c, int 
         return;
     }
     int before = 0;
-    for (int b0 = 0; b0 < B; b0 += kPageThreads) {
-        const int b = b0 + threadIdx.x;
-        RowNeed r;
-        r.s = -1;
-        r.first = r.want = 0;
-        int need = 0;
-        bool copy = false;
-        if (b < B) {
-            r = row_need(c, streams, n_new, b);
-            if (r.page0 >= 0 && sc.row_b[b] == 2) c.ref[r.page0] = 1;
-            copy = r.page0 >= 0 && sc.row_b[b] != 2;
-            need = copy;
-            for (int i = r.first; i < r.want; ++i) need += c.page_at(r.s, i) < 0;
-        }
+#pragma unroll
+    for (int u = 0; u < kRowsPerThread; ++u) {
+        if (u * kPageThreads >= B) break;
         int total;
-        int at = n_free - 1 - before - block_scan(need, &total);
+        int at = n_free - 1 - before - block_scan(need[u], &total);
         before += total;
-        for (int i = r.first; i < r.want; ++i) {
-            const bool replace = copy && i == r.first;
-            if (!replace && c.page_at(r.s, i) >= 0) continue;
+        if (keeper[u]) c.ref[r[u].page0] = 1;
+        const bool copy = r[u].page0 >= 0 && !keeper[u];
+        if (need[u] == 0) continue;
+        for (int i = r[u].first; i < r[u].want; ++i) {
+            const bool replace = copy && i == r[u].first;
+            if (!replace && c.page_at(r[u].s, i) >= 0) continue;
             const int page = c.free_list[at--];
             if (replace) {
                 const int k = atomicAdd(&copies, 1);   // the order of the copies does not matter
-                sc.from[k] = r.page0;
+                sc.from[k] = r[u].page0;
                 sc.to[k] = page;
             }
-            c.row(r.s)[i] = page;
+            c.row(r[u].s)[i] = page;
             if (static_cast<unsigned>(page) < static_cast<unsigned>(c.n_pages)) c.ref[page] = 1;
         }
     }
@@ -206,101 +212,103 @@ __global__ void __launch_bounds__(kCopyThreads) copy_pages_kernel(const uint8_t*
     }
 }
 
-// One block, a warp per row.  The pages that a row gives up are numbered in order of rows, then of positions; a page
-// whose count reaches zero is pushed by its lowest number, which the warps find by an atomic minimum in the count itself.
+// One block.  The pages that rows give up are numbered in order of rows, then of positions; a page whose count reaches zero is
+// pushed by its lowest number, which an atomic minimum in the count itself finds.  First a thread per row moves the lengths on
+// and looks whether there is anything behind them: mostly there is not, and the call ends after one chain of loads.  Otherwise
+// the given-up pages are worked on one per thread, found by a binary search among the rows' first numbers.
 __global__ void __launch_bounds__(kPageThreads) commit_kernel(CacheView c, int B, const int32_t* streams, const int32_t* n_keep) {
     const PageScratch sc = page_scratch(c);
+    extern __shared__ int begin[];          // [rows that give up pages + 1]
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    constexpr int kWarps = kPageThreads / 32;
-    auto keep_pages = [&](int s) { return (c.seq_len[s] + c.page_tokens() - 1) >> c.log_p; };
-
-    for (int b = warp; b < B; b += kWarps) {
-        const int s = c.stream_of(streams, b);
-        int gone = 0;
+    const int n_free = c.meta[0];
+    int rows = 0;
+    for (int b0 = 0; b0 < B; b0 += kPageThreads) {
+        const int b = b0 + threadIdx.x;
+        const int s = b < B ? c.stream_of(streams, b) : -1;
+        int keep = c.max_pages;
+        bool gives = false;
         if (s >= 0) {
             const int64_t len = min(max(static_cast<int64_t>(c.length_of(s)) + n_keep[b], int64_t(0)), static_cast<int64_t>(c.capacity()));
-            __syncwarp();
-            if (lane == 0) c.seq_len[s] = static_cast<int>(len);
-            const int keep = static_cast<int>((len + c.page_tokens() - 1) >> c.log_p);
-            for (int i0 = keep; i0 < c.max_pages; i0 += 32) {
-                const int page = i0 + lane < c.max_pages ? c.page_at(s, i0 + lane) : -1;
-                const unsigned none = __ballot_sync(0xffffffffu, page < 0);
-                const int n = none ? __ffs(none) - 1 : 32;
-                if (lane < n) atomicSub(&c.ref[page], 1);
-                gone += n;
-                if (n < 32) break;
+            keep = static_cast<int>((len + c.page_tokens() - 1) >> c.log_p);
+            gives = keep < c.max_pages && c.page_at(s, keep) >= 0;
+            c.seq_len[s] = static_cast<int>(len);
+        }
+        if (!__syncthreads_or(gives)) continue;
+        int total;
+        const int at = rows + block_scan(gives, &total);
+        if (gives) {
+            sc.row_a[at] = s;
+            sc.row_b[at] = keep;
+        }
+        rows += total;
+    }
+    if (rows == 0) return;
+    __syncthreads();
+    // how many: up to the table's first -1
+    for (int k = warp; k < rows; k += kPageThreads / 32) {
+        const int s = sc.row_a[k], keep = sc.row_b[k];
+        int gone = 0;
+        for (int i0 = keep; i0 < c.max_pages; i0 += 128) {
+            unsigned none[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int i = i0 + u * 32 + lane;
+                none[u] = __ballot_sync(0xffffffffu, i >= c.max_pages || c.page_at(s, min(i, c.max_pages - 1)) < 0);
             }
+            int n = 0;
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (n == u * 32) n += none[u] ? __ffs(none[u]) - 1 : 32;
+            gone += n;
+            if (n < 128) break;
         }
-        if (lane == 0) sc.row_a[b] = gone;
+        if (lane == 0) begin[k] = gone;
     }
     __syncthreads();
-    // numbers of the rows' first given-up pages
-    int base = 0;
-    for (int b0 = 0; b0 < B; b0 += kPageThreads) {
-        const int b = b0 + threadIdx.x;
+    int all = 0;
+    for (int k0 = 0; k0 < rows; k0 += kPageThreads) {
+        const int k = k0 + threadIdx.x;
         int total;
-        const int at = block_scan(b < B ? sc.row_a[b] : 0, &total);
-        if (b < B) sc.row_b[b] = base + at;
-        base += total;
+        const int at = block_scan(k < rows ? begin[k] : 0, &total);
+        if (k < rows) begin[k] = all + at;
+        all += total;
     }
-    if (base == 0) return;
+    if (threadIdx.x == 0) begin[rows] = all;
     __syncthreads();
-    for (int b = warp; b < B; b += kWarps) {
-        const int gone = sc.row_a[b];
-        if (!gone) continue;
-        const int s = c.stream_of(streams, b), keep = keep_pages(s);
-        for (int i = lane; i < gone; i += 32) {
-            const int page = c.page_at(s, keep + i);
-            if (__ldcg(&c.ref[page]) <= 0) atomicMin(&c.ref[page], sc.row_b[b] + i - kClaim);
+    auto entry = [&](int e) -> int32_t* {   // table entry of given-up page e
+        int lo = 0, hi = rows - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (begin[mid] <= e) lo = mid;
+            else hi = mid - 1;
         }
+        return c.row(sc.row_a[lo]) + sc.row_b[lo] + (e - begin[lo]);
+    };
+#pragma unroll 4
+    for (int e = threadIdx.x; e < all; e += kPageThreads) atomicSub(&c.ref[*entry(e)], 1);
+    __syncthreads();
+#pragma unroll 4
+    for (int e = threadIdx.x; e < all; e += kPageThreads) {
+        int32_t* count = &c.ref[*entry(e)];
+        if (__ldcg(count) <= 0) atomicMin(count, e - kClaim);
     }
     __syncthreads();
-    for (int b = warp; b < B; b += kWarps) {
-        const int gone = sc.row_a[b];
-        int freed = 0;
-        if (gone) {
-            const int s = c.stream_of(streams, b), keep = keep_pages(s);
-            for (int i = lane; i < gone; i += 32) freed += __ldcg(&c.ref[c.page_at(s, keep + i)]) == sc.row_b[b] + i - kClaim;
-            freed = __reduce_add_sync(0xffffffffu, freed);
-        }
-        if (lane == 0) sc.to[b] = freed;
-    }
-    __syncthreads();
-    const int n_free = c.meta[0];
     int pushed = 0;
-    for (int b0 = 0; b0 < B; b0 += kPageThreads) {
-        const int b = b0 + threadIdx.x;
+    for (int e0 = 0; e0 < all; e0 += kPageThreads) {
+        const int e = e0 + threadIdx.x;
+        const int page = e < all ? *entry(e) : -1;
+        const bool mine = page >= 0 && __ldcg(&c.ref[page]) == e - kClaim;
         int total;
-        const int at = block_scan(b < B ? sc.to[b] : 0, &total);
-        if (b < B) sc.from[b] = n_free + pushed + at;
+        const int at = n_free + pushed + block_scan(mine, &total);
+        if (mine && at < c.n_pages) c.free_list[at] = page;
         pushed += total;
     }
     __syncthreads();
-    for (int b = warp; b < B; b += kWarps) {
-        const int gone = sc.row_a[b];
-        if (!gone) continue;
-        const int s = c.stream_of(streams, b), keep = keep_pages(s);
-        int at = sc.from[b];
-        for (int i0 = 0; i0 < gone; i0 += 32) {
-            const int i = i0 + lane;
-            const int page = i < gone ? c.page_at(s, keep + i) : -1;
-            const bool mine = page >= 0 && __ldcg(&c.ref[page]) == sc.row_b[b] + i - kClaim;
-            const unsigned m = __ballot_sync(0xffffffffu, mine);
-            const int k = at + __popc(m & ((1u << lane) - 1));
-            if (mine && k < c.n_pages) c.free_list[k] = page;
-            at += __popc(m);
-        }
-    }
-    __syncthreads();
-    for (int b = warp; b < B; b += kWarps) {
-        const int gone = sc.row_a[b];
-        if (!gone) continue;
-        const int s = c.stream_of(streams, b), keep = keep_pages(s);
-        for (int i = lane; i < gone; i += 32) {
-            const int page = c.page_at(s, keep + i);
-            if (__ldcg(&c.ref[page]) < 0) c.ref[page] = 0;
-            c.row(s)[keep + i] = -1;
-        }
+#pragma unroll 4
+    for (int e = threadIdx.x; e < all; e += kPageThreads) {
+        int32_t* at = entry(e);
+        if (__ldcg(&c.ref[*at]) < 0) c.ref[*at] = 0;
+        *at = -1;
     }
     if (threadIdx.x == 0) c.meta[0] = min(n_free + pushed, c.n_pages);
 }
@@ -323,35 +331,45 @@ __global__ void __launch_bounds__(256) fork_kernel(CacheView c, const int32_t* s
     if (threadIdx.x == 0) c.seq_len[z] = len;
 }
 
-// One block: ranks the pages, lists the moves and where each page will be, and moves the counts.
+// One block: ranks the pages, lists the moves and where each page will be, and moves the counts.  A thread has eight pages in
+// each round, so that a pool of 30,000 pages takes four.
+constexpr int kPlanPages = 8;
 __global__ void __launch_bounds__(kPageThreads) compact_plan_kernel(CacheView c) {
     const PageScratch sc = page_scratch(c);
-    int live = 0;
-    for (int p0 = 0; p0 < c.n_pages; p0 += kPageThreads) {
-        const int p = p0 + threadIdx.x;
-        live += __syncthreads_count(p < c.n_pages && c.ref[p] > 0);
-    }
-    int below = 0, at_boundary = 0;   // live pages below p0; below `live`
-    for (int p0 = 0; p0 < c.n_pages; p0 += kPageThreads) {
-        const int p = p0 + threadIdx.x;
-        const bool on = p < c.n_pages && c.ref[p] > 0;
+    __shared__ int boundary;
+    constexpr int kRound = kPageThreads * kPlanPages;
+    auto live_bits = [&](int p) {          // of pages p .. p + 7
+        unsigned m = 0;
+#pragma unroll
+        for (int i = 0; i < kPlanPages; ++i) m |= static_cast<unsigned>(p + i < c.n_pages && c.ref[min(p + i, c.n_pages - 1)] > 0) << i;
+        return m;
+    };
+    int mine = 0;
+    for (int p0 = 0; p0 < c.n_pages; p0 += kRound) mine += __popc(live_bits(p0 + threadIdx.x * kPlanPages));
+    const int live = block_sum(mine);
+    if (threadIdx.x == 0) boundary = live;  // live pages below page `live`; that many when there is no such page
+    int below = 0;
+    for (int p0 = 0; p0 < c.n_pages; p0 += kRound) {
+        const int p = p0 + threadIdx.x * kPlanPages;
+        const unsigned m = live_bits(p);
         int total;
-        const int rank = below + block_scan(on, &total);   // live pages below p
-        if (live >= p0 && live < p0 + kPageThreads) {
-            __shared__ int r;
-            if (p == live) r = rank;
-            __syncthreads();
-            at_boundary = r;
-        }
-        if (p < c.n_pages) {
-            if (on && p >= live) sc.from[rank - at_boundary] = p;
-            if (!on && p < live) sc.to[p - rank] = p;
-            sc.remap[p] = p;
+        const int rank = below + block_scan(__popc(m), &total);   // live pages below p
+        if (p <= live && live < p + kPlanPages) boundary = rank + __popc(m & ((1u << (live - p)) - 1));
+        __syncthreads();
+        const int edge = boundary;
+#pragma unroll
+        for (int i = 0; i < kPlanPages; ++i) {
+            if (p + i >= c.n_pages) break;
+            const int r = rank + __popc(m & ((1u << i) - 1));
+            const bool on = (m >> i) & 1;
+            if (on && p + i >= live) sc.from[r - edge] = p + i;
+            if (!on && p + i < live) sc.to[p + i - r] = p + i;
+            sc.remap[p + i] = p + i;
         }
         below += total;
     }
     __syncthreads();
-    const int moves = live == c.n_pages ? 0 : live - at_boundary;
+    const int moves = live - boundary;
     for (int k = threadIdx.x; k < moves; k += kPageThreads) {
         const int f = sc.from[k], t = sc.to[k];
         sc.remap[f] = t;
