@@ -357,7 +357,7 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int e_col = __shfl_sync(0xffffffffu, e_row, (2 * j + h) * 4);
-                factor[nt][h] = scale_pow2(fabsf(a.scale) * 1.4426950408889634f, c.k_exp - e_col);
+                factor[nt][h] = score_factor(a.scale, c.k_exp - e_col);
                 const int col = nt * 8 + 2 * j + h;
                 pos[nt][h] = col < rows ? cur.ri.len + (cur.rt * kRows + col) / a.group : -1;
                 m[nt][h] = limit[nt][h] = -INFINITY;

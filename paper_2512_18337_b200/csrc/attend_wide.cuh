@@ -352,7 +352,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
 #pragma unroll
                     for (int i = 0; i < kHalf / 2; ++i) x[i] ^= 0x80008000u;
                 }
-                factor = scale_pow2(fabsf(a.scale) * 1.4426950408889634f, c.k_exp - e);
+                factor = score_factor(a.scale, c.k_exp - e);
 #pragma unroll
                 for (int i = 0; i < kHalf / 2; i += 16) tmem_store16(lanes + kColQ + part_no * (kHalf / 2) + i, reinterpret_cast<const uint32_t(&)[16]>(x[i]));
                 tmem_store_wait();

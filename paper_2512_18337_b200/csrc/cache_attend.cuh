@@ -74,6 +74,12 @@ __device__ __forceinline__ float scale_pow2(float x, int e) {
     return x * pow2(h) * pow2(min(max(e, -250), 250) - h);
 }
 
+// From a product of queries and keys (scaled by 2^-e, with the sign of the scale in it) to a score in powers of two.  Never zero,
+// so that a masked score of minus infinity stays one; the least value leaves nothing of any product.
+__device__ __forceinline__ float score_factor(float scale, int e) {
+    return fmaxf(scale_pow2(fabsf(scale) * 1.4426950408889634f, e), 1.17549435e-38f);
+}
+
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

@@ -322,3 +322,96 @@ def test_long_offsets():
         _check(out[b], lse[b], R.attend(q[b].double().cpu().numpy(), kk, vv, np.ones(n0 + 9, bool), n0, 9, 1, D ** -0.5, 0),
                "bf16", D)
     assert math.isfinite(float(lse.max()))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("D,Q,H,Hkv,P", [(128, 12, 32, 8, 16), (64, 9, 40, 8, 64), (128, 5, 32, 8, 32), (64, 2, 32, 8, 16), (128, 1, 24, 8, 128)])
+def test_attend_many_steps(D, Q, H, Hkv, P, dtype):
+    """Enough units for several per warp and CTA, and scores that climb along the context, so that the reference of the
+    weights has to be raised again and again, and row by row at different places."""
+    rng = np.random.default_rng(D + Q)
+    lengths = [2600, 1900, 40, 2222]
+    c, raw, table = _cache(rng, lengths, [Q] * 4, P, Hkv, D, n_layers=1)
+    # the scales of the keys grow with the position: 2^-3 .. 2^3
+    for s in range(4):
+        for i, page in enumerate(table[s][table[s] >= 0]):
+            for t in range(P // 16):
+                e = min(0x50, 0x20 + 8 * ((i * P + t * 16) * 6 // 2600))
+                raw[page, 0, :, t, 16 * D:17 * D] = np.minimum(raw[page, 0, :, t, 16 * D:17 * D] & 7 | e, 0x57)
+    c.pages.copy_(torch.from_numpy(raw))
+    q = torch.from_numpy(rng.standard_normal((4, Q, H, D)) * rng.uniform(0.05, 1.5, (4, Q, H, 1))).to(DEV, DT[dtype])
+    out, lse = c.attend(0, q)
+    for b in range(4):
+        k, v, there = _tokens(raw, table, b, 0, P, D, (0, -3))
+        _check(out[b], lse[b], R.attend(q[b].double().cpu().numpy(), k, v, there, lengths[b], Q, H // Hkv, D ** -0.5, 0), dtype, D)
+    assert c.status()[1] == 0
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.09, 1e-30])
+@pytest.mark.parametrize("Q", [1, 4, 40])
+def test_attend_scales(scale, Q):
+    """No scale, a negative one, and one that makes all weights alike."""
+    rng = np.random.default_rng(12)
+    c, raw, table = _cache(rng, [333], [Q], 16, 2, 128)
+    q = torch.from_numpy(rng.standard_normal((1, Q, 8, 128))).to(DEV, torch.bfloat16)
+    out, lse = c.attend(1, q, scale=scale)
+    k, v, there = _tokens(raw, table, 0, 1, 16, 128, (0, -3))
+    _check(out[0], lse[0], R.attend(q[0].double().cpu().numpy(), k, v, there, 333, Q, 4, scale, 0), "bf16", 128)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Q,H", [(6, 1), (6, 4), (6, 8)])
+def test_nan_reaches_only_the_rows_that_see_it(Q, H, D):
+    """A NaN among the values of a token: earlier rows, and rows whose window has passed it, do not know of it; the others have it
+    in its 16 channels only.  Among the keys: the rows that see it are NaN, the others are not."""
+    window = 4
+    rng = np.random.default_rng(13)
+    for where in ("value", "key"):
+        c, _, _ = _cache(rng, [70], [Q], 16, 1, D, n_layers=1)
+        kv = torch.from_numpy(rng.standard_normal((2, 1, Q, 1, D))).to(DEV, torch.bfloat16)
+        kv[1 if where == "value" else 0, 0, 1, 0, 37] = float("nan")
+        c.append(0, kv[0], kv[1])
+        q = torch.from_numpy(rng.standard_normal((1, Q, H, D))).to(DEV, torch.bfloat16)
+        for win, seen in ((0, range(1, Q)), (window, range(1, 1 + window))):
+            out, lse = c.attend(0, q, window=win)
+            nan = out[0].isnan()
+            for i in range(Q):
+                want = torch.zeros(H, D, dtype=torch.bool, device=DEV)
+                if i in seen:
+                    want[:, 32:48] = True
+                    if where == "key":
+                        want[:] = True
+                assert torch.equal(nan[i], want), (where, win, i)
+                assert bool(lse[0, i].isnan().all()) == (where == "key" and i in seen)
+
+
+def test_attend_refuses_what_does_not_fit():
+    c = S.SamCache(4, 16, 2, 2, 1, 2, 64, device=DEV)
+    q = torch.zeros(2, 1, 4, 64, dtype=torch.bfloat16, device=DEV)
+    i32 = torch.zeros(2, dtype=torch.int32, device=DEV)
+    for bad in (q.float(), q[..., :32], q[0], q.transpose(2, 3), q.cpu()):
+        with pytest.raises(ValueError):
+            c.attend(0, bad)
+    for kw in (dict(out=q.half()), dict(out=q[:1]), dict(lse=torch.zeros(2, 1, 4, device=DEV).half()), dict(n_new=i32[:1]),
+               dict(streams=i32.long())):
+        with pytest.raises(ValueError):
+            c.attend(0, q, **kw)
+    with pytest.raises(S.SamError) as e:
+        c.attend(1, q)
+    assert e.value.status == -1
+    with pytest.raises(S.SamError):
+        c.attend(0, q[:, :, :3])                       # three query heads over two key heads
+    with pytest.raises(S.SamError) as e:
+        c.attend(0, q, workspace=torch.zeros(512, dtype=torch.uint8, device=DEV))
+    assert e.value.status == -5
+    k = torch.zeros(2, 1, 2, 64, dtype=torch.bfloat16, device=DEV)
+    with pytest.raises(ValueError):
+        c.append(0, k, k.half())
+    with pytest.raises(ValueError):
+        c.append(0, k[:, :, :1], k[:, :, :1])
+    with pytest.raises(ValueError):
+        c.append(0, k, k.expand(2, 1, 2, 64).transpose(0, 1).contiguous().transpose(0, 1), n_new=i32.float())
+    with pytest.raises(ValueError):
+        c.read(0, out=(k, k.half()))
+    with pytest.raises(ValueError):
+        S.SamCache(4, 16, 2, 2, 1, 2, 64, device=DEV, tensors=dict(seq_len=i32.long()))
