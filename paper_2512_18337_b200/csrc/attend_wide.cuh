@@ -167,13 +167,13 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const uint32_t sm = shared_addr(smem), bar = shared_addr(bars);
-    // barriers: scores ready, keys and values ready, product done (two each), weights ready, queries
-    // ready
+    // barriers, two each: scores ready, first keys ready, product done, step ready; and queries ready
     auto score_bar = [&](int i) { return bar + 8 * i; };
-    auto k_full = [&](int i) { return bar + 16 + 8 * i; };
-    auto v_full = [&](int i) { return bar + 48 + 8 * i; };
+    auto k_first = [&](int i) { return bar + 16 + 8 * i; };
     auto product_bar = [&](int i) { return bar + 80 + 8 * i; };
-    auto weight_bar = [&](int i) { return bar + 96 + 8 * i; };   // two: a softmax warp may be a step ahead of another
+    // Step n may go on when its weights (eight warps), its values (four) and the keys of step n + 2 (four) are there: one wait of the
+    // issuing warp, where three of them took as long as the products themselves.
+    auto ready_bar = [&](int i) { return bar + 96 + 8 * i; };
     const uint32_t query_bar = bar + 112;
     // Gives up after kCachePolls polls, and at once when some wait of the CTA has: everybody then runs on without waiting, the
     // results are not valid, and the status says so.
@@ -187,10 +187,9 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
             barrier_init(score_bar(i), 1);
-            barrier_init(k_full(i), 4);
-            barrier_init(v_full(i), 4);
+            barrier_init(k_first(i), 4);
             barrier_init(product_bar(i), 1);
-            barrier_init(weight_bar(i), 8);
+            barrier_init(ready_bar(i), 16);
         }
         barrier_init(query_bar, 8);
         abort_flag = 0;
@@ -281,9 +280,9 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
             }
         }
     };
-    auto seen_by_all = [&](const WideSegment& g, int t0) {
-        return t0 + kWideUnit - 1 <= g.first_pos && (a.window == 0 || t0 > g.last_pos - a.window);
-    };
+    // Steps that begin at or before the first number and after the second are seen by all rows of the segment.
+    auto all_until = [&](const WideSegment& g) { return g.first_pos - (kWideUnit - 1); };
+    auto all_after = [&](const WideSegment& g) { return a.window == 0 ? -1 : g.last_pos - a.window; };
 
     // Registers go where they are needed: 256 threads x 96, 512 x 64, 128 x 48, of 896 x 72 at launch.
     if (warp < 8) {
@@ -365,15 +364,23 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
             uint32_t nan_blocks = 0;
 
             // ---- steps
+            const int until = all_until(seg), after = all_after(seg), base = seg.ri.lo + s0 * kWideUnit;
+            auto hand_over = [&](uint32_t i) {           // the weights of step i to the second product
+                tmem_store_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) barrier_arrive(ready_bar(i & 1));
+            };
 #pragma unroll 1
             for (int k = 0; k < count; ++k, ++n) {
                 const uint32_t s_at = lanes + kColS + (n & 1) * 128 + part_no * 64;
                 wait(score_bar(n & 1), (n >> 1) & 1);
+                if (k > 0) hand_over(n - 1);             // the weights of the step before are stored by now
                 tc_fence_after();
-                const int t0 = seg.ri.lo + (s0 + k) * kWideUnit, ring = n & 3;
+                const int t0 = base + k * kWideUnit, ring = n & 3;
                 uint32_t on = *reinterpret_cast<volatile uint32_t*>(tile_there[ring]);
                 on = (on * 0x01041040u) >> 24;            // two bits of each byte, side by side
-                const bool all = seen_by_all(seg, t0);
+                const bool all = t0 <= until && t0 > after;
                 // Weights with the reference at hand, in one pass: a sum of at most kTotalMax means that each of them is within fp16.
                 // Where that fails, and where there are masks, the step is done in two passes, the largest score first.
                 bool done = false;
@@ -473,11 +480,8 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                         tmem_store16(s_at + q * 16, p);      // behind the scores that are still to be read
                     }
                 }
-                tmem_store_wait();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) barrier_arrive(weight_bar(n & 1));
             }
+            hand_over(n - 1);
 
             // ---- the piece's result
             product(n - 1);
@@ -598,12 +602,13 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
         const uint32_t sel0 = D == 64 || !swap ? 0x1010 : 0x3232, sel1 = D == 64 || swap ? 0x1010 : 0x3232;
         constexpr int kCodeParts = 8 * D / 512;            // warp-wide copies of a tile's codes
         constexpr int kScaleLanes = D / 16;                // sixteen-byte parts of a tile's scales
-        const uint32_t full_bar = (values ? v_full(0) : k_full(0)) + 8 * stage, empty_bar = (values ? product_bar(0) : score_bar(0)) + 8 * stage;   // done with: by the products
+        const uint32_t full_bar = ready_bar(stage), empty_bar = (values ? product_bar(0) : score_bar(0)) + 8 * stage;   // done with: by the products
         const int tile_mask = (c.page_tokens() >> 4) - 1;
         const uint32_t page_bytes = static_cast<uint32_t>(c.page_bytes >> 7);   // pages are multiples of 128 bytes
         uint32_t n = 0;                                    // steps in earlier pieces
         for_pieces([&](const WideSegment& g, int s0, int count) {
             const uint8_t* const head = c.head_tiles(0, a.layer, g.head) + (values ? 8 * D : 0) + lane * 16;
+            const int until = all_until(g), after = all_after(g), base = g.ri.lo + s0 * kWideUnit, hi_token = g.ri.hi;
             const int tile0 = (g.ri.lo >> 4) + w * 2;      // number of the warp's first tile of step 0
             int page_base = -16, page_of = -1;              // pages of the warp's tiles of sixteen steps: lane = 2 * (step - page_base) + tile
             const int first = (n ^ stage) & 1;             // our first step of the piece
@@ -658,12 +663,12 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                 __syncwarp();
                 fill(s0 + k + 2 * R, slot);
                 if (++slot == R) slot = 0;
-                const bool all = seen_by_all(g, g.ri.lo + (s0 + k) * kWideUnit);
-                const int t0 = g.ri.lo + (s0 + k) * kWideUnit + w * 32;
+                const int first_token = base + k * kWideUnit, t0 = first_token + w * 32;
+                const bool all = first_token <= until && first_token > after;
                 if (!all || there != 3) {                  // what is absent or masked must not be multiplied with
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
-                        if (!((there >> (x >> 1)) & 1) || (values && t0 + x * 8 + tok >= g.ri.hi)) scales[x] = 0;
+                        if (!((there >> (x >> 1)) & 1) || (values && t0 + x * 8 + tok >= hi_token)) scales[x] = 0;
                         if (values && !all) {
                             if ((scales[x] & 0x7f) == 0x7f) scales[x] &= 0xff00;
                             if ((scales[x] & 0x7f00) == 0x7f00) scales[x] &= 0x00ff;
@@ -718,10 +723,16 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                 }
                 async_proxy_fence();
                 __syncwarp();
-                if (lane == 0) barrier_arrive(full_bar);
+                if (lane == 0) barrier_arrive(!values && i < 2 ? k_first(stage) : full_bar);
             }
             n += count;
         });
+        // the last two steps wait for keys as the others do
+        const uint32_t beyond = n + ((n ^ stage) & 1);
+        if (!values && beyond >= 2) {
+            wait(empty_bar, ((beyond >> 1) - 1) & 1);
+            if (lane == 0) barrier_arrive(full_bar);
+        }
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
         if (warp == 24) {
@@ -731,7 +742,6 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
             const uint64_t k_desc = operand_desc(sm + Plan::kK, 16, 1024), v_desc = operand_desc(sm + Plan::kV, Plan::kChunkBytes, 1024);
             uint32_t n = 0, n_query = 0;                 // steps in earlier pieces
             for_pieces([&](const WideSegment&, int, int count) {
-                auto keys = [&](uint32_t i) { wait(k_full(i & 1), (i >> 1) & 1); };
                 auto scores = [&](uint32_t i) {          // S of step i
                     const int stage = i & 1;
                     const uint64_t k = k_desc + stage * (Plan::kTileBytes >> 4);
@@ -742,16 +752,14 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                 };
                 wait(query_bar, n_query++ & 1);
                 for (int k = 0; k < 2 && k < count; ++k) {
-                    keys(n + k);
+                    if (n + k < 2) wait(k_first(n + k), 0);
                     tc_fence_after();
                     scores(n + k);
                 }
 #pragma unroll 1
                 for (int k = 0; k < count; ++k, ++n) {
                     const int stage = n & 1;
-                    if (k + 2 < count) keys(n + 2);      // long there, as the values are: what is waited for is the weights
-                    wait(v_full(stage), (n >> 1) & 1);
-                    wait(weight_bar(stage), (n >> 1) & 1);
+                    wait(ready_bar(stage), (n >> 1) & 1);
                     tc_fence_after();
                     const uint64_t v = v_desc + stage * (Plan::kTileBytes >> 4);
 #pragma unroll
