@@ -360,6 +360,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                 if (lane == 0) barrier_arrive(query_bar);
             }
             const int pos = mine ? seg.ri.len + qi : -1;
+            const bool idle = !__any_sync(0xffffffffu, mine);
             float m = -INFINITY, l = 0.f;
             uint32_t nan_blocks = 0;
 
@@ -383,8 +384,8 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                 const bool all = t0 <= until && t0 > after;
                 // Weights with the reference at hand, in one pass: a sum of at most kTotalMax means that each of them is within fp16.
                 // Where that fails, and where there are masks, the step is done in two passes, the largest score first.
-                bool done = false;
-                if (all) {                               // that every tile is there is looked at with the sum
+                bool done = idle;                        // a quarter without query rows hands nothing over: its sums are nobody's
+                if (all && !idle) {                      // that every tile is there is looked at with the sum
                     float2 total = make_float2(0.f, 0.f);
                     uint32_t x[2][16], p[2][16];
                     tmem_load16(s_at, x[0]);
@@ -522,6 +523,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                 for (int col = col0; col < col1; col += 32) {
                     float y[32];
                     sums(col, y);
+                    if (!mine) continue;                 // unused rows are not written, nor read below
 #pragma unroll
                     for (int i = 0; i < 32; i += 4)
                         reinterpret_cast<float4*>(out)[((col + i) >> 2) * 128 + row] = make_float4(y[i], y[i + 1], y[i + 2], y[i + 3]);
@@ -539,7 +541,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                     __threadfence();
                 }
                 meet();
-                if (*static_cast<volatile int*>(&last_here)) {
+                if (*static_cast<volatile int*>(&last_here) && mine) {
                     __threadfence();
                     const int parts = c1 - c0 + 1;
                     float m_all = -INFINITY, l_all = 0.f;
@@ -568,7 +570,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                                 y[d + 3] += wt * v.w;
                             }
                         }
-                        if (mine) finish(col, y, m_all, l_all);
+                        finish(col, y, m_all, l_all);
                     }
                 }
                 meet();                // `last_here` is free again
