@@ -521,7 +521,8 @@ typedef struct sam_cache {
 #define SAM_CACHE_OUT_OF_PAGES  1   /* a sam_cache_reserve found too few free pages and reserved none */
 #define SAM_CACHE_TABLE_FULL    2   /* a sam_cache_reserve would have needed more than max_pages pages for a stream, and reserved none */
 #define SAM_CACHE_BAD_FORK      4   /* a sam_cache_fork pair named a destination that holds tokens, or an unknown stream */
-#define SAM_CACHE_GAVE_UP       8   /* a sam_cache_attend gave up on an internal (bounded) wait: its outputs are not valid */
+#define SAM_CACHE_GAVE_UP       8   /* a sam_cache_attend gave up on an internal (bounded) wait: its outputs are not valid, and its workspace
+                                       has to be zero-filled again */
 
 #define SAM_CACHE_BF16  0           /* element types of queries, keys, values and outputs */
 #define SAM_CACHE_FP16  1

@@ -201,7 +201,7 @@ int sam_cache_reserve(const sam_cache* c, int32_t B, const int32_t* streams, con
     reserve_kernel<<<1, kPageThreads, 0, s>>>(v, B, streams, n_new);
     if (int e = launched()) return e;
     const int64_t list = std::max(v.n_streams, v.n_pages);
-    const int32_t* from = v.scratch + kScratchHead + 2ll * v.n_streams;
+    const int32_t* from = v.scratch + kScratchHead + 3ll * v.n_streams;
     copy_pages_kernel<<<grid, kCopyThreads, 0, s>>>(v.pages, v.pages, v.page_bytes, v.n_pages, v.n_pages, v.scratch, 0, from, from + list);
     return launched();
 }
@@ -235,7 +235,7 @@ int sam_cache_compact(const sam_cache* c, void* cuda_stream) {
     compact_plan_kernel<<<1, kPageThreads, 0, s>>>(v);
     if (int e = launched()) return e;
     const int64_t list = std::max(v.n_streams, v.n_pages);
-    const int32_t* from = v.scratch + kScratchHead + 2ll * v.n_streams;
+    const int32_t* from = v.scratch + kScratchHead + 3ll * v.n_streams;
     copy_pages_kernel<<<grid, kCopyThreads, 0, s>>>(v.pages, v.pages, v.page_bytes, v.n_pages, v.n_pages, v.scratch, 0, from, from + list);
     if (int e = launched()) return e;
     compact_tables_kernel<<<512, 256, 0, s>>>(v);

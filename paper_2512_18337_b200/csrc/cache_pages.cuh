@@ -18,13 +18,14 @@ struct PageScratch {
     int32_t* count;     // copies listed
     int32_t* row_a;     // [n_streams]
     int32_t* row_b;     // [n_streams]
+    int32_t* row_c;     // [n_streams]
     int32_t* from;      // [max(n_streams, n_pages)]
     int32_t* to;
     int32_t* remap;     // [n_pages]
 };
 __host__ __device__ inline int64_t page_scratch_ints(int64_t n_streams, int64_t n_pages) {
     const int64_t list = n_streams > n_pages ? n_streams : n_pages;
-    return kScratchHead + 2 * n_streams + 2 * list + n_pages;
+    return kScratchHead + 3 * n_streams + 2 * list + n_pages;
 }
 __device__ __forceinline__ PageScratch page_scratch(const CacheView& c) {
     const int64_t list = max(c.n_streams, c.n_pages);
@@ -32,7 +33,8 @@ __device__ __forceinline__ PageScratch page_scratch(const CacheView& c) {
     s.count = c.scratch;
     s.row_a = c.scratch + kScratchHead;
     s.row_b = s.row_a + c.n_streams;
-    s.from = s.row_b + c.n_streams;
+    s.row_c = s.row_b + c.n_streams;
+    s.from = s.row_c + c.n_streams;
     s.to = s.from + list;
     s.remap = s.to + list;
     return s;
@@ -104,15 +106,18 @@ __device__ __forceinline__ RowNeed row_need(const CacheView& c, const int32_t* s
 }
 
 // One block; a thread looks after up to four rows and keeps them in registers.  What a step costs is the chain of dependent
-// loads (stream, length, table, counts), so each of them is made once.
+// loads (stream, length, table, counts), so each of them is made once.  Rows that need room for many pages (a prompt) are
+// counted and filled by the whole block, one after the other.
 constexpr int kRowsPerThread = 4;   // SAM_CACHE_MAX_B / kPageThreads
+constexpr int kLongSpan = 8;        // pages that a thread looks at by itself
 __global__ void __launch_bounds__(kPageThreads) reserve_kernel(CacheView c, int B, const int32_t* streams, const int32_t* n_new) {
     const PageScratch sc = page_scratch(c);
-    __shared__ int bad, copies;
-    if (threadIdx.x == 0) bad = copies = 0;
+    __shared__ int bad, copies, n_long;
+    if (threadIdx.x == 0) bad = copies = n_long = 0;
     __syncthreads();
     const int n_free = c.meta[0];
     RowNeed r[kRowsPerThread];
+    auto is_long = [](const RowNeed& x) { return x.want - x.first > kLongSpan; };
     int need[kRowsPerThread];
     bool sole[kRowsPerThread], keeper[kRowsPerThread];
     // writers of a page leave it: a count of zero means that all its holders write
@@ -125,9 +130,23 @@ __global__ void __launch_bounds__(kPageThreads) reserve_kernel(CacheView c, int 
         r[u] = row_need(c, streams, n_new, b);
         if (r[u].want > c.max_pages) bad = 1;
         if (r[u].page0 >= 0) atomicSub(&c.ref[r[u].page0], 1);
-        for (int i = r[u].first; i < min(r[u].want, c.max_pages); ++i) need[u] += c.page_at(r[u].s, i) < 0;
+        if (is_long(r[u])) sc.row_a[atomicAdd(&n_long, 1)] = b;   // in any order: each is dealt with by itself
+        else
+            for (int i = r[u].first; i < min(r[u].want, c.max_pages); ++i) need[u] += c.page_at(r[u].s, i) < 0;
     }
     __syncthreads();
+    for (int j = 0; j < n_long; ++j) {
+        const int b = sc.row_a[j];
+        const RowNeed x = row_need(c, streams, n_new, b);
+        int missing = 0;
+        for (int i = x.first + threadIdx.x; i < min(x.want, c.max_pages); i += kPageThreads) missing += c.page_at(x.s, i) < 0;
+        missing = block_sum(missing);
+        if (threadIdx.x == 0) sc.row_b[b] = missing;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kRowsPerThread; ++u)
+        if (is_long(r[u])) need[u] = sc.row_b[u * kPageThreads + threadIdx.x];
 #pragma unroll
     for (int u = 0; u < kRowsPerThread; ++u) sole[u] = r[u].page0 >= 0 && __ldcg(&c.ref[r[u].page0]) == 0;
     __syncthreads();
@@ -168,16 +187,36 @@ __global__ void __launch_bounds__(kPageThreads) reserve_kernel(CacheView c, int 
         if (keeper[u]) c.ref[r[u].page0] = 1;
         const bool copy = r[u].page0 >= 0 && !keeper[u];
         if (need[u] == 0) continue;
-        for (int i = r[u].first; i < r[u].want; ++i) {
-            const bool replace = copy && i == r[u].first;
-            if (!replace && c.page_at(r[u].s, i) >= 0) continue;
-            const int page = c.free_list[at--];
-            if (replace) {
-                const int k = atomicAdd(&copies, 1);   // the order of the copies does not matter
-                sc.from[k] = r[u].page0;
-                sc.to[k] = page;
-            }
+        auto hand_out = [&](int i, int page) {
             c.row(r[u].s)[i] = page;
+            if (static_cast<unsigned>(page) < static_cast<unsigned>(c.n_pages)) c.ref[page] = 1;
+        };
+        if (copy) {
+            const int page = c.free_list[at--], k = atomicAdd(&copies, 1);   // the order of the copies does not matter
+            sc.from[k] = r[u].page0;
+            sc.to[k] = page;
+            hand_out(r[u].first, page);
+        }
+        if (is_long(r[u])) sc.row_c[u * kPageThreads + threadIdx.x] = at;
+        else
+            for (int i = r[u].first; i < r[u].want; ++i)
+                if (c.page_at(r[u].s, i) < 0) hand_out(i, c.free_list[at--]);
+    }
+    __syncthreads();
+    for (int j = 0; j < n_long; ++j) {
+        const int b = sc.row_a[j];
+        const RowNeed x = row_need(c, streams, n_new, b);
+        int at = sc.row_c[b];
+        if (sc.row_b[b] == 0) continue;
+        for (int i0 = x.first; i0 < x.want; i0 += kPageThreads) {
+            const int i = i0 + threadIdx.x;
+            const bool missing = i < x.want && c.page_at(x.s, i) < 0;
+            int total;
+            const int mine_at = at - block_scan(missing, &total);
+            at -= total;
+            if (!missing) continue;
+            const int page = c.free_list[mine_at];
+            c.row(x.s)[i] = page;
             if (static_cast<unsigned>(page) < static_cast<unsigned>(c.n_pages)) c.ref[page] = 1;
         }
     }

@@ -76,6 +76,32 @@ def test_random_walk(P, n_streams, max_pages, n_pages):
     _same(c, book)
 
 
+@pytest.mark.parametrize("P", [16, 64])
+def test_reserving_for_prompts(P):
+    """Rows that need hundreds of pages beside rows that need none or one; holes in a table are filled; shared ends are copied."""
+    c, book, rng = _pair(7000 if P == 16 else 2000, P, 9, 3000, seed=P, layers=1)
+    for step, n in enumerate(([0, 20000, 3, 150, 17 * P, 0, 1, 30001, 8 * P], [40, 5, 0, 2500, 9 * P, 100, 0, 77, 12 * P])):
+        c.reserve(_i32(n))
+        book.reserve(list(enumerate(n)))
+        _same(c, book, content=False)
+        keep = [x if i != 3 else x // 2 for i, x in enumerate(n)]
+        c.commit(_i32(keep))
+        book.commit(list(enumerate(keep)))
+        _same(c, book, content=False)
+        if step == 0:
+            c.fork(_i32([1, 3]), _i32([0, 5]))
+            book.fork([(1, 0), (3, 5)])
+    c.reserve(_i32([20 * P, 20 * P]), streams=_i32([1, 3]))
+    book.reserve([(1, 20 * P), (3, 20 * P)])
+    _same(c, book)
+    # absent pages in the middle of what is reserved
+    c.page_table[1, 1 + int(book.len[1]) // P + 4] = -1
+    book.table[1, 1 + int(book.len[1]) // P + 4] = -1
+    c.reserve(_i32([30 * P, 1]), streams=_i32([1, 8]))
+    book.reserve([(1, 30 * P), (8, 1)])
+    assert (c.page_table.cpu().numpy() == book.table).all()
+
+
 def test_copy_on_write_and_the_last_holder():
     """Three holders of a half-filled page: writers get copies, unless all write: then the last keeps it."""
     c, book, _ = _pair(20, 16, 4, 3)
