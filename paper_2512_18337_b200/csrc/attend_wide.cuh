@@ -2,14 +2,19 @@
 //
 // S = Q K^T and O += P V on a tile of 128 query rows, with 128 tokens a step.  Sixteen warps expand the 4-bit tiles into two stages
 // of fp16 keys and two of fp16 values in shared memory (exact: a value has six significant bits).  Q, two tiles of scores and the
-// sums O lie in tensor memory.  Two threads of the eight softmax warps share a query row, each with
-// half of a step's tokens; they write P as fp16 over S, from where the second product takes it.  While they work on one step's
-// scores, the products of the step before and of the step after run.  (One warp per scheduler, with whole rows, took 2,470 clocks
-// a step: it waits for itself most of the time.)
+// sums O lie in tensor memory.  Two threads of the eight softmax warps share a query row, each with half of a step's tokens; they
+// write P as fp16 over S, from where the second product takes it.  While they work on one step's scores, the products of the step
+// before and of the step after run.
 //
-// Q is read from tensor memory, not from shared memory, because a 128 x 128 product with both operands in shared memory takes all of
-// its bandwidth: the expanding warps and every barrier then stand still (a store gets through at a tenth of its rate, a load at a
-// thirtieth).  With one operand there the products take half of it.
+// Q is read from tensor memory, not from shared memory: a 128 x 128 product with both operands in shared memory takes all of its
+// bandwidth, and beside it a warp gets half the stores and a tenth of the loads through (barriers are loads) that it gets beside
+// products with one operand there.
+//
+// What it measured: a step takes 2,370 to 2,450 clocks (2,048 query tokens over 20,011 positions, 28/4 heads of 128: 715 us,
+// 865 TFLOP/s), of which the products are 1,024 and the exponentials 1,024.  It is bound by the chain scores - exponentials -
+// weights - products, of which two are in flight: no pipe is full.  Tried and slower: two row tiles a CTA with the expanded operands
+// shared and Q in shared memory (2,450 clocks for a tile's step, but only with more than 128 query rows); one softmax warp per
+// scheduler with whole rows (2,640); the scores in two halves; three waits a step for the issuing warp instead of one (2,520).
 //
 // Keys and values have the same layout in shared memory, [token][64 channels] in 128-byte rows with the 128-byte swizzle: for
 // the first product it is read with the channels (the summed index) innermost, for the second with the channels as the N side.
@@ -30,7 +35,7 @@ constexpr int kWideUnit = 128;                     // tokens of a step
 constexpr int kWideRows = 128;                     // query rows of a segment
 constexpr int kWideWarps = 28, kWideThreads = kWideWarps * 32;   // eight softmax warps, sixteen expanding ones, an issuing one (and three that idle)
 constexpr int kWideMaxCtas = 160;
-constexpr float kWideAbove = 8.f, kTotalMax = 32768.f;   // 128 weights of 2^8 add up to no more
+constexpr float kWideAbove = 8.f, kTotalMax = 32768.f;   // 64 weights of 2^8 add up to less
 // columns of tensor memory
 constexpr uint32_t kColQ = 0, kColS = 64, kColO = 320;
 
