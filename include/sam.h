@@ -529,8 +529,8 @@ typedef struct sam_cache {
 
 #define SAM_CACHE_MAX_B 4096        /* rows of one call */
 
-/* Sizes.  page_tokens: a power of two, 16 .. 1024; head_dim: 64 or 128; page_tokens * max_pages < 2^31.
- * Negative SAM_ERR_* on bad sizes. */
+/* Sizes.  page_tokens: a power of two, 16 .. 1024; head_dim: 64 or 128; page_tokens * max_pages <= 2^30;
+ * n_streams * max_pages <= 2^30; up to 2^30 query rows a stream.  Negative SAM_ERR_* on bad sizes. */
 int64_t sam_cache_page_bytes(int32_t page_tokens, int32_t n_layers, int32_t n_kv_heads, int32_t head_dim);
 int64_t sam_cache_scratch_bytes(int32_t n_streams, int32_t n_pages);
 

@@ -22,10 +22,14 @@ bool geometry_ok(int32_t page_tokens, int32_t n_layers, int32_t n_kv_heads, int3
            n_kv_heads >= 1 && n_kv_heads <= 1024 && (head_dim == 64 || head_dim == 128);
 }
 
+constexpr int64_t kLargest = int64_t(1) << 30;   // positions of a stream, entries of the table, query rows of a stream
+
 int check_cache(const sam_cache* c) {
     if (!c || !geometry_ok(c->page_tokens, c->n_layers, c->n_kv_heads, c->head_dim)) return SAM_ERR_INVALID_ARG;
     if (c->n_pages < 1 || c->n_streams < 1 || c->max_pages < 1) return SAM_ERR_INVALID_ARG;
-    if (static_cast<int64_t>(c->max_pages) * c->page_tokens >= (int64_t(1) << 31)) return SAM_ERR_INVALID_ARG;
+    // positions of new tokens, sums of pages over rows and their tags are 32-bit numbers in the kernels
+    if (static_cast<int64_t>(c->max_pages) * c->page_tokens > kLargest || static_cast<int64_t>(c->max_pages) * c->n_streams > kLargest)
+        return SAM_ERR_INVALID_ARG;
     if (c->k_exp < -24 || c->k_exp > 24 || c->v_exp < -24 || c->v_exp > 24) return SAM_ERR_INVALID_ARG;
     if (!c->page_table || !c->seq_len) return SAM_ERR_INVALID_ARG;
     return SAM_OK;
@@ -311,7 +315,7 @@ int sam_cache_attend(const sam_cache* c, int32_t layer, const void* q, int32_t d
     if (!q || !out || !aligned(q, 2) || !aligned(out, 2) || !aligned(lse, 4) || !workspace || !aligned(workspace, 256) || (!streams && B > c->n_streams))
         return SAM_ERR_INVALID_ARG;
     if (workspace_bytes < need) return SAM_ERR_TOO_SMALL;
-    if (static_cast<int64_t>(B) * Q * H >= (int64_t(1) << 31)) return SAM_ERR_TOO_LARGE;
+    if (Q > kLargest || static_cast<int64_t>(B) * Q * H >= (int64_t(1) << 31)) return SAM_ERR_TOO_LARGE;
     AttendArgs a;
     a.c = view(c);
     a.q = q;

@@ -349,7 +349,8 @@ __global__ void __launch_bounds__(kPageThreads) commit_kernel(CacheView c, int B
 #pragma unroll 4
     for (int e = threadIdx.x; e < all; e += kPageThreads) {
         int32_t* at = entry(e);
-        if (__ldcg(&c.ref[*at]) < 0) c.ref[*at] = 0;
+        const int page = *at;
+        if (page >= 0 && __ldcg(&c.ref[page]) < 0) c.ref[page] = 0;
         *at = -1;
     }
     if (threadIdx.x == 0) c.meta[0] = min(n_free + pushed, c.n_pages);

@@ -33,7 +33,8 @@ def test_sizes():
 
 
 BAD_CACHES = [dict(page_tokens=48), dict(head_dim=80), dict(n_pages=0), dict(n_streams=0), dict(max_pages=0),
-              dict(max_pages=1 << 27), dict(k_exp=25), dict(v_exp=-25), dict(page_table=0), dict(seq_len=0), dict(n_layers=0)]
+              dict(max_pages=1 << 27), dict(max_pages=(1 << 26) + 1), dict(n_streams=1 << 20, max_pages=(1 << 10) + 1),
+              dict(k_exp=25), dict(v_exp=-25), dict(page_table=0), dict(seq_len=0), dict(n_layers=0)]
 
 
 @pytest.mark.parametrize("over", BAD_CACHES, ids=str)
@@ -98,8 +99,11 @@ def test_bad_arguments_are_refused():
     for over in (dict(layer=2), dict(q=None), dict(q=17), dict(dtype=5), dict(B=-1), dict(Q=-1), dict(H=3), dict(H=0), dict(window=-1),
                  dict(out=None), dict(lse=2), dict(ws=None), dict(ws=128), dict(B=5)):
         assert attend(**over) == -1, over
+    assert attend(Q=1 << 30, ws_bytes=1 << 40) == -6
+    one = C.addressof(w := _struct(n_kv_heads=1))
+    assert lib.sam_cache_attend(one, 0, 16, 0, 0, 0, 0, 1, (1 << 30) + 1, 1, None, None, 1.0, 0, 16, 0, 0, 0, None, 256, 1 << 40, None) == -6
     assert attend(ws_bytes=need - 1) == -5 and attend(B=0) == 0 and attend(Q=0) == 0
-    del s, u
+    del s, u, w
 
 
 def test_reference_rounds_to_the_nearest_value():
