@@ -689,7 +689,7 @@ class SamCache:
     def append(self, layer: int, k, v, n_new=None, streams=None, stream=None) -> None:
         pk, st = self._rows(k, self.n_kv_heads)
         pv, sv = self._rows(v, self.n_kv_heads)
-        if st != sv or k.shape != v.shape or k.dtype != v.dtype:
+        if k.shape != v.shape or k.dtype != v.dtype or (st != sv and any(x != y and n > 1 for x, y, n in zip(st, sv, k.shape))):
             raise ValueError("keys and values of one shape, type and layout are wanted")
         B, Q = k.shape[:2]
         sam_cache_append(self.handle, layer, pk, pv, self._dtype(k.dtype), *st, B, Q, self._index(streams, B),

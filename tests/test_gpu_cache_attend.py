@@ -299,6 +299,20 @@ def test_append_unaligned_and_named_streams():
         assert (left[page] == raw[page]).all()
 
 
+def test_append_ignores_strides_of_single_rows():
+    """Keys and values of one row and one token whose layouts differ only where there is nothing to step over."""
+    c = S.SamCache(2, 16, 1, 2, 1, 2, 64, device=DEV)
+    k = torch.randn(1, 1, 2, 64, device=DEV).to(torch.bfloat16)
+    v = torch.randn(4, 3, 2, 64, device=DEV).to(torch.bfloat16)[2:3, 1:2]
+    assert k.stride() != v.stride()
+    c.reserve(_i32([1]))
+    c.append(0, k, v)
+    for y, x in zip(c.read(0, max_n=1), (k, v)):
+        assert (y.double().cpu().numpy() == R.values(*R.quantise(x.double().cpu().numpy(), 0), 0)).all()
+    with pytest.raises(ValueError):
+        c.append(0, k.expand(2, 2, 2, 64), torch.zeros(2, 2, 2, 64, dtype=torch.bfloat16, device=DEV))
+
+
 def test_long_offsets():
     """A pool beyond 4 GB: bytes past 2^32 are reached, read and attended to."""
     P, Hkv, D, L = 1024, 8, 128, 4
