@@ -388,9 +388,9 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                 on = (on * 0x01041040u) >> 24;            // two bits of each byte, side by side
                 const bool all = t0 <= until && t0 > after;
                 // Weights with the reference at hand, in one pass: a sum of at most kTotalMax means that each of them is within fp16.
-                // Where that fails, and where there are masks, the step is done in two passes, the largest score first.
+                // Where that fails, and where there are masks or absent tiles, the step is done in two passes, the largest score first.
                 bool done = idle;                        // a quarter without query rows hands nothing over: its sums are nobody's
-                if (all && !idle) {                      // that every tile is there is looked at with the sum
+                if (all && on == 0xff && !idle) {        // absent tiles read as scores of zero, which must not make a reference
                     float2 total = make_float2(0.f, 0.f);
                     uint32_t x[2][16], p[2][16];
                     tmem_load16(s_at, x[0]);
@@ -418,7 +418,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                         }
                     }
                     const float sum = total.x + total.y;
-                    done = !any_of_pair(sum > kTotalMax || on != 0xff);
+                    done = !any_of_pair(sum > kTotalMax);
                     if (done) {
                         l += sum;
                         tmem_store16(s_at, p[0]);
