@@ -623,8 +623,10 @@ class SamCache:
                                     n_pages, page_tokens, n_streams, max_pages, n_layers, n_kv_heads, head_dim, k_exp,
                                     v_exp)
         self.handle = C.addressof(self._struct)
-        self._ws = None
-        self._ws_need = {}      # workspace bytes by (B, Q, H)
+        # Of attend, for calls that bring none: enough for few and for many query rows, so that it is never replaced.
+        # Recorded graphs keep its address, and other streams may still use it.
+        self._ws = self._empty(max(sam_cache_attend_workspace_bytes(self.handle, SAM_CACHE_MAX_B, q, n_kv_heads)
+                                   for q in (1, 1 << 20)), torch.uint8, device, stream, zero=True)
         self._codes = {torch.bfloat16: SAM_CACHE_BF16, torch.float16: SAM_CACHE_FP16}
         if not any(n in given for n in self.BOOKS):
             sam_cache_init(self.handle, stream)
@@ -712,8 +714,8 @@ class SamCache:
 
     def attend(self, layer: int, q, n_new=None, streams=None, scale: Optional[float] = None, window: int = 0, out=None,
                lse=None, workspace=None, stream=None):
-        """(out, lse).  Without a workspace the cache keeps one, grown when a call needs more: calls that may overlap
-        on the device (several streams) bring their own, zero-filled by sam_workspace_init."""
+        """(out, lse).  Without a workspace the call uses the cache's, which lives as long as the cache: calls that may
+        overlap on the device (several streams) bring their own, zero-filled by sam_workspace_init."""
         import torch
         pq, sq = self._rows(q, None)
         B, Q, H = q.shape[:3]
@@ -726,13 +728,8 @@ class SamCache:
         elif tuple(lse.shape) != (B, Q, H) or lse.dtype != torch.float32:
             raise ValueError("a float32 lse [B, Q, H] is wanted")
         po, so = self._rows(out, H)
-        need = self._ws_need.get((B, Q, H))
-        if need is None:
-            need = self._ws_need[B, Q, H] = sam_cache_attend_workspace_bytes(self.handle, B, Q, H)
         if workspace is None:
             workspace = self._ws
-            if workspace is None or workspace.numel() < need:
-                workspace = self._ws = self._empty(need, torch.uint8, q.device, stream, zero=True)
         sam_cache_attend(self.handle, layer, pq, self._dtype(q.dtype), sq, B, Q, H, self._index(streams, B),
                          self._index(n_new, B), self.head_dim ** -0.5 if scale is None else scale, window, po, so, lse,
                          workspace, workspace.numel() * workspace.element_size(), stream)
