@@ -590,8 +590,8 @@ def sam_cache_attend(handle, layer, q, dtype, q_strides, B, Q, H, streams, n_new
 class SamCache:
     """A paged 4-bit key/value cache: owns (or is given) the torch tensors behind a `sam_cache` and marshals its calls.
 
-    tensors: any of pages, page_table, seq_len, ref_count, free_list, meta that exist already; what is missing is
-    allocated.  The cache is emptied on construction when none of its books are given.  `handle` serves the
+    tensors: pages, and the books page_table, seq_len, ref_count, free_list, meta, if they exist already.  The books are
+    given all together or not at all; then they are allocated, and the cache is emptied.  `handle` serves the
     `sam_cache_*` functions directly; the methods below take strided tensors [B, Q, heads, head_dim]."""
 
     BOOKS = ("page_table", "seq_len", "ref_count", "free_list", "meta")
@@ -602,7 +602,10 @@ class SamCache:
         self.page_bytes = sam_cache_page_bytes(page_tokens, n_layers, n_kv_heads, head_dim)
         shapes = dict(page_table=(n_streams, max_pages), seq_len=(n_streams,), ref_count=(n_pages,),
                       free_list=(n_pages,), meta=(4,))
-        given = dict(tensors or {})
+        given = {n: t for n, t in (tensors or {}).items() if t is not None}
+        books = given.keys() - {"pages"}
+        if books and books != set(self.BOOKS):
+            raise ValueError("tensors: the books " + ", ".join(self.BOOKS) + " are given all together or not at all")
         self.pages = given.get("pages")
         if self.pages is None:
             self.pages = torch.empty(n_pages, n_layers, n_kv_heads, page_tokens // 16, 18 * head_dim, dtype=torch.uint8,
@@ -628,7 +631,7 @@ class SamCache:
         self._ws = self._empty(max(sam_cache_attend_workspace_bytes(self.handle, SAM_CACHE_MAX_B, q, n_kv_heads)
                                    for q in (1, 1 << 20)), torch.uint8, device, stream, zero=True)
         self._codes = {torch.bfloat16: SAM_CACHE_BF16, torch.float16: SAM_CACHE_FP16}
-        if not any(n in given for n in self.BOOKS):
+        if not books:
             sam_cache_init(self.handle, stream)
 
     @staticmethod

@@ -47,3 +47,36 @@ def test_a_workspace_of_the_callers_is_used(calls):
     mine = torch.zeros(77, dtype=torch.int32)
     c.attend(0, torch.zeros(1, 1, 2, 128, dtype=torch.bfloat16), workspace=mine)
     assert calls[-1][-3] is mine and calls[-1][-2] == 308
+
+
+def _books():
+    return dict(page_table=torch.full((4, 4), -1, dtype=torch.int32), **{
+        n: torch.zeros(size, dtype=torch.int32) for n, size in (("seq_len", 4), ("ref_count", 8), ("free_list", 8), ("meta", 4))})
+
+
+@pytest.mark.parametrize("without", S.SamCache.BOOKS)
+def test_books_given_in_part_are_refused(calls, without):
+    """What is not given would be neither initialised nor in line with what is."""
+    for names in ({without}, set(_books()) - {without}):
+        with pytest.raises(ValueError, match="all together"):
+            _cache(tensors={n: t for n, t in _books().items() if n in names})
+    assert not calls
+
+
+def test_unknown_tensors_are_refused(calls):
+    with pytest.raises(ValueError, match="all together"):
+        _cache(tensors=dict(_books(), pages_table=torch.zeros(4, 4, dtype=torch.int32)))
+    with pytest.raises(ValueError, match="all together"):
+        _cache(tensors=dict(seq_lens=torch.zeros(4, dtype=torch.int32)))
+
+
+def test_books_given_are_kept_and_others_made(calls):
+    given = _books()
+    c = _cache(tensors=given)
+    assert not calls and all(getattr(c, n) is t for n, t in given.items())
+    pages = torch.zeros(8 * c.page_bytes, dtype=torch.uint8)
+    for tensors in (None, {}, dict(pages=pages), dict(pages=pages, seq_len=None)):
+        del calls[:]
+        c = _cache(tensors=tensors)
+        assert [x[0] for x in calls] == ["sam_cache_init"]
+    assert c.pages is pages
