@@ -552,7 +552,8 @@ int sam_cache_status(const sam_cache* c, int32_t* n_free, int32_t* status, void*
 int sam_cache_reserve(const sam_cache* c, int32_t B, const int32_t* streams, const int32_t* n_new, void* cuda_stream);
 
 /* Commit: seq_len += n_keep[b], which may be negative (roll back; -2^31 empties the stream), clamped to
- * 0 .. page_tokens * max_pages.  The pages behind the new length, up to the table's first -1, are given up; those that
+ * 0 .. page_tokens * max_pages.  The pages behind the new length are given up: whatever the table holds up to the old
+ * length (absent pages among it are passed over), and behind the old length what it holds up to the first -1.  Those that
  * nobody holds any more go onto the free list, in order of rows, then of positions (of their first mention). */
 int sam_cache_commit(const sam_cache* c, int32_t B, const int32_t* streams, const int32_t* n_keep, void* cuda_stream);
 

@@ -254,10 +254,14 @@ __global__ void __launch_bounds__(kCopyThreads) copy_pages_kernel(const uint8_t*
     }
 }
 
-// One block.  The pages that rows give up are numbered in order of rows, then of positions; a page whose count reaches zero is
-// pushed by its lowest number, which an atomic minimum in the count itself finds.  First a thread per row moves the lengths on
-// and looks whether there is anything behind them: mostly there is not, and the call ends after one chain of loads.  Otherwise
-// the given-up pages are worked on one per thread, found by a binary search among the rows' first numbers.
+// One block.  The table entries that rows give up are numbered in order of rows, then of positions; a page whose count reaches
+// zero is pushed by its lowest number, which an atomic minimum in the count itself finds.  First a thread per row moves the
+// lengths on and looks whether there is anything behind them: mostly there is not, and the call ends after one chain of loads.
+// Otherwise the given-up entries are worked on one per thread, found by a binary search among the rows' first numbers.
+//
+// Between the new and the old length any entry may be absent (positions committed after a refused reserve, pages that the caller
+// evicted), so all of them are given up.  What lies behind the old length was reserved from there on without a gap, so its end is
+// the first absent entry, and the rest of the table is not read.
 __global__ void __launch_bounds__(kPageThreads) commit_kernel(CacheView c, int B, const int32_t* streams, const int32_t* n_keep) {
     const PageScratch sc = page_scratch(c);
     extern __shared__ int begin[];          // [rows that give up pages + 1]
@@ -267,12 +271,14 @@ __global__ void __launch_bounds__(kPageThreads) commit_kernel(CacheView c, int B
     for (int b0 = 0; b0 < B; b0 += kPageThreads) {
         const int b = b0 + threadIdx.x;
         const int s = b < B ? c.stream_of(streams, b) : -1;
-        int keep = c.max_pages;
+        int keep = c.max_pages, held = 0;
         bool gives = false;
         if (s >= 0) {
-            const int64_t len = min(max(static_cast<int64_t>(c.length_of(s)) + n_keep[b], int64_t(0)), static_cast<int64_t>(c.capacity()));
+            const int old = c.length_of(s);
+            const int64_t len = min(max(static_cast<int64_t>(old) + n_keep[b], int64_t(0)), static_cast<int64_t>(c.capacity()));
             keep = static_cast<int>((len + c.page_tokens() - 1) >> c.log_p);
-            gives = keep < c.max_pages && c.page_at(s, keep) >= 0;
+            held = (old + c.page_tokens() - 1) >> c.log_p;
+            gives = keep < held || (keep < c.max_pages && c.page_at(s, keep) >= 0);
             c.seq_len[s] = static_cast<int>(len);
         }
         if (!__syncthreads_or(gives)) continue;
@@ -281,16 +287,17 @@ __global__ void __launch_bounds__(kPageThreads) commit_kernel(CacheView c, int B
         if (gives) {
             sc.row_a[at] = s;
             sc.row_b[at] = keep;
+            sc.row_c[at] = max(keep, held);
         }
         rows += total;
     }
     if (rows == 0) return;
     __syncthreads();
-    // how many: up to the table's first -1
+    // how many: up to the old length, and behind it up to the first absent entry
     for (int k = warp; k < rows; k += kPageThreads / 32) {
-        const int s = sc.row_a[k], keep = sc.row_b[k];
-        int gone = 0;
-        for (int i0 = keep; i0 < c.max_pages; i0 += 128) {
+        const int s = sc.row_a[k], held = sc.row_c[k];
+        int gone = held - sc.row_b[k];
+        for (int i0 = held; i0 < c.max_pages; i0 += 128) {
             unsigned none[4];
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
@@ -317,7 +324,7 @@ __global__ void __launch_bounds__(kPageThreads) commit_kernel(CacheView c, int B
     }
     if (threadIdx.x == 0) begin[rows] = all;
     __syncthreads();
-    auto entry = [&](int e) -> int32_t* {   // table entry of given-up page e
+    auto entry = [&](int e) -> int32_t* {   // given-up table entry e
         int lo = 0, hi = rows - 1;
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
@@ -326,19 +333,26 @@ __global__ void __launch_bounds__(kPageThreads) commit_kernel(CacheView c, int B
         }
         return c.row(sc.row_a[lo]) + sc.row_b[lo] + (e - begin[lo]);
     };
+    auto page_of = [&](const int32_t* at) -> int {   // -1: absent
+        const int page = *at;
+        return static_cast<unsigned>(page) < static_cast<unsigned>(c.n_pages) ? page : -1;
+    };
 #pragma unroll 4
-    for (int e = threadIdx.x; e < all; e += kPageThreads) atomicSub(&c.ref[*entry(e)], 1);
+    for (int e = threadIdx.x; e < all; e += kPageThreads) {
+        const int page = page_of(entry(e));
+        if (page >= 0) atomicSub(&c.ref[page], 1);
+    }
     __syncthreads();
 #pragma unroll 4
     for (int e = threadIdx.x; e < all; e += kPageThreads) {
-        int32_t* count = &c.ref[*entry(e)];
-        if (__ldcg(count) <= 0) atomicMin(count, e - kClaim);
+        const int page = page_of(entry(e));
+        if (page >= 0 && __ldcg(&c.ref[page]) <= 0) atomicMin(&c.ref[page], e - kClaim);
     }
     __syncthreads();
     int pushed = 0;
     for (int e0 = 0; e0 < all; e0 += kPageThreads) {
         const int e = e0 + threadIdx.x;
-        const int page = e < all ? *entry(e) : -1;
+        const int page = e < all ? page_of(entry(e)) : -1;
         const bool mine = page >= 0 && __ldcg(&c.ref[page]) == e - kClaim;
         int total;
         const int at = n_free + pushed + block_scan(mine, &total);
@@ -349,7 +363,7 @@ __global__ void __launch_bounds__(kPageThreads) commit_kernel(CacheView c, int B
 #pragma unroll 4
     for (int e = threadIdx.x; e < all; e += kPageThreads) {
         int32_t* at = entry(e);
-        const int page = *at;
+        const int page = page_of(at);
         if (page >= 0 && __ldcg(&c.ref[page]) < 0) c.ref[page] = 0;
         *at = -1;
     }
