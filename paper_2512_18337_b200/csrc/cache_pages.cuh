@@ -374,12 +374,16 @@ __global__ void __launch_bounds__(kPageThreads) commit_kernel(CacheView c, int B
 __global__ void __launch_bounds__(256) fork_kernel(CacheView c, const int32_t* src, const int32_t* dst) {
     const int a = src[blockIdx.x], z = dst[blockIdx.x];
     const bool known = static_cast<unsigned>(a) < static_cast<unsigned>(c.n_streams) && static_cast<unsigned>(z) < static_cast<unsigned>(c.n_streams);
-    if (!known || a == z || c.seq_len[z] != 0 || c.row(z)[0] != -1) {
+    bool taken = !known || a == z || c.seq_len[z] != 0;
+    if (!taken) {   // a page anywhere in the row would be lost
+#pragma unroll 4
+        for (int i = threadIdx.x; i < c.max_pages; i += blockDim.x) taken |= c.row(z)[i] != -1;
+    }
+    const int len = known ? c.length_of(a) : 0, held = (len + c.page_tokens() - 1) >> c.log_p;
+    if (__syncthreads_or(taken)) {
         if (threadIdx.x == 0) atomicOr(&c.meta[1], kStatusBadFork);
         return;
     }
-    const int len = c.length_of(a), held = (len + c.page_tokens() - 1) >> c.log_p;
-    __syncthreads();
     for (int i = threadIdx.x; i < held; i += blockDim.x) {
         const int page = c.page_at(a, i);
         c.row(z)[i] = page;

@@ -95,6 +95,22 @@ def test_evicted_pages_do_not_hide_the_others():
     assert c.status()[0] == 100
 
 
+@pytest.mark.parametrize("max_pages,at", [(3, 1), (3, 2), (700, 256), (700, 699)])
+def test_fork_refuses_a_row_with_a_page_anywhere(max_pages, at):
+    """No tokens and no first page, but a page further on (the caller's table): it would be lost."""
+    c, book, _ = _books(12, 16, 3, max_pages, seed=2)
+    _both(c, book, "reserve", [(0, 20)])
+    _both(c, book, "commit", [(0, 20)])
+    page, n_free = book.free.pop(), int(c.meta[0])
+    c.page_table[1, at], c.ref_count[page], c.meta[0] = page, 1, n_free - 1
+    book.table[1, at], book.ref[page] = page, 1
+    c.fork(_i32([0, 0]), _i32([1, 2]))
+    book.fork([(0, 2)])
+    book.status = S.SAM_CACHE_BAD_FORK
+    _same(c, book)
+    _whole(c)
+
+
 @pytest.mark.parametrize("P,n_streams,max_pages,n_pages", [(16, 5, 9, 24), (32, 40, 6, 120), (16, 33, 90, 700), (64, 1100, 5, 2500), (16, 3, 700, 900)])
 def test_random_walk_with_gaps(P, n_streams, max_pages, n_pages):
     """Commits by any number of tokens, whatever was reserved before them, or refused."""
