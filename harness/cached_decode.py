@@ -73,6 +73,7 @@ class CachedDecoder:
         one = torch.tensor([stream], dtype=torch.int32, device=t.device)
         n = torch.tensor([t.shape[1]], dtype=torch.int32, device=t.device)
         self.cache.reserve(n, streams=one)
+        self.check()
         self.model.forward(self.cache, t, n, streams=one)
         self.cache.commit(n, streams=one)
         self.pending[stream] = int(tokens[-1])
@@ -80,6 +81,13 @@ class CachedDecoder:
             self.feed(torch.nn.functional.pad(torch.from_numpy(np.ascontiguousarray(tokens, dtype=np.int32))[None],
                                               (0, 0, stream, self.B - 1 - stream)).to(t.device),
                       torch.nn.functional.pad(n + 1, (stream, self.B - 1 - stream)))
+
+    def check(self):
+        """A refused call shows in the cache's status only; what is computed after it does not stand."""
+        n_free, status = self.cache.status()
+        if status:
+            names = [n for n in ("OUT_OF_PAGES", "TABLE_FULL", "BAD_FORK", "GAVE_UP") if status & getattr(S, "SAM_CACHE_" + n)]
+            raise RuntimeError(f"the cache refused a call: {', '.join(names)} ({n_free} free pages)")
 
     def feed(self, tokens, n):
         S.sam_draft(self.index.handle, self.B, self.state, self.mlen, tokens.contiguous(), tokens.shape[1], n, self.K,
@@ -93,7 +101,8 @@ class CachedDecoder:
             t[d.long()] = t[src].clone()
 
     def step(self):
-        """One verification step of all streams; returns (tokens [B, K+1], counts [B]) on the device."""
+        """One verification step of all streams; returns (tokens [B, K+1], counts [B]) on the device.  They stand if check()
+        finds nothing."""
         rows = torch.cat([self.pending[:, None], self.drafts], 1)
         n_new = self.n_draft + 1
         self.cache.reserve(n_new)
@@ -115,6 +124,7 @@ class CachedDecoder:
         out = [[] for _ in range(self.B)]
         for _ in range(steps):
             t, n = (x.cpu().numpy() for x in self.step())
+            self.check()
             for b in range(self.B):
                 out[b] += t[b, :n[b]].tolist()
         return out
