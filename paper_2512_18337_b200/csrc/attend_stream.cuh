@@ -175,6 +175,7 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
     __shared__ RowInfo row_found[kStreamWarps];
     __shared__ StreamPiece pieces[kStreamWarps][2];
     __shared__ int last_here;
+    __shared__ bool gave_up[kStreamWarps];
 
     const CacheView& c = a.c;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -211,6 +212,7 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
     };
     if (tid < kStreamWarps * kStages) barrier_init(shared_addr(&bars[0][0]) + tid * 8, 1);
     if (tid < kStreamWarps * 2) pieces[tid >> 1][tid & 1].used = 0;
+    if (tid < kStreamWarps) gave_up[tid] = false;
     barrier_init_fence();
     int64_t units = 0, mine = 0, before = 0, unused;
     for (int b0 = 0; b0 < a.B; b0 += kStreamThreads) {
@@ -254,7 +256,7 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
     const uint32_t ring = shared_addr(own), bar0 = shared_addr(&bars[warp][0]);
     const int64_t u0 = cta_begin + warp_shares.begin(warp), u1 = cta_begin + warp_shares.begin(warp + 1);
     int64_t left = u1 - u0, to_load = left;
-    bool gave_up = false;
+    const RingWaits waits{&gave_up[warp]};
 
     // ---- the filling side of the ring: lane l knows where the tiles of step page_step + l are, and issues their copies
     StreamCursor in{}, cur{};
@@ -376,7 +378,13 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
 
         for (int k = 0; k < count; ++k) {
             const int stage = it % kStages;
-            if (!barrier_wait(bar0 + stage * 8, (it / kStages) & 1)) gave_up = true;
+            const bool late = !waits.unit([&] { return barrier_try(bar0 + stage * 8, (it / kStages) & 1); });
+            // (kept for the vote further down instead: two streams of 250,001 positions 142.7 -> 144.0 us, registers spilled)
+            if (__any_sync(0xffffffffu, late)) {
+                waits.give_up(static_cast<int>(min(left - k - to_load, static_cast<int64_t>(kStages))),
+                              [&](int i) { return barrier_try(bar0 + (it + i) % kStages * 8, ((it + i) / kStages) & 1); });
+                to_load = 0;
+            }
             const int t0 = cur.ri.lo + (s0 + k) * kStreamUnit;
             const uint32_t unit = ring + stage * Plan::kUnitBytes;
             const uint32_t here = (present >> (2 * stage)) & 3;
@@ -612,7 +620,7 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
         cur.step += count;
         if (left) cur.next_segment<kRows>(a);
     }
-    if (gave_up && c.meta && lane == 0) atomicOr(&c.meta[1], kStatusGaveUp);
+    if (gave_up[warp] && c.meta && lane == 0) atomicOr(&c.meta[1], kStatusGaveUp);
     if (!busy) return;
     __syncthreads();
 

@@ -3,9 +3,9 @@
 
 #include <cstdint>
 
-namespace samb200 {
+#include "bounded_wait.h"
 
-constexpr uint32_t kCachePolls = 1u << 20;
+namespace samb200 {
 
 __device__ __forceinline__ uint32_t shared_addr(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
 
@@ -24,12 +24,6 @@ __device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity) {
     asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                  : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
-}
-// False when the phase did not complete in time.
-__device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity) {
-    for (uint32_t i = 0; i < kCachePolls; ++i)
-        if (barrier_try(bar, parity)) return true;
-    return false;
 }
 
 // global -> shared, both 16-byte aligned, bytes a multiple of 16; completion is counted on bar.
