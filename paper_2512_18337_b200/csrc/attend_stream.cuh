@@ -533,6 +533,7 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
                                             for (int mt = 0; mt < MT; ++mt) o[mt][nt][x] = o[mt][nt][x + 2] = __int_as_float(0x7fffffff);
                             }
                         }
+                        __syncwarp();                        // the products below want the warp together
                     }
                 }
                 const uint32_t f0 = e4m3x2_to_half2(b0 | b1 << 8), f1 = e4m3x2_to_half2(b2 | b3 << 8);

@@ -189,6 +189,12 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
         }
         abort_flag = 1;
     };
+    // For whole warps.  Lanes leave a wait, and a branch of their own, one by one; what follows in tensor memory and at the hardware
+    // barriers wants the warp together, so it is brought together there, here and below.
+    auto wait_warp = [&](uint32_t b, uint32_t parity) {
+        wait(b, parity);
+        __syncwarp();
+    };
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
             barrier_init(score_bar(i), 1);
@@ -254,6 +260,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
     }
     clear_unused_rows<T, D>(a, cta, gridDim.x);
     if (!busy) return;
+    __syncwarp();
     if (warp == 24) tmem_alloc(shared_addr(&tmem_base), 512);
     tc_fence_before();
     __syncthreads();
@@ -314,7 +321,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
         // Product n complete.  Asked for when the scores of step n + 1 are there, or none are to come: the product before n has been
         // complete since, so that the parity of n's barrier tells.
         auto product = [&](uint32_t i) {
-            wait(product_bar(i & 1), (i >> 1) & 1);
+            wait_warp(product_bar(i & 1), (i >> 1) & 1);
             tc_fence_after();
         };
         for_pieces([&](const WideSegment& seg, int s0, int count) {
@@ -339,6 +346,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                 };
 #pragma unroll
                 for (int d = 0; d < kHalf; d += 8) load8(part_no * kHalf + d, reinterpret_cast<uint32_t(&)[4]>(x[d / 2]));
+                __syncwarp();
                 int e = 0;
                 if constexpr (!std::is_same<T, __half>::value) {
                     auto lo = [](uint32_t w) { return __uint_as_float(w << 16); };
@@ -363,6 +371,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) barrier_arrive(query_bar);
+                __syncwarp();
             }
             const int pos = mine ? seg.ri.len + qi : -1;
             const bool idle = !__any_sync(0xffffffffu, mine);
@@ -376,11 +385,12 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) barrier_arrive(ready_bar(i & 1));
+                __syncwarp();
             };
 #pragma unroll 1
             for (int k = 0; k < count; ++k, ++n) {
                 const uint32_t s_at = lanes + kColS + (n & 1) * 128 + part_no * 64;
-                wait(score_bar(n & 1), (n >> 1) & 1);
+                wait_warp(score_bar(n & 1), (n >> 1) & 1);
                 if (k > 0) hand_over(n - 1);             // the weights of the step before are stored by now
                 tc_fence_after();
                 const int t0 = base + k * kWideUnit, ring = n & 3;
@@ -430,6 +440,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                         for (int t = 0; t < kWideUnit; ++t)
                             if (static_cast<volatile uint8_t*>(nan_flag[ring])[t >> 5] && t0 + t <= pos && (a.window == 0 || t0 + t > pos - a.window))
                                 nan_blocks |= static_cast<volatile uint8_t*>(nan_block[ring])[t];
+                        __syncwarp();
                     }
                     // which of 32 columns a row sees, as bits; q: 0 .. 3 over the step
                     const int from = a.window > 0 ? max(pos - a.window + 1 - t0, 0) : 0, to_col = min(pos - t0, kWideUnit - 1);
@@ -519,6 +530,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                     float y[32];
                     sums(col, y);
                     if (mine) finish(col, y, m, l);
+                    __syncwarp();
                 }
             } else {
                 // [D / 4][128] float4, then references and totals
@@ -528,10 +540,12 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                 for (int col = col0; col < col1; col += 32) {
                     float y[32];
                     sums(col, y);
-                    if (!mine) continue;                 // unused rows are not written, nor read below
+                    if (mine) {                          // unused rows are not written, nor read below
 #pragma unroll
-                    for (int i = 0; i < 32; i += 4)
-                        reinterpret_cast<float4*>(out)[((col + i) >> 2) * 128 + row] = make_float4(y[i], y[i + 1], y[i + 2], y[i + 3]);
+                        for (int i = 0; i < 32; i += 4)
+                            reinterpret_cast<float4*>(out)[((col + i) >> 2) * 128 + row] = make_float4(y[i], y[i + 1], y[i + 2], y[i + 3]);
+                    }
+                    __syncwarp();
                 }
                 if (part_no == 0) {
                     out[128 * D + row] = m;
@@ -545,6 +559,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                     if (last_here) a.counters[c0] = 0;
                     __threadfence();
                 }
+                __syncwarp();
                 meet();
                 if (*static_cast<volatile int*>(&last_here) && mine) {
                     __threadfence();
@@ -578,6 +593,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                         finish(col, y, m_all, l_all);
                     }
                 }
+                __syncwarp();
                 meet();                // `last_here` is free again
             }
             tc_fence_before();
