@@ -3,7 +3,6 @@
 
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
-#include <cuda_fp4.h>
 
 #include <cstdint>
 
@@ -56,11 +55,6 @@ __device__ __forceinline__ void e2m1x8_to_half2(uint32_t codes, uint32_t (&h)[4]
         "cvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\t"
         "cvt.rn.f16x2.e2m1x2 %2, c;\n\tcvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
         : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(codes));
-}
-
-// Two e2m1 codes (a byte) -> a pair of fp16.
-__device__ __forceinline__ float2 e2m1x2_to_float2(uint8_t codes) {
-    return __half22float2(__half2(__nv_cvt_fp4x2_to_halfraw2(codes, __NV_E2M1)));
 }
 
 // Two e4m3 bytes -> a pair of fp16 (exact).

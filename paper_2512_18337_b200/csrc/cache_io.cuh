@@ -16,13 +16,13 @@ struct KvStrides {
 constexpr int kIoThreads = 256, kIoBlocks = 2;   // 16-channel blocks of a thread: both loads are under way together
 
 // Block number g of a row -> token and block of the token.  A CTA starts at a 64-bit number and goes on in 32 bits; magic =
-// ceil(2^32 / per_token) divides numbers below 2^16 exactly.
+// ceil(2^32 / per_token) divides numbers below 2^16 exactly (per_token is 4 or 8 a head, so the multiplier fits 32 bits).
 struct IoPlace {
     int64_t token0;
     int rest0;
     __device__ __forceinline__ IoPlace(int64_t begin, int per_token) : token0(begin / per_token), rest0(static_cast<int>(begin - token0 * per_token)) {}
     __device__ __forceinline__ void at(int i, int per_token, uint32_t magic, int64_t& token, int& block) const {
-        const uint32_t g = rest0 + i, q = per_token == 1 ? g : __umulhi(g, magic);
+        const uint32_t g = rest0 + i, q = __umulhi(g, magic);
         token = token0 + q;
         block = g - q * per_token;
     }
