@@ -590,6 +590,7 @@ int sam_cache_read(const sam_cache* c, int32_t layer, int32_t B, int32_t Q, cons
  * query head h reads key/value head h / (H / n_kv_heads).  Query row i < n_new[b] (NULL: Q) of row b stands at position
  * p = seq_len + i and sees the positions j <= p - with window > 0 those with j > p - window only - whose page is
  * present:   out = sum_j softmax_j(scale * q.k_j) v_j,   lse = ln sum_j exp(scale * q.k_j)  (float [B, Q, H], or NULL).
+ * scale is finite (of either sign, or zero).
  * A row that sees nothing, and rows from n_new[b] on: out = 0, lse = -inf.  So the keys and values of the new tokens
  * are appended first; one call serves a single token, a proposal, or a chunk of a prompt.  Masked positions are never
  * computed with: what their bytes hold (NaN included) does not matter.

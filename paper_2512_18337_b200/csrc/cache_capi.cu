@@ -2,6 +2,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdint>
 
 #include "sam.h"
@@ -308,7 +309,7 @@ int sam_cache_attend(const sam_cache* c, int32_t layer, const void* q, int32_t d
                      void* workspace, int64_t workspace_bytes, void* cuda_stream) {
     if (int e = check_cache(c)) return e;
     if (int e = check_pages(c)) return e;
-    if (layer < 0 || layer >= c->n_layers || window < 0 || (dtype != SAM_CACHE_BF16 && dtype != SAM_CACHE_FP16)) return SAM_ERR_INVALID_ARG;
+    if (layer < 0 || layer >= c->n_layers || window < 0 || !std::isfinite(scale) || (dtype != SAM_CACHE_BF16 && dtype != SAM_CACHE_FP16)) return SAM_ERR_INVALID_ARG;
     const int64_t need = sam_cache_attend_workspace_bytes(c, B, Q, H);
     if (need < 0) return static_cast<int>(need);
     if (B == 0 || Q == 0) return SAM_OK;
