@@ -608,19 +608,19 @@ class SamCache:
             raise ValueError("tensors: the books " + ", ".join(self.BOOKS) + " are given all together or not at all")
         self.pages = given.get("pages")
         if self.pages is None:
-            self.pages = torch.empty(n_pages, n_layers, n_kv_heads, page_tokens // 16, 18 * head_dim, dtype=torch.uint8,
-                                     device=device)
+            self.pages = self._empty((n_pages, n_layers, n_kv_heads, page_tokens // 16, 18 * head_dim), torch.uint8, device,
+                                     stream)
         if self.pages.numel() * self.pages.element_size() != n_pages * self.page_bytes:
             raise ValueError("pages: n_pages * sam_cache_page_bytes() bytes are wanted")
         for name, shape in shapes.items():
             t = given.get(name)
             if t is None:
-                t = torch.empty(shape, dtype=torch.int32, device=device)
+                t = self._empty(shape, torch.int32, device, stream)
             if tuple(t.shape) != shape or t.dtype != torch.int32:
                 raise ValueError(f"{name}: an int32 tensor of shape {shape} is wanted")
             setattr(self, name, t)
         n_scratch = sam_cache_scratch_bytes(n_streams, n_pages)
-        self.scratch = torch.empty(n_scratch, dtype=torch.uint8, device=device)
+        self.scratch = self._empty(n_scratch, torch.uint8, device, stream)
         self.n_streams, self.n_kv_heads, self.head_dim = n_streams, n_kv_heads, head_dim
         self._struct = _CacheStruct(*(_dev(getattr(self, n)) for n in ("pages", *self.BOOKS, "scratch")), n_scratch,
                                     n_pages, page_tokens, n_streams, max_pages, n_layers, n_kv_heads, head_dim, k_exp,

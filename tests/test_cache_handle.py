@@ -80,3 +80,20 @@ def test_books_given_are_kept_and_others_made(calls):
         c = _cache(tensors=tensors)
         assert [x[0] for x in calls] == ["sam_cache_init"]
     assert c.pages is pages
+
+
+def test_what_a_cache_allocates_belongs_to_its_stream(calls, monkeypatch):
+    """The cache is emptied on the stream that it is made on: memory that another stream has just released, and may still be
+    writing to, must not be under it."""
+    made = []
+
+    def empty(shape, dtype, device, stream, zero=False):
+        made.append(stream)
+        return torch.zeros(shape, dtype=dtype)
+    monkeypatch.setattr(binding.SamCache, "_empty", staticmethod(empty))
+    for name in ("empty", "zeros"):
+        monkeypatch.setattr(torch, name, lambda *a, _make=getattr(torch, name), **kw: _make(*a, **kw) if "device" not in kw
+                            else pytest.fail("allocated without the stream"))
+    c = _cache(stream=1234)
+    assert calls == [("sam_cache_init", c.handle, 1234)]
+    assert made == [1234] * 8                              # pages, five books, scratch, workspace
