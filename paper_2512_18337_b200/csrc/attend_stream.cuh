@@ -17,10 +17,11 @@
 // from unit to unit, over the ends of segments.  Results of segments that end inside the warp's share are written directly;
 // the others meet in shared memory, and through global memory where a segment crosses CTAs.
 //
-// What it measured: two streams of 250,001 positions, 64/8 heads of 128: 141 us, 4.1 TB/s; 32 streams of 4,400 on average: 55 us, at
-// 6.2 TB/s between its first tiles and its last.  Some 640 instructions per unit, half of them on the half-rate pipes of the
-// conversions and packed multiplications, keep the issue slots 0.6 to 0.8 full: that, and 11 us of numbering, first tiles and
-// joining, is what it is bound by.
+// What it measured, from clocks that its warps wrote down: two streams of 250,001 positions, 64/8 heads of 128: 143 us, 4.0 TB/s.
+// The first tiles are there after 8 us (numbering, then a chain of dependent loads), half of the warps are through after 112, the
+// last after 125, and joining takes the other 18.  Until then 5.6 TB/s are read, 0.85 of the copy rate, with 0.7 of the issue slots
+// (677 instructions per unit).  32 streams of 4,400 on average: 57 us for 159 MB, 8 + 32 (at 5.0 TB/s) + 7 until the last warp + 10
+// for joining.  So it is the ends that bound it: the start, warps that are not through together, and the joining.
 #pragma once
 
 #include <type_traits>

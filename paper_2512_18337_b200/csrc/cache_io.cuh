@@ -1,8 +1,10 @@
 // Keys and values into the 4-bit cache (append) and back (read): one thread per 16-channel block.
 //
-// Both are bound by memory (a prompt of 49,152 tokens, 8 heads of 128: 258 MB each way) as long as a block costs few
-// instructions: with 64-bit divisions for the position, a correctly rounded division per element and element-wise maxima the
-// two took 163 us there; now it is 62 us (append, 4.2 TB/s) and 53 us (read, 4.9 TB/s).
+// A prompt of 49,152 tokens, 8 heads of 128, is 258 MB each way: append 62 us (4.2 TB/s), read 53 us (4.9 TB/s).  append is bound
+// by instructions: 288 for the 32 blocks of a warp, 0.84 of the issue slots (with 64-bit divisions for the position, a correctly
+// rounded division per element and element-wise maxima the two took 163 us).  It writes 2.4 million sectors where 1.8 hold the
+// bytes, since a warp's scales lie in four tiles.  read uses 0.67 of the slots; a thread's 32 bytes go out as two stores that fill
+// half a sector each, twice the write requests that the bytes need.
 #pragma once
 
 #include "cache_format.cuh"
