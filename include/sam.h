@@ -604,6 +604,126 @@ int sam_cache_attend(const sam_cache* c, int32_t layer, const void* q, int32_t d
                      void* out, int64_t out_row_stride, int64_t out_token_stride, int64_t out_head_stride,
                      float* lse, void* workspace, int64_t workspace_bytes, void* cuda_stream);
 
+/* ---------------------------------------------------------------- rotated appends, and attention over selected pages */
+
+/* For models that turn queries and keys by their position, and for contexts of which a query need not read everything:
+ *   sam_cache_append_rotated -> sam_cache_bounds_update -> sam_cache_select -> sam_cache_attend_blocks
+ * in a layer, between sam_cache_reserve and sam_cache_commit.  A block is a page's worth of positions: block i of a stream holds
+ * positions i * page_tokens ... and lies in the page that entry i of its table names. */
+
+/* Rotation: channel pair i < rotary_dim / 2 of a token at position p, (a, b) -> (a cos - b sin, b cos + a sin) with the angle
+ * p * inv_freq[i], sine and cosine times factor.  interleaved: the pair is channels (2i, 2i + 1), else (i, i + rotary_dim / 2).
+ * Channels from rotary_dim on stay as they are. */
+typedef struct sam_rope {
+    const uint64_t* turns;   /* device [rotary_dim / 2], from sam_rope_turns */
+    int32_t rotary_dim;      /* a multiple of 32, up to head_dim */
+    int32_t interleaved;
+    float factor;            /* finite; 1 for none */
+} sam_rope;
+
+/* inv_freq[0 .. n) (host, radians per position, finite, up to 10^6 in magnitude; n <= 64) -> turns (host): the turns per position in units of 2^-64, so that
+ * the angle of any position is exact to within 2^-31 of a turn.  Host only. */
+int sam_rope_turns(const double* inv_freq, int32_t n, uint64_t* turns);
+
+/* Append with rotation: queries q [B, Q, H, head_dim] are turned into q_out (which may be q itself with the same strides,
+ * and overlaps with it in no other way), keys are turned and quantised, values are quantised, into the positions that
+ * sam_cache_append would take.  Token i of row b stands at positions[b * Q + i] (device [B, Q], any int32), or with positions NULL where it is
+ * appended, seq_len + i.  Arithmetic is in 32 bits: a query is rounded once, to dtype, and a key once, to its code; values are stored as sam_cache_append
+ * stores them.  Query rows from n_new[b] on, and those of unknown streams, are zero in q_out.
+ * q and q_out have strides of their own (row, token, head in elements, channels contiguous); k and v share theirs.  H = 0: no queries (q, q_out are not used).
+ * H <= 16384, B * Q < 2^31. */
+int sam_cache_append_rotated(const sam_cache* c, int32_t layer,
+                             const void* q, int64_t q_row_stride, int64_t q_token_stride, int64_t q_head_stride,
+                             const void* k, const void* v, int64_t row_stride, int64_t token_stride, int64_t head_stride,
+                             void* q_out, int64_t out_row_stride, int64_t out_token_stride, int64_t out_head_stride,
+                             int32_t dtype, const sam_rope* rope, int32_t B, int32_t Q, int32_t H,
+                             const int32_t* streams, const int32_t* n_new, const int32_t* positions, void* cuda_stream);
+
+/* Bounds of pages: for each page, layer and key/value head the largest and the smallest key of every channel,
+ *   codes  device int8 [n_pages, n_layers, n_kv_heads, 2, head_dim], 16-byte aligned: ceil(largest / 2^e), floor(smallest / 2^e)
+ *   exps   device int8 [n_pages, n_layers, n_kv_heads]: the least e with |largest|, |smallest| <= 127 * 2^e for all channels
+ *          (0 for a page of zeros; 127, with codes of zero, for a page with a NaN among its keys)
+ * Both are the caller's; only pages that are full count, so they need no initialisation.
+ * sam_cache_bounds_update makes the bounds of one layer for the pages that the n_new[b] tokens behind seq_len fill up: call
+ * it after the append (a page that is filled again, after a roll back, is made again).
+ * sam_cache_bounds_rebuild makes those of all layers for the listed pages (device [n]; ids out of range are left out), or
+ * with pages NULL for pages 0 .. n - 1: after sam_cache_compact, after pages were copied in, or for a context that was cached without them. */
+int sam_cache_bounds_update(const sam_cache* c, int32_t layer, int8_t* codes, int8_t* exps,
+                            int32_t B, int32_t Q, const int32_t* streams, const int32_t* n_new, void* cuda_stream);
+int sam_cache_bounds_rebuild(const sam_cache* c, int8_t* codes, int8_t* exps, int32_t n, const int32_t* pages, void* cuda_stream);
+
+/* Select: which blocks each run of `share` consecutive query tokens reads, for each key/value head.  List l of row b serves the
+ * query tokens l * share ... of it that are below n_new[b] (NULL: Q); blocks is device [B, ceil(Q / share), n_kv_heads, n_blocks].
+ * Blocks that begin at or before the run's last position, and whose page is present, are listed
+ *   first: the first n_sink blocks, and from the block n_recent - 1 before that of the run's first token on (n_recent >= 1);
+ *   then, as far as there is room: pages with a NaN; then those with the largest scores, the lowest block of equal ones.
+ * The list is ascending and ends in -1s.  The score of a page is the largest over the run's tokens and the heads of the group of
+ *     2^(e_q + e_k) * sum over channels of max(q * largest, q * smallest)
+ * with the bounds' codes and the query in 8 bits: codes round(q / 2^e_q) with the least e_q >= -100 for which they are at most 127 (nearest, ties to even;
+ * infinities count as 127 and NaN, and rows below 2^-126, as zero).  The sum is exact, its product with the powers of two is a float (which may overflow to infinity).
+ * It bounds q.k from above, up to the rounding of q.  No score is computed where all blocks fit.
+ * n_sink + n_recent + (the blocks that `share` tokens can lie in) - 1 <= n_blocks is required.
+ * workspace: sam_cache_select_workspace_bytes() of device memory, 256-byte aligned, contents undefined between calls; calls
+ * that share it must not overlap on the device. */
+int64_t sam_cache_select_workspace_bytes(const sam_cache* c, int32_t B, int32_t Q, int32_t share);
+int sam_cache_select(const sam_cache* c, int32_t layer, const int8_t* codes, const int8_t* exps, const void* q, int32_t dtype,
+                     int64_t q_row_stride, int64_t q_token_stride, int64_t q_head_stride, int32_t B, int32_t Q, int32_t H,
+                     const int32_t* streams, const int32_t* n_new, int32_t share, int32_t n_sink, int32_t n_recent,
+                     int32_t* blocks, int32_t n_blocks, void* workspace, int64_t workspace_bytes, void* cuda_stream);
+
+/* Attend over listed blocks: as sam_cache_attend without a window, but a query token sees, of the positions up to its own, only
+ * those in the blocks of its list (blocks as sam_cache_select leaves them; any other list will do).  Of a list the first
+ * min(n_blocks, blocks up to the run's last position) entries are looked at: no list of different blocks is longer.
+ * Entries out of range, blocks without a page and blocks behind the run are passed over; a block that stands there twice counts twice.
+ * workspace as for sam_cache_attend, with sam_cache_attend_blocks_workspace_bytes(). */
+int64_t sam_cache_attend_blocks_workspace_bytes(const sam_cache* c, int32_t B, int32_t Q, int32_t H, int32_t share);
+int sam_cache_attend_blocks(const sam_cache* c, int32_t layer, const void* q, int32_t dtype,
+                            int64_t q_row_stride, int64_t q_token_stride, int64_t q_head_stride,
+                            int32_t B, int32_t Q, int32_t H, const int32_t* streams, const int32_t* n_new,
+                            const int32_t* blocks, int32_t n_blocks, int32_t share, float scale,
+                            void* out, int64_t out_row_stride, int64_t out_token_stride, int64_t out_head_stride,
+                            float* lse, void* workspace, int64_t workspace_bytes, void* cuda_stream);
+
+/* ---------------------------------------------------------------- penalties, biases and masks in verification */
+
+/* Verification of logits that are shaped first, without writing them: sam_argmax_shaped reduces every row to a packed word as
+ * sam_argmax_partial does, sam_verify_from_keys or sam_step_from_keys go on from there.  Row (b, j), asked after drafts[b, 0 .. j):
+ *     n = times that token t was said by stream streams[b], and stands in drafts[b, 0 .. j)        told = t was in its prompt
+ *     x = logits[b, j, t];   told or n > 0: x = x > 0 ? x / repetition[b] : x * repetition[b]
+ *     n > 0: x = (x - frequency[b] * n) - presence[b];     x = x + (sum of t's biases, in order);     t not in the mask: t is left out
+ * in 32 bits, every operation rounded to nearest.  The choice of a row is its largest x, the lowest t of equal ones; a NaN is
+ * no choice.  Where nothing allowed is above -inf it is the lowest allowed t, and -1 where nothing is allowed.
+ * All device memory; what is NULL is left out (repetition 1, presence and frequency 0). */
+typedef struct sam_shape {
+    const int32_t*  counts;        /* [n_streams, V]: times said; the sign bit: told */
+    const uint32_t* seen;          /* [n_streams, ceil(V / 32)]: bit t % 32 of word t / 32 is set where counts is not 0 */
+    const float*    repetition;    /* [B] */
+    const float*    presence;      /* [B] */
+    const float*    frequency;     /* [B] */
+    const int32_t*  bias_tokens;   /* [B, max_bias]; ids outside 0 .. V - 1 are passed over; biases of one token add up */
+    const float*    bias_values;   /* [B, max_bias] */
+    const int32_t*  n_bias;        /* [B], clamped to 0 .. max_bias; NULL: max_bias */
+    const uint32_t* masks;         /* [n_masks, ceil(V / 32)]: a set bit allows the token */
+    const int32_t*  mask_of;       /* [B, K + 1]: mask of each row; none for ids outside 0 .. n_masks - 1 */
+    int32_t n_streams, max_bias, n_masks;
+} sam_shape;
+
+/* logits, row_stride_elems, B, K, V, drafts: as in sam_verify (ids of drafts outside 0 .. V - 1 are passed over).  streams: device [B], or NULL
+ * for row b = stream b; an unknown stream has said nothing.  keys: device int64 [B * (K + 1)], 8-byte aligned, overwritten.
+ * sam_verify_from_keys decodes them (they are re-zeroed) and accepts as sam_verify does; values (device float [B, K + 1], or NULL) receives
+ * the shaped logit of each choice, -inf for none; keys of sam_argmax_partial will do too. */
+int sam_argmax_shaped(const void* logits_bf16, int64_t row_stride_elems, int32_t B, int32_t K, int32_t V, const int32_t* drafts,
+                      const int32_t* streams, const sam_shape* shape, int64_t* keys, void* cuda_stream);
+int sam_verify_from_keys(int64_t* keys, int32_t B, int32_t K, const int32_t* drafts, const int32_t* n_draft, int32_t* argmax_out,
+                         int32_t* accepted, int32_t* n_accepted, float* values, void* cuda_stream);
+
+/* The counts: sam_history_add adds tokens[b, 0 .. n[b]) (device [B, ld]; n NULL: ld; ids outside 0 .. V - 1 are passed over) to stream
+ * streams[b] (NULL: b; unknown ones are left out, one may be named more than once), as said, or with `told` as prompt.  sam_history_copy makes stream dst[i] a copy of stream src[i]
+ * (a dst appears once and is no src), or empty with src NULL.  A new table is empty: all bytes zero. */
+int sam_history_add(int32_t* counts, uint32_t* seen, int32_t n_streams, int32_t V, int32_t B, const int32_t* streams,
+                    const int32_t* tokens, int32_t ld, const int32_t* n, int32_t told, void* cuda_stream);
+int sam_history_copy(int32_t* counts, uint32_t* seen, int32_t n_streams, int32_t V, int32_t n, const int32_t* src, const int32_t* dst, void* cuda_stream);
+
 /* ---------------------------------------------------------------- diagnostics */
 
 /* Number of kernels this library has enqueued in this process so far (all entry points, all

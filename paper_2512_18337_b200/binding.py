@@ -6,6 +6,7 @@ path runs in the library's kernels - nothing is computed here.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 from pathlib import Path
 from typing import Optional
@@ -88,6 +89,21 @@ _SIGNATURES = {
     "sam_cache_attend_workspace_bytes": (_i64, [_vp, _i32, _i32, _i32]),
     "sam_cache_attend": (C.c_int, [_vp, _i32, _vp, _i32, _i64, _i64, _i64, _i32, _i32, _i32, _vp, _vp, C.c_float, _i32,
                                    _vp, _i64, _i64, _i64, _vp, _vp, _i64, _vp]),
+    "sam_rope_turns": (C.c_int, [_vp, _i32, _vp]),
+    "sam_cache_append_rotated": (C.c_int, [_vp, _i32, _vp, _i64, _i64, _i64, _vp, _vp, _i64, _i64, _i64, _vp, _i64, _i64,
+                                           _i64, _i32, _vp, _i32, _i32, _i32, _vp, _vp, _vp, _vp]),
+    "sam_cache_bounds_update": (C.c_int, [_vp, _i32, _vp, _vp, _i32, _i32, _vp, _vp, _vp]),
+    "sam_cache_bounds_rebuild": (C.c_int, [_vp, _vp, _vp, _i32, _vp, _vp]),
+    "sam_cache_select_workspace_bytes": (_i64, [_vp, _i32, _i32, _i32]),
+    "sam_cache_select": (C.c_int, [_vp, _i32, _vp, _vp, _vp, _i32, _i64, _i64, _i64, _i32, _i32, _i32, _vp, _vp, _i32, _i32,
+                                   _i32, _vp, _i32, _vp, _i64, _vp]),
+    "sam_cache_attend_blocks_workspace_bytes": (_i64, [_vp, _i32, _i32, _i32, _i32]),
+    "sam_cache_attend_blocks": (C.c_int, [_vp, _i32, _vp, _i32, _i64, _i64, _i64, _i32, _i32, _i32, _vp, _vp, _vp, _i32,
+                                          _i32, C.c_float, _vp, _i64, _i64, _i64, _vp, _vp, _i64, _vp]),
+    "sam_argmax_shaped": (C.c_int, [_vp, _i64, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp]),
+    "sam_verify_from_keys": (C.c_int, [_vp, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "sam_history_add": (C.c_int, [_vp, _vp, _i32, _i32, _i32, _vp, _vp, _i32, _vp, _i32, _vp]),
+    "sam_history_copy": (C.c_int, [_vp, _vp, _i32, _i32, _i32, _vp, _vp, _vp]),
 }
 
 
@@ -587,6 +603,75 @@ def sam_cache_attend(handle, layer, q, dtype, q_strides, B, Q, H, streams, n_new
                                     _stream(stream)), "sam_cache_attend")
 
 
+class _RopeStruct(C.Structure):
+    """struct sam_rope of include/sam.h."""
+    _fields_ = [("turns", _vp), ("rotary_dim", _i32), ("interleaved", _i32), ("factor", C.c_float)]
+
+
+def sam_rope_turns(inv_freq) -> np.ndarray:
+    """Radians per position -> turns per position in units of 2^-64 (uint64)."""
+    f = np.ascontiguousarray(inv_freq, dtype=np.float64)
+    turns = np.empty(f.size, np.uint64)
+    _check(_load().sam_rope_turns(f.ctypes.data, f.size, turns.ctypes.data), "sam_rope_turns")
+    return turns
+
+
+def sam_cache_append_rotated(handle, layer, q, q_strides, k, v, kv_strides, q_out, out_strides, dtype, rope, B, Q, H, streams,
+                             n_new, positions, stream=None) -> None:
+    """q, k, v, q_out: raw addresses or contiguous tensors; strides: (row, token, head) in elements; rope: address of a
+    sam_rope (SamRope.handle)."""
+    _check(_load().sam_cache_append_rotated(handle, layer, _dev(q), *q_strides, _dev(k), _dev(v), *kv_strides, _dev(q_out),
+                                            *out_strides, dtype, rope, B, Q, H, _dev(streams), _dev(n_new),
+                                            _dev(positions), _stream(stream)), "sam_cache_append_rotated")
+
+
+def sam_cache_bounds_update(handle, layer, codes, exps, B, Q, streams, n_new, stream=None) -> None:
+    _check(_load().sam_cache_bounds_update(handle, layer, _dev(codes), _dev(exps), B, Q, _dev(streams), _dev(n_new),
+                                           _stream(stream)), "sam_cache_bounds_update")
+
+
+def sam_cache_bounds_rebuild(handle, codes, exps, n, pages, stream=None) -> None:
+    _check(_load().sam_cache_bounds_rebuild(handle, _dev(codes), _dev(exps), n, _dev(pages), _stream(stream)),
+           "sam_cache_bounds_rebuild")
+
+
+def sam_cache_select_workspace_bytes(handle, B: int, Q: int, share: int) -> int:
+    return _size(_load().sam_cache_select_workspace_bytes(handle, B, Q, share), "sam_cache_select_workspace_bytes")
+
+
+def sam_cache_select(handle, layer, codes, exps, q, dtype, q_strides, B, Q, H, streams, n_new, share, n_sink, n_recent,
+                     blocks, n_blocks, workspace, workspace_bytes, stream=None) -> None:
+    _check(_load().sam_cache_select(handle, layer, _dev(codes), _dev(exps), _dev(q), dtype, *q_strides, B, Q, H,
+                                    _dev(streams), _dev(n_new), share, n_sink, n_recent, _dev(blocks), n_blocks,
+                                    _dev(workspace), workspace_bytes, _stream(stream)), "sam_cache_select")
+
+
+def sam_cache_attend_blocks_workspace_bytes(handle, B: int, Q: int, H: int, share: int) -> int:
+    return _size(_load().sam_cache_attend_blocks_workspace_bytes(handle, B, Q, H, share),
+                 "sam_cache_attend_blocks_workspace_bytes")
+
+
+def sam_cache_attend_blocks(handle, layer, q, dtype, q_strides, B, Q, H, streams, n_new, blocks, n_blocks, share, scale, out,
+                            out_strides, lse, workspace, workspace_bytes, stream=None) -> None:
+    _check(_load().sam_cache_attend_blocks(handle, layer, _dev(q), dtype, *q_strides, B, Q, H, _dev(streams), _dev(n_new),
+                                           _dev(blocks), n_blocks, share, scale, _dev(out), *out_strides, _dev(lse),
+                                           _dev(workspace), workspace_bytes, _stream(stream)), "sam_cache_attend_blocks")
+
+
+class SamRope:
+    """A rotation: inv_freq (radians per position of each channel pair, in double precision) and how channels pair up."""
+
+    def __init__(self, inv_freq, interleaved: bool = False, factor: float = 1.0, device="cuda:0", stream=None):
+        import torch
+        turns = torch.from_numpy(sam_rope_turns(inv_freq).view(np.int64))
+        self.turns = SamCache._empty(turns.shape, torch.int64, device, stream)
+        with SamCache._on(device, stream):
+            self.turns.copy_(turns)
+        self.rotary_dim = 2 * turns.numel()
+        self._struct = _RopeStruct(_dev(self.turns), self.rotary_dim, int(interleaved), factor)
+        self.handle = C.addressof(self._struct)
+
+
 class SamCache:
     """A paged 4-bit key/value cache: owns (or is given) the torch tensors behind a `sam_cache` and marshals its calls.
 
@@ -635,15 +720,23 @@ class SamCache:
             sam_cache_init(self.handle, stream)
 
     @staticmethod
+    def _on(device, stream):
+        """The context of the stream that a call runs on."""
+        import torch
+        if stream is None:
+            return contextlib.nullcontext()
+        if isinstance(stream, int):
+            stream = torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
+        return torch.cuda.stream(stream)
+
+    @staticmethod
     def _empty(shape, dtype, device, stream, zero=False):
         """A tensor that belongs to the stream that the call runs on, so that its memory is not handed on too early."""
         import torch
         make = torch.zeros if zero else torch.empty
         if stream is None:
             return make(shape, dtype=dtype, device=device)
-        if isinstance(stream, int):
-            stream = torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
-        with torch.cuda.stream(stream):
+        with SamCache._on(device, stream):
             return make(shape, dtype=dtype, device=device)
 
     def _dtype(self, t) -> int:
@@ -737,6 +830,212 @@ class SamCache:
                          self._index(n_new, B), self.head_dim ** -0.5 if scale is None else scale, window, po, so, lse,
                          workspace, workspace.numel() * workspace.element_size(), stream)
         return out, lse
+
+
+    def append_rotated(self, layer: int, q, k, v, rope: SamRope, n_new=None, streams=None, positions=None, out=None,
+                       stream=None):
+        """Queries and keys turned to their positions, keys and values appended; returns the turned queries (out may be q)."""
+        pq, sq = self._rows(q, None)
+        pk, sk = self._rows(k, self.n_kv_heads)
+        pv, sv = self._rows(v, self.n_kv_heads)
+        if k.shape != v.shape or k.dtype != v.dtype or (sk != sv and any(x != y and n > 1 for x, y, n in zip(sk, sv, k.shape))):
+            raise ValueError("keys and values of one shape, type and layout are wanted")
+        if q.dtype != k.dtype or q.shape[:2] != k.shape[:2]:
+            raise ValueError("queries of the keys' type, rows and tokens are wanted")
+        B, Q, H = q.shape[:3]
+        if out is None:
+            out = self._empty(q.shape, q.dtype, q.device, stream)
+        elif out.shape != q.shape or out.dtype != q.dtype:
+            raise ValueError("out like q is wanted")
+        po, so = self._rows(out, H)
+        if positions is not None and (tuple(positions.shape) != (B, Q) or positions.dtype != self.page_table.dtype):
+            raise ValueError("int32 positions [B, Q] are wanted")
+        sam_cache_append_rotated(self.handle, layer, pq, sq, pk, pv, sk, po, so, self._dtype(q.dtype), rope.handle, B, Q, H,
+                                 self._index(streams, B), self._index(n_new, B), positions, stream)
+        return out
+
+    def attend_blocks(self, layer: int, q, blocks, share: int = 1, n_new=None, streams=None, scale: Optional[float] = None,
+                      out=None, lse=None, workspace=None, stream=None):
+        """(out, lse) over the listed blocks [B, ceil(Q / share), n_kv_heads, n]; otherwise as attend."""
+        import torch
+        pq, sq = self._rows(q, None)
+        B, Q, H = q.shape[:3]
+        if out is None:
+            out = self._empty(q.shape, q.dtype, q.device, stream)
+        elif out.shape != q.shape or out.dtype != q.dtype:
+            raise ValueError("out like q is wanted")
+        if lse is None:
+            lse = self._empty((B, Q, H), torch.float32, q.device, stream)
+        elif tuple(lse.shape) != (B, Q, H) or lse.dtype != torch.float32:
+            raise ValueError("a float32 lse [B, Q, H] is wanted")
+        if share < 1 or tuple(blocks.shape[:3]) != (B, -(-Q // share), self.n_kv_heads) or blocks.dim() != 4 or \
+                blocks.dtype != torch.int32:
+            raise ValueError("int32 blocks [B, ceil(Q / share), n_kv_heads, n] are wanted")
+        po, so = self._rows(out, H)
+        if workspace is None:
+            workspace = self._ws
+        sam_cache_attend_blocks(self.handle, layer, pq, self._dtype(q.dtype), sq, B, Q, H, self._index(streams, B),
+                                self._index(n_new, B), blocks, blocks.shape[3], share,
+                                self.head_dim ** -0.5 if scale is None else scale, po, so, lse, workspace,
+                                workspace.numel() * workspace.element_size(), stream)
+        return out, lse
+
+
+class SamBounds:
+    """Bounds of the keys of a cache's pages, and the selection of blocks from them.  Owns (or is given) codes int8
+    [n_pages, n_layers, n_kv_heads, 2, head_dim] and exps int8 [n_pages, n_layers, n_kv_heads]."""
+
+    def __init__(self, cache: SamCache, codes=None, exps=None, device=None, stream=None):
+        import torch
+        self.cache = cache
+        n_pages, n_layers = cache._struct.n_pages, cache._struct.n_layers
+        shape = (n_pages, n_layers, cache.n_kv_heads)
+        device = cache.pages.device if device is None else device
+        for name, t, want in (("codes", codes, shape + (2, cache.head_dim)), ("exps", exps, shape)):
+            if t is None:
+                t = SamCache._empty(want, torch.int8, device, stream)
+            if tuple(t.shape) != want or t.dtype != torch.int8:
+                raise ValueError(f"{name}: an int8 tensor of shape {want} is wanted")
+            setattr(self, name, t)
+
+    def update(self, layer: int, max_new: int, n_new=None, streams=None, stream=None) -> None:
+        """After an append of up to max_new tokens a row: the bounds of the pages that it filled up."""
+        c = self.cache
+        B = next((t.numel() for t in (streams, n_new) if t is not None), c.n_streams)
+        sam_cache_bounds_update(c.handle, layer, self.codes, self.exps, B, max_new, c._index(streams, B),
+                                c._index(n_new, B), stream)
+
+    def rebuild(self, pages=None, stream=None) -> None:
+        """The bounds of the listed pages, or of all, in all layers."""
+        n = self.cache._struct.n_pages if pages is None else pages.numel()
+        sam_cache_bounds_rebuild(self.cache.handle, self.codes, self.exps, n, self.cache._index(pages, n), stream)
+
+    def select(self, layer: int, q, n_blocks: int, n_sink: int = 1, n_recent: int = 2, share: int = 1, n_new=None,
+               streams=None, out=None, workspace=None, stream=None):
+        """int32 blocks [B, ceil(Q / share), n_kv_heads, n_blocks] for attend_blocks."""
+        import torch
+        c = self.cache
+        pq, sq = c._rows(q, None)
+        B, Q, H = q.shape[:3]
+        n = sam_cache_select_workspace_bytes(c.handle, B, Q, share)
+        shape = (B, -(-Q // share), c.n_kv_heads, n_blocks)
+        if out is None:
+            out = c._empty(shape, torch.int32, q.device, stream)
+        elif tuple(out.shape) != shape or out.dtype != torch.int32:
+            raise ValueError(f"an int32 tensor of shape {shape} is wanted")
+        if workspace is None:
+            workspace = c._empty(n, torch.uint8, q.device, stream)
+        sam_cache_select(c.handle, layer, self.codes, self.exps, pq, c._dtype(q.dtype), sq, B, Q, H, c._index(streams, B),
+                         c._index(n_new, B), share, n_sink, n_recent, out, n_blocks, workspace,
+                         workspace.numel() * workspace.element_size(), stream)
+        return out
+
+
+# ------------------------------------------------------------------ penalties, biases and masks
+class _ShapeStruct(C.Structure):
+    """struct sam_shape of include/sam.h."""
+    _fields_ = [(n, _vp) for n in ("counts", "seen", "repetition", "presence", "frequency", "bias_tokens", "bias_values",
+                                   "n_bias", "masks", "mask_of")] + \
+        [(n, _i32) for n in ("n_streams", "max_bias", "n_masks")]
+
+
+def sam_argmax_shaped(logits, row_stride, B, K, V, drafts, shape, keys, streams=None, stream=None) -> None:
+    """shape: a SamShape (or the address of a sam_shape); keys: int64 [B * (K + 1)]."""
+    handle = shape.check(B, K, V) if isinstance(shape, SamShape) else shape
+    _check(_load().sam_argmax_shaped(_dev(logits), row_stride, B, K, V, _dev(drafts), _dev(streams), handle, _dev(keys),
+                                     _stream(stream)), "sam_argmax_shaped")
+
+
+def sam_verify_from_keys(keys, B, K, drafts, n_draft, argmax_out, accepted, n_accepted, values=None, stream=None) -> None:
+    _check(_load().sam_verify_from_keys(_dev(keys), B, K, _dev(drafts), _dev(n_draft), _dev(argmax_out), _dev(accepted),
+                                        _dev(n_accepted), _dev(values), _stream(stream)), "sam_verify_from_keys")
+
+
+def sam_history_add(counts, seen, n_streams, V, B, streams, tokens, ld, n, told, stream=None) -> None:
+    _check(_load().sam_history_add(_dev(counts), _dev(seen), n_streams, V, B, _dev(streams), _dev(tokens), ld, _dev(n),
+                                   int(told), _stream(stream)), "sam_history_add")
+
+
+def sam_history_copy(counts, seen, n_streams, V, n, src, dst, stream=None) -> None:
+    _check(_load().sam_history_copy(_dev(counts), _dev(seen), n_streams, V, n, _dev(src), _dev(dst), _stream(stream)),
+           "sam_history_copy")
+
+
+class SamHistory:
+    """What each stream was told and has said: counts int32 [n_streams, V] and seen int32 [n_streams, ceil(V / 32)]."""
+
+    def __init__(self, n_streams: int, V: int, device="cuda:0", stream=None):
+        import torch
+        self.n_streams, self.V = n_streams, V
+        self.counts = SamCache._empty((n_streams, V), torch.int32, device, stream, zero=True)
+        self.seen = SamCache._empty((n_streams, -(-V // 32)), torch.int32, device, stream, zero=True)
+
+    def _rows(self, t, B: int):
+        if t is not None and (t.dtype != self.counts.dtype or t.numel() != B):
+            raise ValueError("an int32 tensor with one entry per row is wanted")
+        return t
+
+    def add(self, tokens, n=None, streams=None, told: bool = False, stream=None) -> None:
+        """tokens int32 [B, ld], of which the first n[b] count; told: they were in the prompt."""
+        if tokens.dim() != 2 or tokens.dtype != self.counts.dtype:
+            raise ValueError("int32 tokens [B, ld] are wanted")
+        B, ld = tokens.shape
+        sam_history_add(self.counts, self.seen, self.n_streams, self.V, B, self._rows(streams, B), tokens, ld,
+                        self._rows(n, B), told, stream)
+
+    def fork(self, src, dst, stream=None) -> None:
+        n = src.numel()
+        sam_history_copy(self.counts, self.seen, self.n_streams, self.V, n, self._rows(src, n), self._rows(dst, n), stream)
+
+    def reset(self, streams, stream=None) -> None:
+        n = streams.numel()
+        sam_history_copy(self.counts, self.seen, self.n_streams, self.V, n, None, self._rows(streams, n), stream)
+
+
+class SamShape:
+    """What logits are shaped by: keeps the tensors behind a `sam_shape` (all but V may be absent).
+
+    counts, seen: of a SamHistory; repetition, presence, frequency: float32 [B]; bias_tokens int32, bias_values float32
+    [B, n], n_bias int32 [B]; masks int32 [n, ceil(V / 32)] (a set bit allows a token) and mask_of int32 [B, K + 1]."""
+
+    def __init__(self, V: int, counts=None, seen=None, repetition=None, presence=None, frequency=None, bias_tokens=None,
+                 bias_values=None, n_bias=None, masks=None, mask_of=None):
+        import torch
+        words = -(-V // 32)
+        self.V, self.mask_of, self.tensors = V, mask_of, dict(
+            counts=counts, seen=seen, repetition=repetition, presence=presence, frequency=frequency, bias_tokens=bias_tokens,
+            bias_values=bias_values, n_bias=n_bias, masks=masks, mask_of=mask_of)
+        for name, last in (("counts", V), ("seen", words), ("masks", words), ("bias_tokens", None), ("mask_of", None)):
+            t = self.tensors[name]
+            if t is not None and (t.dim() != 2 or t.dtype != torch.int32 or (last and t.shape[1] != last)):
+                raise ValueError(f"{name}: an int32 matrix{f' with {last} columns' if last else ''} is wanted")
+        for pair in (("counts", "seen"), ("bias_tokens", "bias_values"), ("masks", "mask_of")):
+            if len({self.tensors[n] is None for n in pair}) > 1:
+                raise ValueError(" and ".join(pair) + " are given together or not at all")
+        if counts is not None and counts.shape[0] != seen.shape[0]:
+            raise ValueError("counts and seen of the same streams are wanted")
+        if bias_tokens is not None and (bias_values.shape != bias_tokens.shape or bias_values.dtype != torch.float32):
+            raise ValueError("bias_values: a float32 tensor like bias_tokens is wanted")
+        for name, kind in (("repetition", torch.float32), ("presence", torch.float32), ("frequency", torch.float32),
+                           ("n_bias", torch.int32)):
+            t = self.tensors[name]
+            if t is not None and (t.dim() != 1 or t.dtype != kind):
+                raise ValueError(f"{name}: a {str(kind)[6:]} vector is wanted")
+        n_bias_columns = 0 if bias_tokens is None else bias_tokens.shape[1]
+        address = {n: None if t is not None and t.numel() == 0 else _dev(t) for n, t in self.tensors.items()}
+        self._struct = _ShapeStruct(*address.values(), 0 if counts is None else counts.shape[0], n_bias_columns,
+                                    0 if masks is None else masks.shape[0])
+        self.handle = C.addressof(self._struct)
+
+    def check(self, B: int, K: int, V: int) -> int:
+        """The handle, if the tensors fit a call of this shape."""
+        if V != self.V:
+            raise ValueError("made for another vocabulary")
+        for name in ("repetition", "presence", "frequency", "bias_tokens", "n_bias", "mask_of"):
+            t = self.tensors[name]
+            if t is not None and (t.shape[0] < B or (name == "mask_of" and t.shape[1] != K + 1)):
+                raise ValueError(f"{name}: too small for {B} rows of {K + 1}")
+        return self.handle
 
 
 # ------------------------------------------------------------------ convenience holder

@@ -123,7 +123,7 @@ struct StreamCursor {
     }
     __device__ __forceinline__ int64_t seg_begin() const { return base + (static_cast<int64_t>(head) * tiles + rt) * steps; }
     // To the first unit of the next segment; the caller knows that there is one.
-    template <int kRows>
+    template <int kRows, bool kListed>
     __device__ __forceinline__ void next_segment(const AttendArgs& a) {
         step = 0;
         if (++rt < tiles) return;
@@ -131,8 +131,8 @@ struct StreamCursor {
         if (++head < a.c.n_kv) return;
         head = 0;
         base += static_cast<int64_t>(steps) * tiles * a.c.n_kv;
-        do enter<kRows>(a, b + 1, row_info<kStreamUnit>(a, b + 1));
-        while (steps == 0 && b + 1 < a.B);
+        do enter<kRows>(a, b + 1, row_info<kStreamUnit, kListed>(a, b + 1));
+        while (steps == 0 && b + 1 < a.runs);
     }
 };
 
@@ -164,7 +164,9 @@ __device__ __forceinline__ void join_partials(int count, Get get, Put put) {
     }
 }
 
-template <typename T, int D, int NT>
+// kListed: over listed blocks.  The tokens of a segment are then the places of its list; where the two tiles of a unit really begin
+// stands beside the ring.
+template <typename T, int D, int NT, bool kListed>
 __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm) attend_stream_kernel(const __grid_constant__ AttendArgs a) {
     using Plan = StreamPlan<D, NT>;
     constexpr int KW = D / 32, VW = D / 64, MT = D / 16;     // words of a token that a thread reads: keys, values; M tiles of O^T
@@ -177,6 +179,7 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
     __shared__ StreamPiece pieces[kStreamWarps][2];
     __shared__ int last_here;
     __shared__ bool gave_up[kStreamWarps];
+    __shared__ int2 unit_begin[kListed ? kStreamWarps : 1][kStages];   // listed: positions of the first tokens of a unit's tiles
 
     const CacheView& c = a.c;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -187,7 +190,7 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
     bool count_segments = true;
     RowInfo ri{};                                          // of the row that the thread looked at last
     auto units_of = [&](int b) -> int64_t {
-        ri = row_info<kStreamUnit>(a, b);
+        ri = row_info<kStreamUnit, kListed>(a, b);
         const int tiles = (ri.n * a.group + kRows - 1) / kRows;
         if (count_segments) segments += tiles * c.n_kv;
         return static_cast<int64_t>(row_steps<kStreamUnit>(ri)) * tiles * c.n_kv;
@@ -216,8 +219,8 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
     if (tid < kStreamWarps) gave_up[tid] = false;
     barrier_init_fence();
     int64_t units = 0, mine = 0, before = 0, unused;
-    for (int b0 = 0; b0 < a.B; b0 += kStreamThreads) {
-        mine = b0 + tid < a.B ? units_of(b0 + tid) : 0;
+    for (int b0 = 0; b0 < a.runs; b0 += kStreamThreads) {
+        mine = b0 + tid < a.runs ? units_of(b0 + tid) : 0;
         units += block_sum(mine, &before);
     }
     count_segments = false;
@@ -232,11 +235,11 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
     const int64_t cta_begin = busy ? shares.begin(cta) : 0, cta_units = busy ? shares.begin(cta + 1) - cta_begin : 0;
     const Shares warp_shares(cta_units, kStreamWarps);
     if (busy) {
-        const bool once = a.B <= kStreamThreads;
+        const bool once = a.runs <= kStreamThreads;
         int64_t sum = 0;
-        for (int b0 = 0; b0 < a.B; b0 += kStreamThreads) {
+        for (int b0 = 0; b0 < a.runs; b0 += kStreamThreads) {
             if (!once) {
-                mine = b0 + tid < a.B ? units_of(b0 + tid) : 0;
+                mine = b0 + tid < a.runs ? units_of(b0 + tid) : 0;
                 const int64_t all = block_sum(mine, &before);
                 before += sum;
                 sum += all;
@@ -265,14 +268,35 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
     const uint8_t* from0 = nullptr;    // the two tiles of the lane's step
     const uint8_t* from1 = nullptr;
     uint32_t have0 = 0, have1 = 0;     // bit l: lane l has them
+    int begin0 = 0, begin1 = 0;        // listed: positions of their first tokens
     int page_step = -1;
     auto fill = [&](int stage) {
         if (to_load == 0) return;
         if (page_step < 0 || in.step - page_step >= 32) {
             page_step = in.step;
             const int t = in.ri.lo + (page_step + lane) * kStreamUnit, i = t >> c.log_p, slot = t & (c.page_tokens() - 1);
-            const int page0 = t < in.ri.hi && t >= 0 ? c.page_at(in.ri.s, i) : -1;
-            const int page1 = t + 16 >= in.ri.hi || t < 0 ? -1 : c.log_p > 4 ? page0 : c.page_at(in.ri.s, i + 1);
+            int page0, page1;
+            if constexpr (kListed) {
+                const int32_t* list = a.blocks + (static_cast<int64_t>(in.b) * c.n_kv + in.head) * a.n_blocks;
+                const int end = run_end(a, in.ri);
+                // of a place in the list: the page, if there is one and some query sees of its tile that begins at `slot`
+                auto look = [&](bool on, int place, int at, int& begin) {
+                    const int block = on ? list[place] : -1;
+                    if (static_cast<unsigned>(block) >= static_cast<unsigned>(c.max_pages)) return -1;
+                    begin = (block << c.log_p) + at;
+                    return begin < end ? c.page_at(in.ri.s, block) : -1;
+                };
+                page0 = look(t < in.ri.hi && t >= 0, i, slot, begin0);
+                if (c.log_p > 4) {
+                    begin1 = begin0 + 16;
+                    page1 = begin1 < end ? page0 : -1;
+                } else {
+                    page1 = look(t + 16 < in.ri.hi && t >= 0, i + 1, 0, begin1);
+                }
+            } else {
+                page0 = t < in.ri.hi && t >= 0 ? c.page_at(in.ri.s, i) : -1;
+                page1 = t + 16 >= in.ri.hi || t < 0 ? -1 : c.log_p > 4 ? page0 : c.page_at(in.ri.s, i + 1);
+            }
             from0 = c.tile(max(page0, 0), a.layer, in.head, slot);
             from1 = c.tile(max(page1, 0), a.layer, in.head, c.log_p > 4 ? slot + 16 : 0);
             have0 = __ballot_sync(0xffffffffu, page0 >= 0);
@@ -283,6 +307,7 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
         present = (present & ~(3u << (2 * stage))) | on << (2 * stage);
         if (lane == l) {
             const uint32_t dst = ring + stage * Plan::kUnitBytes, bar = bar0 + stage * 8;
+            if constexpr (kListed) unit_begin[warp][stage] = make_int2(begin0, begin1);
             barrier_expect(bar, __popc(on) * Plan::kTile);
             if (on == 3 && c.log_p > 4) {
                 bulk_load(dst, from0, Plan::kUnitBytes, bar);
@@ -293,7 +318,7 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
         }
         --to_load;
         if (++in.step == in.steps && to_load) {
-            in.next_segment<kRows>(a);
+            in.next_segment<kRows, kListed>(a);
             page_step = -1;
         }
     };
@@ -329,7 +354,8 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
             int e_row = 0;
             alignas(16) T x[KW * 8];
             if (n < rows) {
-                const T* q = static_cast<const T*>(a.q) + cur.b * a.q_row + rho / a.group * a.q_token +
+                const RunPlace at = run_place<kListed>(a, cur.b);
+                const T* q = static_cast<const T*>(a.q) + at.b * a.q_row + (at.i0 + rho / a.group) * a.q_token +
                              (cur.head * a.group + rho % a.group) * a.q_head + j * (D / 4);
                 if (a.q_wide) {
 #pragma unroll
@@ -386,10 +412,16 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
                               [&](int i) { return barrier_try(bar0 + (it + i) % kStages * 8, ((it + i) / kStages) & 1); });
                 to_load = 0;
             }
-            const int t0 = cur.ri.lo + (s0 + k) * kStreamUnit;
+            int t0 = cur.ri.lo + (s0 + k) * kStreamUnit, t1 = t0 + 16;   // positions of the first tokens of the unit's tiles
+            if constexpr (kListed) {
+                __syncwarp();                              // the lane that filled the unit wrote them
+                const int2 begin = unit_begin[warp][stage];
+                t0 = begin.x;
+                t1 = begin.y;
+            }
             const uint32_t unit = ring + stage * Plan::kUnitBytes;
             const uint32_t here = (present >> (2 * stage)) & 3;
-            const bool full = here == 3 && t0 + kStreamUnit - 1 <= first_pos && (a.window == 0 || t0 > last_pos - a.window);
+            const bool full = here == 3 && t1 + 15 <= first_pos && (kListed ? t0 + 15 <= first_pos : a.window == 0 || t0 > last_pos - a.window);
 
             // ---- S^T = K Q^T
             float s[2][NT][4];
@@ -441,8 +473,8 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
                     for (int h = 0; h < 2; ++h)
 #pragma unroll
                         for (int x = 0; x < 4; ++x) {
-                            const int t = t0 + h * 16 + tok + (x >> 1) * 8, p = pos[nt][x & 1];
-                            const bool seen = ((here >> h) & 1) && t <= p && (a.window == 0 || t > p - a.window);
+                            const int t = (h ? t1 : t0) + tok + (x >> 1) * 8, p = pos[nt][x & 1];
+                            const bool seen = ((here >> h) & 1) && t <= p && (kListed || a.window == 0 || t > p - a.window);
                             s[h][nt][x] = seen ? s[h][nt][x] : -INFINITY;
                         }
             }
@@ -505,11 +537,11 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
                 if (!full) {
                     // what is masked must not be multiplied with: absent tiles and tokens behind the last get a zero scale; a NaN
                     // that only some rows see is taken out here and given to those rows
-                    const int t = t0 + h * 16;
+                    const int t = h ? t1 : t0, end = kListed ? run_end(a, cur.ri) : cur.ri.hi;
                     const bool on = (here >> h) & 1;
                     uint32_t nans = 0;
                     auto clean = [&](uint32_t& b, int token, int bit) {
-                        if (!on || t + token >= cur.ri.hi) b = 0;
+                        if (!on || t + token >= end) b = 0;
                         if ((b & 0x7f) == 0x7f) {
                             b = 0;
                             nans |= 1u << bit;
@@ -529,7 +561,7 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
                                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                                     for (int x = 0; x < 2; ++x)
-                                        if (token <= pos[nt][x] && (a.window == 0 || token > pos[nt][x] - a.window))
+                                        if (token <= pos[nt][x] && (kListed || a.window == 0 || token > pos[nt][x] - a.window))
 #pragma unroll
                                             for (int mt = 0; mt < MT; ++mt) o[mt][nt][x] = o[mt][nt][x + 2] = __int_as_float(0x7fffffff);
                             }
@@ -589,12 +621,13 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
                 }
                 if (begins && ends) {
                     if (n < rows) {
-                        const int rho = cur.rt * kRows + n, i = rho / a.group, h = cur.head * a.group + rho % a.group;
+                        const RunPlace at = run_place<kListed>(a, cur.b);
+                        const int rho = cur.rt * kRows + n, i = at.i0 + rho / a.group, h = cur.head * a.group + rho % a.group;
                         const float f = finish_factor(l[nt][x], c.v_exp);
 #pragma unroll
                         for (int d = 0; d < MT * 2; ++d) y[d] = l[nt][x] == 0.f ? 0.f : y[d] * f;
-                        store_row<T>(static_cast<T*>(a.out) + cur.b * a.o_row + i * a.o_token + h * a.o_head + r * (MT * 2), y, a.o_wide);
-                        if (a.lse && r == 0) a.lse[(static_cast<int64_t>(cur.b) * a.Q + i) * a.H + h] = finish_lse(m[nt][x], l[nt][x]);
+                        store_row<T>(static_cast<T*>(a.out) + at.b * a.o_row + i * a.o_token + h * a.o_head + r * (MT * 2), y, a.o_wide);
+                        if (a.lse && r == 0) a.lse[(static_cast<int64_t>(at.b) * a.Q + i) * a.H + h] = finish_lse(m[nt][x], l[nt][x]);
                     }
                 } else {
 #pragma unroll
@@ -620,7 +653,7 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
         }
         left -= count;
         cur.step += count;
-        if (left) cur.next_segment<kRows>(a);
+        if (left) cur.next_segment<kRows, kListed>(a);
     }
     if (gave_up[warp] && c.meta && lane == 0) atomicOr(&c.meta[1], kStatusGaveUp);
     if (!busy) return;
@@ -630,9 +663,10 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
     auto write_row = [&](const StreamPiece& d, int n, int ch, float4 x, float top, float l) {
         const int rho = d.rt * kRows + n;
         if (rho >= d.n * a.group) return;
-        const int i = rho / a.group, h = d.head * a.group + rho % a.group;
+        const RunPlace at = run_place<kListed>(a, d.b);
+        const int i = at.i0 + rho / a.group, h = d.head * a.group + rho % a.group;
         const float f = finish_factor(l, c.v_exp);
-        T* out = static_cast<T*>(a.out) + d.b * a.o_row + i * a.o_token + h * a.o_head + ch;
+        T* out = static_cast<T*>(a.out) + at.b * a.o_row + i * a.o_token + h * a.o_head + ch;
         const float y[4] = {l == 0.f ? 0.f : x.x * f, l == 0.f ? 0.f : x.y * f, l == 0.f ? 0.f : x.z * f, l == 0.f ? 0.f : x.w * f};
         alignas(8) T e[4];
 #pragma unroll
@@ -643,7 +677,7 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
 #pragma unroll
             for (int k = 0; k < 4; ++k) out[k] = e[k];
         }
-        if (a.lse && ch == 0) a.lse[(static_cast<int64_t>(d.b) * a.Q + i) * a.H + h] = finish_lse(top, l);
+        if (a.lse && ch == 0) a.lse[(static_cast<int64_t>(at.b) * a.Q + i) * a.H + h] = finish_lse(top, l);
     };
     int crossing = -1, crossing2 = -1;   // first pieces of the segments that cross CTAs (at most two): warp * 2 + slot
     for (int w0 = 0; w0 < kStreamWarps; ++w0)

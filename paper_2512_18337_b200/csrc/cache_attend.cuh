@@ -27,17 +27,47 @@ struct AttendArgs {
     bool q_wide, o_wide;      // every row starts on a 16-byte boundary
     int32_t* counters;        // [grid], zero between calls
     float* partials;          // [2 * grid] partial results
+    // Attention over listed blocks only: `share` query tokens in a row of the batch have a list in common, and such a run is what
+    // the kernels take for a row ("run"): number v of it is run v % lists of row v / lists.  Otherwise a run is a row.
+    const int32_t* blocks;    // [B, lists, n_kv, n_blocks]
+    int32_t runs, lists, share, n_blocks;
 };
+
+// Row of the batch and first query token of a run.
+struct RunPlace {
+    int b, i0;
+};
+template <bool kListed>
+__device__ __forceinline__ RunPlace run_place(const AttendArgs& a, int v) {
+    if constexpr (!kListed) return {v, 0};
+    const int b = v / a.lists;
+    return {b, (v - b * a.lists) * a.share};
+}
 
 // One row of the batch as every kernel sees it.
 struct RowInfo {
     int s;          // stream, -1 = unknown
-    int len, n;     // committed tokens; query rows that are computed
-    int lo, hi;     // tokens [lo, hi) may be seen by one of the query rows; lo is a multiple of the unit
+    int len, n;     // tokens before the first query token; query tokens that are computed
+    int lo, hi;     // tokens [lo, hi) may be seen by one of the query rows; lo is a multiple of the unit.  Listed: places in the list times page_tokens
 };
-template <int kUnit>
-__device__ __forceinline__ RowInfo row_info(const AttendArgs& a, int b) {
+// First position behind all that a run's queries see.
+__device__ __forceinline__ int run_end(const AttendArgs& a, const RowInfo& r) {
+    return static_cast<int>(min(static_cast<int64_t>(r.len) + r.n, static_cast<int64_t>(a.c.capacity())));
+}
+template <int kUnit, bool kListed = false>
+__device__ __forceinline__ RowInfo row_info(const AttendArgs& a, int v) {
     RowInfo r;
+    if constexpr (kListed) {
+        const RunPlace at = run_place<true>(a, v);
+        r.s = a.c.stream_of(a.streams, at.b);
+        r.n = r.s < 0 ? 0 : min(max((a.n_new ? min(a.n_new[at.b], a.Q) : a.Q) - at.i0, 0), a.share);
+        r.len = r.s < 0 ? 0 : a.c.length_of(r.s) + at.i0;
+        r.lo = 0;
+        // no list of different blocks is longer than the blocks up to the last query's own
+        r.hi = min(a.n_blocks, ((run_end(a, r) - 1) >> a.c.log_p) + 1) << a.c.log_p;
+        return r;
+    }
+    const int b = v;
     r.s = a.c.stream_of(a.streams, b);
     r.n = r.s < 0 ? 0 : max(a.n_new ? min(a.n_new[b], a.Q) : a.Q, 0);
     r.len = r.s < 0 ? 0 : a.c.length_of(r.s);

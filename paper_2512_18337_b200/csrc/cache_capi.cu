@@ -13,6 +13,8 @@
 #include "cache_format.cuh"
 #include "cache_io.cuh"
 #include "cache_pages.cuh"
+#include "cache_rotate.cuh"
+#include "cache_select.cuh"
 
 using namespace samb200;
 
@@ -133,12 +135,12 @@ int allow_shared(K* kernel, int bytes, uint64_t* asked) {   // asked: the kernel
     return SAM_OK;
 }
 
-template <typename T, int D, int NT>
+template <typename T, int D, int NT, bool kListed>
 int launch_stream(const AttendArgs& a, int sms, cudaStream_t s) {
     using Plan = StreamPlan<D, NT>;
     static thread_local uint64_t asked = 0;
-    if (int e = allow_shared(attend_stream_kernel<T, D, NT>, Plan::kSmem, &asked)) return e;
-    attend_stream_kernel<T, D, NT><<<std::min(sms * Plan::kCtasPerSm, kMaxCtas), kStreamThreads, Plan::kSmem, s>>>(a);
+    if (int e = allow_shared(attend_stream_kernel<T, D, NT, kListed>, Plan::kSmem, &asked)) return e;
+    attend_stream_kernel<T, D, NT, kListed><<<std::min(sms * Plan::kCtasPerSm, kMaxCtas), kStreamThreads, Plan::kSmem, s>>>(a);
     return launched();
 }
 
@@ -156,9 +158,59 @@ int launch_attend(const AttendArgs& a, cudaStream_t s) {
     DeviceInfo di;
     if (int e = device_info(&di)) return e;
     const int64_t rows = static_cast<int64_t>(a.Q) * a.group;
-    if (rows <= 8) return launch_stream<T, D, 1>(a, di.sms, s);
-    if (rows <= kNarrowRows) return launch_stream<T, D, 2>(a, di.sms, s);
+    if (rows <= 8) return launch_stream<T, D, 1, false>(a, di.sms, s);
+    if (rows <= kNarrowRows) return launch_stream<T, D, 2, false>(a, di.sms, s);
     return launch_wide<T, D>(a, di.sms, s);
+}
+
+template <typename T, int D>
+int launch_attend_blocks(const AttendArgs& a, cudaStream_t s) {
+    DeviceInfo di;
+    if (int e = device_info(&di)) return e;
+    const int64_t rows = static_cast<int64_t>(a.share) * a.group;
+    if (rows <= 8) return launch_stream<T, D, 1, true>(a, di.sms, s);
+    return launch_stream<T, D, 2, true>(a, di.sms, s);
+}
+
+// Scores and picks for all lists, as many at a time as the keys have room for.
+template <typename T>
+int launch_select(SelectArgs a, int64_t key_bytes, cudaStream_t s) {
+    DeviceInfo di;
+    if (int e = device_info(&di)) return e;
+    const int64_t runs = static_cast<int64_t>(a.B) * a.lists, each = static_cast<int64_t>(a.c.n_kv) * a.c.max_pages * 4;
+    const int64_t most = std::min<int64_t>(std::max<int64_t>(key_bytes / each, 1), 65535);
+    for (int64_t at = 0; at < runs; at += most) {
+        a.first_run = at;
+        a.runs = static_cast<int32_t>(std::min(runs - at, most));
+        // a warp takes sixteen pages; about eight blocks an SM
+        const int64_t full = (static_cast<int64_t>(a.c.max_pages) + kScoreThreads / 2 - 1) / (kScoreThreads / 2);
+        const int64_t wanted = (static_cast<int64_t>(di.sms) * 8 + a.runs * a.c.n_kv - 1) / (static_cast<int64_t>(a.runs) * a.c.n_kv);
+        const dim3 grid(static_cast<unsigned>(std::min(full, wanted)), a.c.n_kv, a.runs);
+        if (a.c.D == 64) select_score_kernel<T, 64><<<grid, kScoreThreads, 0, s>>>(a);
+        else select_score_kernel<T, 128><<<grid, kScoreThreads, 0, s>>>(a);
+        if (int e = launched()) return e;
+        select_pick_kernel<<<dim3(a.c.n_kv, a.runs), kPickThreads, 0, s>>>(a);
+        if (int e = launched()) return e;
+    }
+    return SAM_OK;
+}
+
+int check_layer_call(const sam_cache* c, int32_t layer, int32_t B, int32_t Q, const int32_t* streams) {
+    if (int e = check_cache(c)) return e;
+    if (int e = check_pages(c)) return e;
+    if (layer < 0 || layer >= c->n_layers || B < 0 || Q < 0) return SAM_ERR_INVALID_ARG;
+    if (B > SAM_CACHE_MAX_B || Q > kLargest) return SAM_ERR_TOO_LARGE;
+    return !streams && B > c->n_streams ? SAM_ERR_INVALID_ARG : SAM_OK;
+}
+
+int check_bounds(const int8_t* codes, const int8_t* exps) { return codes && exps && aligned(codes, 16) ? SAM_OK : SAM_ERR_INVALID_ARG; }
+
+constexpr int64_t kKeyBytes = int64_t(128) << 20;   // of the keys that are in flight at a time, where there are as many
+
+template <typename T>
+int launch_turn(const TurnArgs& a, cudaStream_t s) {
+    append_rotated_kernel<T><<<dim3((a.Q + a.tokens - 1) / a.tokens, a.B), kTurnThreads, 0, s>>>(a);
+    return launched();
 }
 
 }  // namespace
@@ -341,10 +393,201 @@ int sam_cache_attend(const sam_cache* c, int32_t layer, const void* q, int32_t d
     a.o_wide = aligned(out, 16) && (out_row_stride | out_token_stride | out_head_stride) % 8 == 0;
     a.counters = static_cast<int32_t*>(workspace);
     a.partials = reinterpret_cast<float*>(static_cast<char*>(workspace) + kCounterBytes);
+    a.blocks = nullptr;
+    a.runs = B;
+    a.lists = 1;
+    a.share = Q;
+    a.n_blocks = 0;
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     const bool bf16 = dtype == SAM_CACHE_BF16;
     if (c->head_dim == 64) return bf16 ? launch_attend<__nv_bfloat16, 64>(a, s) : launch_attend<__half, 64>(a, s);
     return bf16 ? launch_attend<__nv_bfloat16, 128>(a, s) : launch_attend<__half, 128>(a, s);
+}
+
+int64_t sam_cache_attend_blocks_workspace_bytes(const sam_cache* c, int32_t B, int32_t Q, int32_t H, int32_t share) {
+    return share < 1 ? SAM_ERR_INVALID_ARG : sam_cache_attend_workspace_bytes(c, B, std::min(Q, share), H);
+}
+
+int sam_cache_attend_blocks(const sam_cache* c, int32_t layer, const void* q, int32_t dtype, int64_t q_row_stride, int64_t q_token_stride,
+                            int64_t q_head_stride, int32_t B, int32_t Q, int32_t H, const int32_t* streams, const int32_t* n_new,
+                            const int32_t* blocks, int32_t n_blocks, int32_t share, float scale, void* out, int64_t out_row_stride,
+                            int64_t out_token_stride, int64_t out_head_stride, float* lse, void* workspace, int64_t workspace_bytes, void* cuda_stream) {
+    if (int e = check_layer_call(c, layer, B, Q, streams)) return e;
+    if (n_blocks < 1 || !std::isfinite(scale) || (dtype != SAM_CACHE_BF16 && dtype != SAM_CACHE_FP16)) return SAM_ERR_INVALID_ARG;
+    const int64_t need = sam_cache_attend_blocks_workspace_bytes(c, B, Q, H, share);
+    if (need < 0) return static_cast<int>(need);
+    if (B == 0 || Q == 0) return SAM_OK;
+    if (!q || !out || !blocks || !aligned(q, 2) || !aligned(out, 2) || !aligned(lse, 4) || !aligned(blocks, 4) || !workspace || !aligned(workspace, 256))
+        return SAM_ERR_INVALID_ARG;
+    if (workspace_bytes < need) return SAM_ERR_TOO_SMALL;
+    if (static_cast<int64_t>(B) * Q * H >= (int64_t(1) << 31)) return SAM_ERR_TOO_LARGE;
+    AttendArgs a;
+    a.c = view(c);
+    a.q = q;
+    a.out = out;
+    a.lse = lse;
+    a.streams = streams;
+    a.n_new = n_new;
+    a.q_row = q_row_stride;
+    a.q_token = q_token_stride;
+    a.q_head = q_head_stride;
+    a.o_row = out_row_stride;
+    a.o_token = out_token_stride;
+    a.o_head = out_head_stride;
+    a.layer = layer;
+    a.B = B;
+    a.Q = Q;
+    a.H = H;
+    a.window = 0;
+    a.group = H / c->n_kv_heads;
+    a.scale = scale;
+    a.q_wide = aligned(q, 16) && (q_row_stride | q_token_stride | q_head_stride) % 8 == 0;
+    a.o_wide = aligned(out, 16) && (out_row_stride | out_token_stride | out_head_stride) % 8 == 0;
+    a.counters = static_cast<int32_t*>(workspace);
+    a.partials = reinterpret_cast<float*>(static_cast<char*>(workspace) + kCounterBytes);
+    a.blocks = blocks;
+    a.share = std::min(share, Q);
+    a.lists = (Q - 1) / a.share + 1;
+    a.runs = B * a.lists;
+    a.n_blocks = n_blocks;
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    const bool bf16 = dtype == SAM_CACHE_BF16;
+    if (c->head_dim == 64) return bf16 ? launch_attend_blocks<__nv_bfloat16, 64>(a, s) : launch_attend_blocks<__half, 64>(a, s);
+    return bf16 ? launch_attend_blocks<__nv_bfloat16, 128>(a, s) : launch_attend_blocks<__half, 128>(a, s);
+}
+
+int sam_rope_turns(const double* inv_freq, int32_t n, uint64_t* turns) {
+    if (n < 1 || n > 64 || !inv_freq || !turns) return SAM_ERR_INVALID_ARG;
+    for (int32_t i = 0; i < n; ++i) {
+        if (!std::isfinite(inv_freq[i]) || std::fabs(inv_freq[i]) > 1e6) return SAM_ERR_INVALID_ARG;
+        const long double x = static_cast<long double>(inv_freq[i]) / 6.283185307179586476925286766559L;
+        const long double part = x - floorl(x);                      // of a turn, 0 .. 1
+        turns[i] = part >= 1.0L ? 0 : static_cast<uint64_t>(part * 18446744073709551616.0L);
+    }
+    return SAM_OK;
+}
+
+int sam_cache_append_rotated(const sam_cache* c, int32_t layer, const void* q, int64_t q_row_stride, int64_t q_token_stride, int64_t q_head_stride,
+                             const void* k, const void* v, int64_t row_stride, int64_t token_stride, int64_t head_stride, void* q_out,
+                             int64_t out_row_stride, int64_t out_token_stride, int64_t out_head_stride, int32_t dtype, const sam_rope* rope, int32_t B,
+                             int32_t Q, int32_t H, const int32_t* streams, const int32_t* n_new, const int32_t* positions, void* cuda_stream) {
+    if (int e = check_layer_call(c, layer, B, Q, streams)) return e;
+    if (dtype != SAM_CACHE_BF16 && dtype != SAM_CACHE_FP16) return SAM_ERR_INVALID_ARG;
+    if (!rope || !rope->turns || !aligned(rope->turns, 8) || rope->rotary_dim < 32 || rope->rotary_dim > c->head_dim || rope->rotary_dim % 32 ||
+        !std::isfinite(rope->factor) || H < 0)
+        return SAM_ERR_INVALID_ARG;
+    if (H > 16384 || static_cast<int64_t>(Q) * B >= (int64_t(1) << 31)) return SAM_ERR_TOO_LARGE;
+    if (B == 0 || Q == 0) return SAM_OK;
+    if (!k || !v || !aligned(k, 2) || !aligned(v, 2) || (H > 0 && (!q || !q_out || !aligned(q, 2) || !aligned(q_out, 2))) || !aligned(positions, 4))
+        return SAM_ERR_INVALID_ARG;
+    DeviceInfo di;
+    if (int e = device_info(&di)) return e;
+    TurnArgs a;
+    a.c = view(c);
+    a.q = q;
+    a.k = k;
+    a.v = v;
+    a.q_out = q_out;
+    a.qs = KvStrides{q_row_stride, q_token_stride, q_head_stride};
+    a.ks = KvStrides{row_stride, token_stride, head_stride};
+    a.os = KvStrides{out_row_stride, out_token_stride, out_head_stride};
+    a.turns = rope->turns;
+    a.positions = positions;
+    a.streams = streams;
+    a.n_new = n_new;
+    a.factor = rope->factor;
+    a.layer = layer;
+    a.B = B;
+    a.Q = Q;
+    a.H = H;
+    a.rotary = rope->rotary_dim;
+    a.interleaved = rope->interleaved != 0;
+    // more tokens share a CTA once there are enough CTAs; unit numbers stay below 2^16, where the multiplier divides exactly
+    const int32_t heads = H + 2 * c->n_kv_heads;
+    a.tokens = static_cast<int32_t>(std::min<int64_t>({int64_t(kTurnTokens), std::max<int64_t>(1, static_cast<int64_t>(B) * Q / (di.sms * 4)), 65535 / heads}));
+    a.magic = static_cast<uint32_t>(((int64_t(1) << 32) + heads - 1) / heads);
+    auto wide = [](const void* p, const KvStrides& t) { return aligned(p, 16) && (t.row | t.token | t.head) % 8 == 0; };
+    a.q_wide = wide(q, a.qs);
+    a.k_wide = wide(k, a.ks) && aligned(v, 16);
+    a.o_wide = wide(q_out, a.os);
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    return dtype == SAM_CACHE_BF16 ? launch_turn<__nv_bfloat16>(a, s) : launch_turn<__half>(a, s);
+}
+
+int sam_cache_bounds_update(const sam_cache* c, int32_t layer, int8_t* codes, int8_t* exps, int32_t B, int32_t Q, const int32_t* streams,
+                            const int32_t* n_new, void* cuda_stream) {
+    if (int e = check_layer_call(c, layer, B, Q, streams)) return e;
+    if (int e = check_bounds(codes, exps)) return e;
+    if (B == 0 || Q == 0) return SAM_OK;
+    const CacheView v = view(c);
+    const unsigned pages = static_cast<unsigned>(std::min<int64_t>(Q / c->page_tokens + 1, 1024));
+    bounds_update_kernel<<<dim3(c->n_kv_heads, B, pages), kBoundThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(v, BoundsView{codes, exps}, layer, Q, streams, n_new);
+    return launched();
+}
+
+int sam_cache_bounds_rebuild(const sam_cache* c, int8_t* codes, int8_t* exps, int32_t n, const int32_t* pages, void* cuda_stream) {
+    if (int e = check_cache(c)) return e;
+    if (int e = check_pages(c)) return e;
+    if (int e = check_bounds(codes, exps)) return e;
+    if (n < 0 || (!pages && n > c->n_pages)) return SAM_ERR_INVALID_ARG;
+    if (n == 0) return SAM_OK;
+    DeviceInfo di;
+    if (int e = device_info(&di)) return e;
+    const int64_t all = static_cast<int64_t>(n) * c->n_layers * c->n_kv_heads;
+    bounds_rebuild_kernel<<<static_cast<unsigned>(std::min<int64_t>(all, di.sms * 16)), kBoundThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(
+        view(c), BoundsView{codes, exps}, n, pages);
+    return launched();
+}
+
+int64_t sam_cache_select_workspace_bytes(const sam_cache* c, int32_t B, int32_t Q, int32_t share) {
+    if (int e = check_cache(c)) return e;
+    if (B < 0 || Q < 0 || share < 1) return SAM_ERR_INVALID_ARG;
+    if (B > SAM_CACHE_MAX_B || Q > kLargest) return SAM_ERR_TOO_LARGE;
+    const int64_t each = static_cast<int64_t>(c->n_kv_heads) * c->max_pages * 4, runs = B * ((static_cast<int64_t>(Q) + share - 1) / share);
+    return std::max<int64_t>(std::min(runs * each, kKeyBytes), each);
+}
+
+int sam_cache_select(const sam_cache* c, int32_t layer, const int8_t* codes, const int8_t* exps, const void* q, int32_t dtype, int64_t q_row_stride,
+                     int64_t q_token_stride, int64_t q_head_stride, int32_t B, int32_t Q, int32_t H, const int32_t* streams, const int32_t* n_new,
+                     int32_t share, int32_t n_sink, int32_t n_recent, int32_t* blocks, int32_t n_blocks, void* workspace, int64_t workspace_bytes,
+                     void* cuda_stream) {
+    if (int e = check_layer_call(c, layer, B, Q, streams)) return e;
+    if (int e = check_bounds(codes, exps)) return e;
+    if ((dtype != SAM_CACHE_BF16 && dtype != SAM_CACHE_FP16) || H < 1 || H % c->n_kv_heads || share < 1 || n_sink < 0 || n_recent < 1 || n_blocks < 1)
+        return SAM_ERR_INVALID_ARG;
+    if (B == 0 || Q == 0) return SAM_OK;
+    share = std::min(share, Q);
+    // what is listed whatever its score has to fit: a run of `share` tokens lies in up to (share - 2) / page_tokens + 2 blocks
+    const int64_t own = share == 1 ? 1 : (static_cast<int64_t>(share) - 2) / c->page_tokens + 2;
+    if (static_cast<int64_t>(n_sink) + n_recent - 1 + own > n_blocks) return SAM_ERR_INVALID_ARG;
+    const int64_t need = sam_cache_select_workspace_bytes(c, B, Q, share), lists = (static_cast<int64_t>(Q) - 1) / share + 1;
+    if (!q || !aligned(q, 2) || !blocks || !aligned(blocks, 4) || !workspace || !aligned(workspace, 256)) return SAM_ERR_INVALID_ARG;
+    if (workspace_bytes < need) return SAM_ERR_TOO_SMALL;
+    if (static_cast<int64_t>(B) * Q * H >= (int64_t(1) << 31)) return SAM_ERR_TOO_LARGE;
+    SelectArgs a;
+    a.c = view(c);
+    a.o = BoundsView{const_cast<int8_t*>(codes), const_cast<int8_t*>(exps)};
+    a.q = q;
+    a.streams = streams;
+    a.n_new = n_new;
+    a.q_row = q_row_stride;
+    a.q_token = q_token_stride;
+    a.q_head = q_head_stride;
+    a.layer = layer;
+    a.B = B;
+    a.Q = Q;
+    a.H = H;
+    a.group = H / c->n_kv_heads;
+    a.lists = static_cast<int32_t>(lists);
+    a.share = share;
+    a.n_blocks = n_blocks;
+    a.n_sink = n_sink;
+    a.n_recent = n_recent;
+    a.keys = static_cast<uint32_t*>(workspace);
+    a.out = blocks;
+    a.q_wide = aligned(q, 16) && (q_row_stride | q_token_stride | q_head_stride) % 8 == 0;
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    return dtype == SAM_CACHE_BF16 ? launch_select<__nv_bfloat16>(a, workspace_bytes, s) : launch_select<__half>(a, workspace_bytes, s);
 }
 
 }  // extern "C"

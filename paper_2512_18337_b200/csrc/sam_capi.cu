@@ -16,6 +16,7 @@
 #include "sam_kernels.cuh"
 #include "argmax_bulk.cuh"
 #include "sam_update.cuh"
+#include "shape.cuh"
 
 using namespace samb200;
 
@@ -903,6 +904,101 @@ int sam_step_from_keys(const sam_index* idx, int64_t* keys, int32_t B, int32_t K
                         reinterpret_cast<unsigned long long*>(keys), state, matched_len, min_match, next_drafts,
                         next_n_draft, nullptr, nullptr, 0u, nullptr};
     return launch_accept<kTailFullWalk>(idx->dev, aa, static_cast<cudaStream_t>(cuda_stream), false);
+}
+
+int sam_verify_from_keys(int64_t* keys, int32_t B, int32_t K, const int32_t* drafts, const int32_t* n_draft, int32_t* argmax_out,
+                         int32_t* accepted, int32_t* n_accepted, float* values, void* cuda_stream) {
+    if (B < 0 || K < 1 || K > SAM_K_MAX) return SAM_ERR_INVALID_ARG;
+    if (B == 0) return SAM_OK;
+    if (!keys || !aligned(keys, 8) || !drafts || !n_draft || !argmax_out || !accepted || !n_accepted || !aligned(values, 4)) return SAM_ERR_INVALID_ARG;
+    AcceptArgs aa{nullptr, 0, B, K, drafts, n_draft, argmax_out, accepted, n_accepted, reinterpret_cast<unsigned long long*>(keys)};
+    aa.values = values;
+    return launch_accept<kTailVerifyOnly>(DeviceSam{}, aa, static_cast<cudaStream_t>(cuda_stream), false);
+}
+
+namespace {
+
+int64_t shape_words(int32_t V) { return (static_cast<int64_t>(V) + 31) / 32; }
+
+int check_shape(const sam_shape* s, int32_t B) {
+    if (!s || s->max_bias < 0 || s->n_masks < 0 || s->n_streams < 0) return SAM_ERR_INVALID_ARG;
+    if (!aligned(s->counts, 4) || !aligned(s->seen, 4) || !aligned(s->masks, 4)) return SAM_ERR_INVALID_ARG;
+    if (!s->counts != !s->seen || (s->counts && s->n_streams < 1)) return SAM_ERR_INVALID_ARG;
+    if (s->max_bias > 0 && (!s->bias_tokens || !s->bias_values)) return SAM_ERR_INVALID_ARG;
+    if (!s->masks != !s->mask_of || (s->masks && s->n_masks < 1)) return SAM_ERR_INVALID_ARG;
+    (void)B;
+    return SAM_OK;
+}
+
+}  // namespace
+
+int sam_argmax_shaped(const void* logits_bf16, int64_t row_stride_elems, int32_t B, int32_t K, int32_t V, const int32_t* drafts,
+                      const int32_t* streams, const sam_shape* shape, int64_t* keys, void* cuda_stream) {
+    if (B < 0 || K < 1 || K > SAM_K_MAX || V < 1 || row_stride_elems < V || V > (1 << 30)) return SAM_ERR_INVALID_ARG;
+    if (int e = check_shape(shape, B)) return e;
+    if (B == 0) return SAM_OK;
+    if (!logits_bf16 || !keys || !drafts || !aligned(logits_bf16, 2) || !aligned(keys, 8)) return SAM_ERR_INVALID_ARG;
+    if (!streams && shape->counts && B > shape->n_streams) return SAM_ERR_INVALID_ARG;
+    DeviceInfo di;
+    if (int e = device_info(&di)) return e;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    const int64_t R = static_cast<int64_t>(B) * (K + 1);
+    SAM_CUDA(cudaMemsetAsync(keys, 0, static_cast<size_t>(R) * 8, st));
+    ShapeArgs a{};
+    a.logits = static_cast<const __nv_bfloat16*>(logits_bf16);
+    a.stride = row_stride_elems;
+    a.drafts = drafts;
+    a.streams = streams;
+    a.counts = shape->counts;
+    a.seen = shape->seen;
+    a.repetition = shape->repetition;
+    a.presence = shape->presence;
+    a.frequency = shape->frequency;
+    a.bias_tokens = shape->bias_tokens;
+    a.bias_values = shape->bias_values;
+    a.n_bias = shape->n_bias;
+    a.masks = shape->masks;
+    a.mask_of = shape->mask_of;
+    a.keys = reinterpret_cast<unsigned long long*>(keys);
+    a.B = B;
+    a.K = K;
+    a.V = V;
+    a.words = static_cast<int32_t>(shape_words(V));
+    a.n_streams = shape->n_streams;
+    a.max_bias = shape->max_bias;
+    a.n_masks = shape->n_masks;
+    a.tiles_per_row = static_cast<int32_t>((static_cast<int64_t>(V) + 7 + kShapeTile - 1) / kShapeTile);
+    const int64_t grid = std::min<int64_t>(R * a.tiles_per_row, static_cast<int64_t>(di.sms) * kShapeCtasPerSm);
+    argmax_shaped_kernel<<<static_cast<unsigned>(grid), kShapeThreads, 0, st>>>(a);
+    SAM_CUDA(cudaGetLastError());
+    ++g_launches;
+    return SAM_OK;
+}
+
+int sam_history_add(int32_t* counts, uint32_t* seen, int32_t n_streams, int32_t V, int32_t B, const int32_t* streams, const int32_t* tokens,
+                    int32_t ld, const int32_t* n, int32_t told, void* cuda_stream) {
+    if (n_streams < 1 || V < 1 || V > (1 << 30) || B < 0 || ld < 0 || !counts || !seen || !aligned(counts, 4) || !aligned(seen, 4)) return SAM_ERR_INVALID_ARG;
+    if (B > 65535) return SAM_ERR_TOO_LARGE;
+    if (B == 0 || ld == 0) return SAM_OK;
+    if (!tokens || (!streams && B > n_streams)) return SAM_ERR_INVALID_ARG;
+    const unsigned blocks = static_cast<unsigned>(std::min<int64_t>((static_cast<int64_t>(ld) + 255) / 256, 1024));
+    history_add_kernel<<<dim3(blocks, B), 256, 0, static_cast<cudaStream_t>(cuda_stream)>>>(counts, seen, n_streams, V, static_cast<int>(shape_words(V)), B, streams,
+                                                                                             tokens, ld, n, told != 0);
+    SAM_CUDA(cudaGetLastError());
+    ++g_launches;
+    return SAM_OK;
+}
+
+int sam_history_copy(int32_t* counts, uint32_t* seen, int32_t n_streams, int32_t V, int32_t n, const int32_t* src, const int32_t* dst, void* cuda_stream) {
+    if (n_streams < 1 || V < 1 || V > (1 << 30) || n < 0 || !counts || !seen || !aligned(counts, 4) || !aligned(seen, 4)) return SAM_ERR_INVALID_ARG;
+    if (n > 65535) return SAM_ERR_TOO_LARGE;
+    if (n == 0) return SAM_OK;
+    if (n > n_streams || !dst) return SAM_ERR_INVALID_ARG;
+    const unsigned blocks = static_cast<unsigned>(std::min<int64_t>((static_cast<int64_t>(V) + 255) / 256, 128));
+    history_copy_kernel<<<dim3(blocks, n), 256, 0, static_cast<cudaStream_t>(cuda_stream)>>>(counts, seen, n_streams, V, static_cast<int>(shape_words(V)), src, dst);
+    SAM_CUDA(cudaGetLastError());
+    ++g_launches;
+    return SAM_OK;
 }
 
 int64_t sam_set_bytes(int32_t n_members) {

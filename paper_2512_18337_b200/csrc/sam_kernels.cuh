@@ -308,6 +308,15 @@ __device__ __forceinline__ unsigned long long pack_candidate(float x, unsigned i
     return (static_cast<unsigned long long>(ordered_key(x)) << 32) | (0xFFFFFFFFu - idx);
 }
 
+// The value behind a packed candidate: its key is that of a bf16 (below 2^16) or of a float (above); 0 and 1 are no values.
+__device__ __forceinline__ float packed_value(unsigned long long k) {
+    const unsigned key = static_cast<unsigned>(k >> 32);
+    if (key == 0xFFFFu) return __int_as_float(0x7FFFFFFF);
+    if (key <= 1u) return __int_as_float(0xFF800000);
+    if (key < 0x10000u) return __uint_as_float((key & 0x8000u ? key & 0x7FFFu : ~key & 0xFFFFu) << 16);
+    return __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key);
+}
+
 // A row whose element 0 is NaN keeps index 0 (nothing ever compares greater than NaN): this
 // candidate beats every real one (value keys stop at 0xFF80) and decodes to index 0.
 constexpr unsigned long long kCandidateFirstIsNaN = 0x0000FFFFFFFFFFFFull;
@@ -587,6 +596,7 @@ struct AcceptArgs {
     unsigned long long* counters;   // [6] running statistics, or nullptr
     int* next_list;           // row list of the NEXT step (rows 0..next_n_draft[b] of every stream, any order), or nullptr
     int* list_meta;           // its meta words (see RowMap)
+    float* values;            // [B*(K+1)] logit of every row's choice, or nullptr
     int* acc_epoch;           // [B] number of the launch in which the stream's accept step last ran inside the argmax kernel, or nullptr
 };
 
@@ -644,6 +654,7 @@ __device__ __forceinline__ void accept_stream(const DeviceSam& sam, const Accept
             if ((p.flags & kSkipUnusedRows) && j > nd) idx = -1;        // the row was not looked at
             am[h] = idx;
             p.argmax_out[row0 + j] = idx;
+            if (p.values != nullptr) p.values[row0 + j] = packed_value(k);
         }
     }
 
