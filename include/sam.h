@@ -705,8 +705,9 @@ typedef struct sam_shape {
     const int32_t*  n_bias;        /* [B], clamped to 0 .. max_bias; NULL: max_bias */
     const uint32_t* masks;         /* [n_masks, ceil(V / 32)]: a set bit allows the token */
     const int32_t*  mask_of;       /* [B, K + 1]: mask of each row; none for ids outside 0 .. n_masks - 1 */
-    int32_t n_streams, max_bias, n_masks;
+    int32_t n_streams, max_bias, n_masks;   /* max_bias <= SAM_MAX_BIAS */
 } sam_shape;
+#define SAM_MAX_BIAS 512
 
 /* logits, row_stride_elems, B, K, V, drafts: as in sam_verify (ids of drafts outside 0 .. V - 1 are passed over).  streams: device [B], or NULL
  * for row b = stream b; an unknown stream has said nothing.  keys: device int64 [B * (K + 1)], 8-byte aligned, overwritten.

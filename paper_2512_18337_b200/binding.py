@@ -20,6 +20,7 @@ _lib = None
 SAM_K_MAX = 32
 SAM_MAX_SEPARATORS = 16
 SAM_STATIC_MAX_ROWS = 16384
+SAM_MAX_BIAS = 512
 
 _vp, _i32, _i64 = C.c_void_p, C.c_int32, C.c_int64
 

@@ -632,6 +632,33 @@ int sync_updates(sam_index* idx, cudaStream_t st, const Renorm* rn, int64_t* tok
     return SAM_OK;
 }
 
+template <bool kMasks>
+int launch_shaped(const ShapeArgs& a, unsigned grid, cudaStream_t st) {
+    static thread_local uint64_t asked = 0;               // one bit per device
+    int dev = 0;
+    SAM_CUDA(cudaGetDevice(&dev));
+    const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
+    if (!(asked & bit)) {
+        SAM_CUDA(cudaFuncSetAttribute(argmax_shaped_kernel<kMasks>, cudaFuncAttributeMaxDynamicSharedMemorySize, shape_smem(kMasks)));
+        asked |= bit;
+    }
+    argmax_shaped_kernel<kMasks><<<grid, kShapeThreads, shape_smem(kMasks), st>>>(a);
+    SAM_CUDA(cudaGetLastError());
+    ++g_launches;
+    return SAM_OK;
+}
+
+int64_t shape_words(int32_t V) { return (static_cast<int64_t>(V) + 31) / 32; }
+
+int check_shape(const sam_shape* s) {
+    if (!s || s->max_bias < 0 || s->n_masks < 0 || s->n_streams < 0) return SAM_ERR_INVALID_ARG;
+    if (!aligned(s->counts, 4) || !aligned(s->seen, 4) || !aligned(s->masks, 4)) return SAM_ERR_INVALID_ARG;
+    if (!s->counts != !s->seen || (s->counts && s->n_streams < 1)) return SAM_ERR_INVALID_ARG;
+    if (s->max_bias > 0 && (!s->bias_tokens || !s->bias_values)) return SAM_ERR_INVALID_ARG;
+    if (!s->masks != !s->mask_of || (s->masks && s->n_masks < 1)) return SAM_ERR_INVALID_ARG;
+    return SAM_OK;
+}
+
 }  // namespace
 
 struct sam_set {
@@ -916,26 +943,11 @@ int sam_verify_from_keys(int64_t* keys, int32_t B, int32_t K, const int32_t* dra
     return launch_accept<kTailVerifyOnly>(DeviceSam{}, aa, static_cast<cudaStream_t>(cuda_stream), false);
 }
 
-namespace {
-
-int64_t shape_words(int32_t V) { return (static_cast<int64_t>(V) + 31) / 32; }
-
-int check_shape(const sam_shape* s, int32_t B) {
-    if (!s || s->max_bias < 0 || s->n_masks < 0 || s->n_streams < 0) return SAM_ERR_INVALID_ARG;
-    if (!aligned(s->counts, 4) || !aligned(s->seen, 4) || !aligned(s->masks, 4)) return SAM_ERR_INVALID_ARG;
-    if (!s->counts != !s->seen || (s->counts && s->n_streams < 1)) return SAM_ERR_INVALID_ARG;
-    if (s->max_bias > 0 && (!s->bias_tokens || !s->bias_values)) return SAM_ERR_INVALID_ARG;
-    if (!s->masks != !s->mask_of || (s->masks && s->n_masks < 1)) return SAM_ERR_INVALID_ARG;
-    (void)B;
-    return SAM_OK;
-}
-
-}  // namespace
-
 int sam_argmax_shaped(const void* logits_bf16, int64_t row_stride_elems, int32_t B, int32_t K, int32_t V, const int32_t* drafts,
                       const int32_t* streams, const sam_shape* shape, int64_t* keys, void* cuda_stream) {
     if (B < 0 || K < 1 || K > SAM_K_MAX || V < 1 || row_stride_elems < V || V > (1 << 30)) return SAM_ERR_INVALID_ARG;
-    if (int e = check_shape(shape, B)) return e;
+    if (int e = check_shape(shape)) return e;
+    if (shape->max_bias > SAM_MAX_BIAS) return SAM_ERR_TOO_LARGE;
     if (B == 0) return SAM_OK;
     if (!logits_bf16 || !keys || !drafts || !aligned(logits_bf16, 2) || !aligned(keys, 8)) return SAM_ERR_INVALID_ARG;
     if (!streams && shape->counts && B > shape->n_streams) return SAM_ERR_INVALID_ARG;
@@ -969,10 +981,7 @@ int sam_argmax_shaped(const void* logits_bf16, int64_t row_stride_elems, int32_t
     a.n_masks = shape->n_masks;
     a.tiles_per_row = static_cast<int32_t>((static_cast<int64_t>(V) + 7 + kShapeTile - 1) / kShapeTile);
     const int64_t grid = std::min<int64_t>(R * a.tiles_per_row, static_cast<int64_t>(di.sms) * kShapeCtasPerSm);
-    argmax_shaped_kernel<<<static_cast<unsigned>(grid), kShapeThreads, 0, st>>>(a);
-    SAM_CUDA(cudaGetLastError());
-    ++g_launches;
-    return SAM_OK;
+    return a.masks ? launch_shaped<true>(a, static_cast<unsigned>(grid), st) : launch_shaped<false>(a, static_cast<unsigned>(grid), st);
 }
 
 int sam_history_add(int32_t* counts, uint32_t* seen, int32_t n_streams, int32_t V, int32_t B, const int32_t* streams, const int32_t* tokens,

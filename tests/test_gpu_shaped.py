@@ -146,7 +146,7 @@ def test_vocabularies(V):
 
 
 @pytest.mark.parametrize("penalties", [None, "usual", "any"])
-@pytest.mark.parametrize("n_bias", [0, 1, 300])
+@pytest.mark.parametrize("n_bias", [0, 1, 300, 512])
 @pytest.mark.parametrize("masks", [0, 5])
 def test_everything(penalties, n_bias, masks):
     Case(np.random.default_rng(n_bias + masks), 5, 8, 3001, said=200, penalties=penalties, n_bias=n_bias, masks=masks).check()

@@ -151,7 +151,7 @@ def test_shaped_verification_refuses():
                  dict(masks=4), dict(mask_of=4), dict(masks=4, mask_of=4), dict(masks=2, mask_of=4, n_masks=1)):
         assert call(**over) == -1, over
     assert lib.sam_argmax_shaped(16, 100, 2, 3, 100, 16, None, None, 8, None) == -1
-    assert call(B=0) == 0
+    assert call(B=0) == 0 and call(max_bias=513, bias_tokens=4, bias_values=4) == -6
 
     def verify(keys=8, B=1, K=3, drafts=4, n_draft=4, argmax=4, accepted=4, n_accepted=4, values=None):
         return lib.sam_verify_from_keys(keys, B, K, drafts, n_draft, argmax, accepted, n_accepted, values, None)
