@@ -133,24 +133,33 @@ struct WideSegment {
     int b, rt, head, steps;
     int rows;            // query rows of the tile
     int first_pos, last_pos;
+    int end;             // listed: first position that none of them sees
     int64_t begin;       // number of its first unit
 };
+template <bool kListed>
 __device__ __forceinline__ void wide_tile(const AttendArgs& a, int tiles, int64_t e, WideSegment& g) {   // e = b * tiles + rt
     g.b = static_cast<int>(quotient(e, tiles));
     g.rt = static_cast<int>(e - static_cast<int64_t>(g.b) * tiles);
-    g.ri = row_info<kWideUnit>(a, g.b);
+    g.ri = row_info<kWideUnit, kListed>(a, g.b);
     g.rows = min(g.ri.n * a.group - g.rt * kWideRows, kWideRows);
     g.steps = 0;
     if (g.rows <= 0) return;
     const int i0 = g.rt * kWideRows / a.group, i1 = (g.rt * kWideRows + g.rows - 1) / a.group, cap = a.c.capacity();
     g.first_pos = g.ri.len + i0;
     g.last_pos = g.ri.len + i1;
-    g.ri.hi = static_cast<int>(min(static_cast<int64_t>(g.ri.len) + i1 + 1, static_cast<int64_t>(cap)));
+    g.end = static_cast<int>(min(static_cast<int64_t>(g.ri.len) + i1 + 1, static_cast<int64_t>(cap)));
+    if constexpr (kListed) {
+        g.steps = (g.ri.hi + kWideUnit - 1) / kWideUnit;
+        return;
+    }
+    g.ri.hi = g.end;
     g.ri.lo = a.window > 0 ? min(max(g.first_pos - a.window + 1, 0), cap - 1) & ~(kWideUnit - 1) : 0;
     g.steps = max((g.ri.hi - g.ri.lo + kWideUnit - 1) / kWideUnit, 1);
 }
 
-template <typename T, int D>
+// kListed: over listed blocks.  The tokens of a segment are then the places of its list; the expanding warps say where the tiles of a
+// step really begin, and whether every row sees all of them.
+template <typename T, int D, bool kListed>
 __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __grid_constant__ AttendArgs a) {
     using Plan = WidePlan<D>;
     extern __shared__ uint8_t smem_raw[];
@@ -160,6 +169,9 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
     __shared__ alignas(4) uint8_t tile_there[4][4];    // per step (mod 4) and expanding warp: which of its two tiles are there
     __shared__ alignas(4) uint8_t nan_flag[4][4];      // NaN among the values of the warp's tokens (written where there are masks)
     __shared__ uint8_t nan_block[4][128];              // which 16-channel blocks of a token's values are NaN
+    __shared__ alignas(4) uint8_t tile_all[4][4];      // listed: every row sees all of the warp's two tiles
+    __shared__ int tile_begin[kListed ? 4 : 1][8];     // listed: positions of the first tokens of the step's tiles
+    __shared__ int2 slot_begin[kListed ? 16 : 1][Plan::kRawSlots];   // listed: of the tiles in an expanding warp's slots
     __shared__ float shared_row[2][128];               // what the two threads of a query row tell each other
     __shared__ int last_here;
     __shared__ volatile int abort_flag;
@@ -204,8 +216,8 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
     barrier_init_fence();
 
     // ---- how many units there are, and where our share begins
-    const int tiles = static_cast<int>((static_cast<int64_t>(a.Q) * a.group + kWideRows - 1) / kWideRows);
-    const int64_t n_tiles = static_cast<int64_t>(a.B) * tiles;
+    const int tiles = static_cast<int>((static_cast<int64_t>(a.share) * a.group + kWideRows - 1) / kWideRows);
+    const int64_t n_tiles = static_cast<int64_t>(a.runs) * tiles;
     auto block_sum = [&](int64_t x, int64_t* before) -> int64_t {
         int64_t y = x;
 #pragma unroll
@@ -227,7 +239,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
     auto units_of = [&](int64_t e) -> int64_t {
         if (e >= n_tiles) return 0;
         WideSegment g;
-        wide_tile(a, tiles, e, g);
+        wide_tile<kListed>(a, tiles, e, g);
         return static_cast<int64_t>(g.steps) * c.n_kv;
     };
     int64_t units = 0, mine = 0, before = 0;
@@ -267,7 +279,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
     auto for_pieces = [&](auto f) {
         WideSegment g;
         int64_t e = start_e;
-        wide_tile(a, tiles, e, g);
+        wide_tile<kListed>(a, tiles, e, g);
         const int64_t rel = u0 - start_begin;
         g.head = static_cast<int>(quotient(rel, g.steps));
         g.begin = start_begin + static_cast<int64_t>(g.head) * g.steps;
@@ -282,7 +294,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
             if (++g.head == c.n_kv) {
                 g.head = 0;
                 const int64_t next = g.begin;
-                do wide_tile(a, tiles, ++e, g);
+                do wide_tile<kListed>(a, tiles, ++e, g);
                 while (g.steps == 0 && e + 1 < n_tiles);
                 g.begin = next;
             }
@@ -323,10 +335,11 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
         for_pieces([&](const WideSegment& seg, int s0, int count) {
             // ---- queries into tensor memory
             const bool mine = row < seg.rows;
-            const int rho = seg.rt * kWideRows + row, qi = rho / a.group, qh = seg.head * a.group + rho % a.group;
+            const RunPlace place = run_place<kListed>(a, seg.b);
+            const int rho = seg.rt * kWideRows + row, qi = place.i0 + rho / a.group, qh = seg.head * a.group + rho % a.group;
             float factor;
             {
-                const T* q = static_cast<const T*>(a.q) + seg.b * a.q_row + static_cast<int64_t>(qi) * a.q_token + static_cast<int64_t>(qh) * a.q_head;
+                const T* q = static_cast<const T*>(a.q) + place.b * a.q_row + static_cast<int64_t>(qi) * a.q_token + static_cast<int64_t>(qh) * a.q_head;
                 constexpr int kHalf = D / 2;            // channels of a thread; the size of the row is taken over all of them
                 uint32_t x[kHalf / 2];
                 auto load8 = [&](int d, uint32_t (&w)[4]) {
@@ -369,7 +382,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                 if (lane == 0) barrier_arrive(query_bar);
                 __syncwarp();
             }
-            const int pos = mine ? seg.ri.len + qi : -1;
+            const int pos = mine ? seg.ri.len + rho / a.group : -1;
             const bool idle = !__any_sync(0xffffffffu, mine);
             float m = -INFINITY, l = 0.f;
             uint32_t nan_blocks = 0;
@@ -392,7 +405,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                 const int t0 = base + k * kWideUnit, ring = n & 3;
                 uint32_t on = *reinterpret_cast<volatile uint32_t*>(tile_there[ring]);
                 on = (on * 0x01041040u) >> 24;            // two bits of each byte, side by side
-                const bool all = t0 <= until && t0 > after;
+                const bool all = kListed ? *reinterpret_cast<volatile uint32_t*>(tile_all[ring]) == 0x01010101u : t0 <= until && t0 > after;
                 // Weights with the reference at hand, in one pass: a sum of at most kTotalMax means that each of them is within fp16.
                 // Where that fails, and where there are masks or absent tiles, the step is done in two passes, the largest score first.
                 bool done = idle;                        // a quarter without query rows hands nothing over: its sums are nobody's
@@ -434,13 +447,23 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                 if (!done) {
                     if (!all && *reinterpret_cast<volatile uint32_t*>(nan_flag[ring])) {
                         for (int t = 0; t < kWideUnit; ++t)
-                            if (static_cast<volatile uint8_t*>(nan_flag[ring])[t >> 5] && t0 + t <= pos && (a.window == 0 || t0 + t > pos - a.window))
+                            if (static_cast<volatile uint8_t*>(nan_flag[ring])[t >> 5] &&
+                                (kListed ? static_cast<volatile int*>(tile_begin[kListed ? ring : 0])[t >> 4] + (t & 15) <= pos : t0 + t <= pos && (a.window == 0 || t0 + t > pos - a.window)))
                                 nan_blocks |= static_cast<volatile uint8_t*>(nan_block[ring])[t];
                         __syncwarp();
                     }
                     // which of 32 columns a row sees, as bits; q: 0 .. 3 over the step
                     const int from = a.window > 0 ? max(pos - a.window + 1 - t0, 0) : 0, to_col = min(pos - t0, kWideUnit - 1);
                     auto seen = [&](int q) -> uint32_t {
+                        if constexpr (kListed) {
+                            uint32_t bits = 0;
+#pragma unroll
+                            for (int x = 0; x < 2; ++x) {
+                                const int last = min(pos - static_cast<volatile int*>(tile_begin[ring])[2 * q + x], 15);   // of the tile's tokens
+                                if (last >= 0 && ((on >> (2 * q + x)) & 1)) bits |= ((2u << last) - 1) << (16 * x);
+                            }
+                            return bits;
+                        }
                         const int lo = max(from - q * 32, 0), hi = to_col - q * 32;
                         uint32_t bits = hi < 0 || lo > 31 ? 0u : (0xffffffffu >> (31 - min(hi, 31))) & (0xffffffffu << lo);
                         if (!((on >> (2 * q)) & 1)) bits &= 0xffff0000u;
@@ -517,8 +540,8 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                 const float f = finish_factor(l_all, c.v_exp);
 #pragma unroll
                 for (int i = 0; i < 32; ++i) y[i] = l_all == 0.f ? 0.f : y[i] * f;
-                store_row<T>(static_cast<T*>(a.out) + seg.b * a.o_row + static_cast<int64_t>(qi) * a.o_token + static_cast<int64_t>(qh) * a.o_head + col, y, a.o_wide);
-                if (a.lse && col == 0) a.lse[(static_cast<int64_t>(seg.b) * a.Q + qi) * a.H + qh] = finish_lse(m_all, l_all);
+                store_row<T>(static_cast<T*>(a.out) + place.b * a.o_row + static_cast<int64_t>(qi) * a.o_token + static_cast<int64_t>(qh) * a.o_head + col, y, a.o_wide);
+                if (a.lse && col == 0) a.lse[(static_cast<int64_t>(place.b) * a.Q + qi) * a.H + qh] = finish_lse(m_all, l_all);
             };
             if (begins && ends) {
 #pragma unroll 1
@@ -627,7 +650,9 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
         uint32_t n = 0;                                    // steps in earlier pieces
         for_pieces([&](const WideSegment& g, int s0, int count) {
             const uint8_t* const head = c.head_tiles(0, a.layer, g.head) + (values ? 8 * D : 0) + lane * 16;
-            const int until = all_until(g), after = all_after(g), base = g.ri.lo + s0 * kWideUnit, hi_token = g.ri.hi;
+            const int until = all_until(g), after = all_after(g), base = g.ri.lo + s0 * kWideUnit, hi_token = kListed ? g.end : g.ri.hi;
+            const int32_t* const list = kListed ? a.blocks + (static_cast<int64_t>(g.b) * c.n_kv + g.head) * a.n_blocks : nullptr;
+            int begin_of = 0;                              // listed: positions of the first tokens of those tiles
             const int tile0 = (g.ri.lo >> 4) + w * 2;      // number of the warp's first tile of step 0
             int page_base = -16, page_of = -1;              // pages of the warp's tiles of sixteen steps: lane = 2 * (step - page_base) + tile
             const int first = (n ^ stage) & 1;             // our first step of the piece
@@ -637,7 +662,16 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                     if (step - page_base >= 16) {
                         page_base = step;
                         const int t = g.ri.lo + (step + (lane >> 1)) * kWideUnit + (w * 2 + (lane & 1)) * 16;
-                        page_of = t < g.ri.hi && t >= 0 ? c.page_at(g.ri.s, t >> c.log_p) : -1;
+                        if constexpr (kListed) {
+                            const int block = t < g.ri.hi && t >= 0 ? list[t >> c.log_p] : -1;
+                            page_of = -1;
+                            if (static_cast<unsigned>(block) < static_cast<unsigned>(c.max_pages)) {
+                                begin_of = (block << c.log_p) + (t & (c.page_tokens() - 1));
+                                if (begin_of < hi_token) page_of = c.page_at(g.ri.s, block);
+                            }
+                        } else {
+                            page_of = t < g.ri.hi && t >= 0 ? c.page_at(g.ri.s, t >> c.log_p) : -1;
+                        }
                     }
                     const uint32_t dst = raw + slot * Plan::kRawHalf + lane * 16;
                     uint32_t on = 0;
@@ -654,6 +688,10 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                         }
                     }
                     present = (present & ~(3u << (2 * slot))) | on << (2 * slot);
+                    if constexpr (kListed) {
+                        const int begin0 = __shfl_sync(0xffffffffu, begin_of, 2 * (step - page_base)), begin1 = __shfl_sync(0xffffffffu, begin_of, 2 * (step - page_base) + 1);
+                        if (lane == 0) slot_begin[warp - 8][slot] = make_int2(begin0, begin1);
+                    }
                 }
                 asm volatile("cp.async.commit_group;" ::: "memory");
             };
@@ -679,15 +717,28 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                         scales[x] = lds8(at + scales_at + (x & 1) * 32) * 0x0101u;
                     }
                 }
+                int t0, t1;                                // positions of the first tokens of the two tiles
+                if constexpr (kListed) {
+                    const int2 begin = slot_begin[warp - 8][slot];
+                    t0 = begin.x;
+                    t1 = begin.y;
+                }
                 __syncwarp();
                 fill(s0 + k + 2 * R, slot);
                 if (++slot == R) slot = 0;
-                const int first_token = base + k * kWideUnit, t0 = first_token + w * 32;
-                const bool all = first_token <= until && first_token > after;
+                const int first_token = base + k * kWideUnit;
+                bool all;                                  // every row sees all of the step; listed: of the two tiles
+                if constexpr (kListed) {
+                    all = there == 3 && max(t0, t1) + 15 <= g.first_pos;
+                } else {
+                    t0 = first_token + w * 32;
+                    t1 = t0 + 16;
+                    all = first_token <= until && first_token > after;
+                }
                 if (!all || there != 3) {                  // what is absent or masked must not be multiplied with
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
-                        if (!((there >> (x >> 1)) & 1) || (values && t0 + x * 8 + tok >= hi_token)) scales[x] = 0;
+                        if (!((there >> (x >> 1)) & 1) || (values && (x < 2 ? t0 : t1) + (x & 1) * 8 + tok >= hi_token)) scales[x] = 0;
                         if (values && !all) {
                             if ((scales[x] & 0x7f) == 0x7f) scales[x] &= 0xff00;
                             if ((scales[x] & 0x7f00) == 0x7f00) scales[x] &= 0x00ff;
@@ -712,14 +763,22 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                 }
                 if (!values) {
                     const int ring = i & 3;
-                    if (lane == 0) tile_there[ring][w] = static_cast<uint8_t>(there);
+                    if (lane == 0) {
+                        tile_there[ring][w] = static_cast<uint8_t>(there);
+                        if constexpr (kListed) {
+                            tile_all[ring][w] = all;
+                            tile_begin[ring][2 * w] = t0;
+                            tile_begin[ring][2 * w + 1] = t1;
+                            if (all) nan_flag[ring][w] = 0;   // others' tiles may make the step one with masks
+                        }
+                    }
                     if (!all) {
                         // NaN among the values of these tokens, for the rows that do see them
                         uint32_t nans = 0;
 #pragma unroll 1
                         for (int x = 0; x < 4; ++x) {
-                            const int t = t0 + x * 8 + tok;
-                            if (!((there >> (x >> 1)) & 1) || t >= g.ri.hi) continue;
+                            const int t = (x < 2 ? t0 : t1) + (x & 1) * 8 + tok;
+                            if (!((there >> (x >> 1)) & 1) || t >= hi_token) continue;
                             const uint8_t* z = c.tile(c.page_at(g.ri.s, t >> c.log_p), a.layer, g.head, t & (c.page_tokens() - 1)) + 17 * D +
                                                ((x & 1) * 8 + tok) * (D / 16) + (D == 128 ? quarter * 2 : quarter);
                             const uint32_t s = D == 128 ? __ldg(reinterpret_cast<const uint16_t*>(z)) : __ldg(z);

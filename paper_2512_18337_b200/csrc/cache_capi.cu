@@ -144,12 +144,12 @@ int launch_stream(const AttendArgs& a, int sms, cudaStream_t s) {
     return launched();
 }
 
-template <typename T, int D>
+template <typename T, int D, bool kListed>
 int launch_wide(const AttendArgs& a, int sms, cudaStream_t s) {
     using Plan = WidePlan<D>;
     static thread_local uint64_t asked = 0;
-    if (int e = allow_shared(attend_wide_kernel<T, D>, Plan::kSmem, &asked)) return e;
-    attend_wide_kernel<T, D><<<std::min(sms, kWideMaxCtas), kWideThreads, Plan::kSmem, s>>>(a);
+    if (int e = allow_shared(attend_wide_kernel<T, D, kListed>, Plan::kSmem, &asked)) return e;
+    attend_wide_kernel<T, D, kListed><<<std::min(sms, kWideMaxCtas), kWideThreads, Plan::kSmem, s>>>(a);
     return launched();
 }
 
@@ -160,7 +160,7 @@ int launch_attend(const AttendArgs& a, cudaStream_t s) {
     const int64_t rows = static_cast<int64_t>(a.Q) * a.group;
     if (rows <= 8) return launch_stream<T, D, 1, false>(a, di.sms, s);
     if (rows <= kNarrowRows) return launch_stream<T, D, 2, false>(a, di.sms, s);
-    return launch_wide<T, D>(a, di.sms, s);
+    return launch_wide<T, D, false>(a, di.sms, s);
 }
 
 template <typename T, int D>
@@ -169,7 +169,8 @@ int launch_attend_blocks(const AttendArgs& a, cudaStream_t s) {
     if (int e = device_info(&di)) return e;
     const int64_t rows = static_cast<int64_t>(a.share) * a.group;
     if (rows <= 8) return launch_stream<T, D, 1, true>(a, di.sms, s);
-    return launch_stream<T, D, 2, true>(a, di.sms, s);
+    if (rows <= kNarrowRows) return launch_stream<T, D, 2, true>(a, di.sms, s);
+    return launch_wide<T, D, true>(a, di.sms, s);
 }
 
 // Scores and picks for all lists, as many at a time as the keys have room for.
