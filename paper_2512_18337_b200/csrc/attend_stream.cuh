@@ -104,16 +104,17 @@ struct StreamCursor {
     RowInfo ri;
     int b, steps, tiles, head, rt, step;
 
-    template <int kRows>
+    template <int kRows, bool kListed>
     __device__ __forceinline__ void enter(const AttendArgs& a, int row, const RowInfo& info) {
         b = row;
         ri = info;
         steps = row_steps<kStreamUnit>(ri);
-        tiles = (ri.n * a.group + kRows - 1) / kRows;
+        tiles = (run_rows<kListed>(a, ri.n) + kRows - 1) / kRows;
+        if (kListed && tiles <= 0) steps = 0;
     }
-    template <int kRows>
+    template <int kRows, bool kListed>
     __device__ __forceinline__ void seek(const AttendArgs& a, int row, const RowInfo& info, int64_t row_begin, int64_t u) {
-        enter<kRows>(a, row, info);
+        enter<kRows, kListed>(a, row, info);
         base = row_begin;
         const int64_t rel = u - base;
         const int seg = static_cast<int>(quotient(rel, steps));
@@ -131,7 +132,7 @@ struct StreamCursor {
         if (++head < a.c.n_kv) return;
         head = 0;
         base += static_cast<int64_t>(steps) * tiles * a.c.n_kv;
-        do enter<kRows>(a, b + 1, row_info<kStreamUnit, kListed>(a, b + 1));
+        do enter<kRows, kListed>(a, b + 1, row_info<kStreamUnit, kListed>(a, b + 1));
         while (steps == 0 && b + 1 < a.runs);
     }
 };
@@ -184,6 +185,7 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
     const CacheView& c = a.c;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int r = lane >> 2, j = lane & 3;
+    const int first_row = kListed ? a.row0 : 0;
 
     // ---- how many units there are, and where our share begins
     int64_t segments = 0;
@@ -191,7 +193,7 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
     RowInfo ri{};                                          // of the row that the thread looked at last
     auto units_of = [&](int b) -> int64_t {
         ri = row_info<kStreamUnit, kListed>(a, b);
-        const int tiles = (ri.n * a.group + kRows - 1) / kRows;
+        const int tiles = max((run_rows<kListed>(a, ri.n) + kRows - 1) / kRows, 0);
         if (count_segments) segments += tiles * c.n_kv;
         return static_cast<int64_t>(row_steps<kStreamUnit>(ri)) * tiles * c.n_kv;
     };
@@ -323,7 +325,7 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
         }
     };
     if (left > 0) {
-        in.seek<kRows>(a, row_of[warp], row_found[warp], row_base[warp], u0);
+        in.seek<kRows, kListed>(a, row_of[warp], row_found[warp], row_base[warp], u0);
         cur = in;
         for (int s = 0; s < kStages; ++s) fill(s);
     }
@@ -337,19 +339,19 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
         // ---- a piece: the units of one segment that are ours
         const int s0 = cur.step;
         const int count = static_cast<int>(min(left, static_cast<int64_t>(cur.steps - s0)));
-        const int rows = cur.ri.n * a.group - cur.rt * kRows;   // query rows of the segment (more than kRows: kRows)
+        const int rows = run_rows<kListed>(a, cur.ri.n) - cur.rt * kRows;   // query rows of the segment (more than kRows: kRows)
         uint32_t qf[NT][KW][4];
         float factor[NT][2], m[NT][2], limit[NT][2], l[NT][2], o[MT][NT][4];   // limit: m + kRaiseAt
         int pos[NT][2];
         int first_pos, last_pos;
         {
-            const int row0 = cur.rt * kRows;
+            const int row0 = cur.rt * kRows + first_row;
             first_pos = cur.ri.len + row0 / a.group;
             last_pos = cur.ri.len + min(row0 + kRows - 1, cur.ri.n * a.group - 1) / a.group;
         }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const int n = nt * 8 + r, rho = cur.rt * kRows + n;
+            const int n = nt * 8 + r, rho = first_row + cur.rt * kRows + n;
             float e_scale = 1.f;
             int e_row = 0;
             alignas(16) T x[KW * 8];
@@ -393,7 +395,7 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
                 const int e_col = __shfl_sync(0xffffffffu, e_row, (2 * j + h) * 4);
                 factor[nt][h] = score_factor(a.scale, c.k_exp - e_col);
                 const int col = nt * 8 + 2 * j + h;
-                pos[nt][h] = col < rows ? cur.ri.len + (cur.rt * kRows + col) / a.group : -1;
+                pos[nt][h] = col < rows ? cur.ri.len + (first_row + cur.rt * kRows + col) / a.group : -1;
                 m[nt][h] = limit[nt][h] = -INFINITY;
                 l[nt][h] = 0.f;
             }
@@ -622,7 +624,7 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
                 if (begins && ends) {
                     if (n < rows) {
                         const RunPlace at = run_place<kListed>(a, cur.b);
-                        const int rho = cur.rt * kRows + n, i = at.i0 + rho / a.group, h = cur.head * a.group + rho % a.group;
+                        const int rho = first_row + cur.rt * kRows + n, i = at.i0 + rho / a.group, h = cur.head * a.group + rho % a.group;
                         const float f = finish_factor(l[nt][x], c.v_exp);
 #pragma unroll
                         for (int d = 0; d < MT * 2; ++d) y[d] = l[nt][x] == 0.f ? 0.f : y[d] * f;
@@ -661,8 +663,8 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
 
     // ---- join the pieces of segments that several warps hold; those that several CTAs hold go on through global memory
     auto write_row = [&](const StreamPiece& d, int n, int ch, float4 x, float top, float l) {
-        const int rho = d.rt * kRows + n;
-        if (rho >= d.n * a.group) return;
+        const int rho = first_row + d.rt * kRows + n;
+        if (rho >= (kListed ? min(d.n * a.group, a.row1) : d.n * a.group)) return;
         const RunPlace at = run_place<kListed>(a, d.b);
         const int i = at.i0 + rho / a.group, h = d.head * a.group + rho % a.group;
         const float f = finish_factor(l, c.v_exp);

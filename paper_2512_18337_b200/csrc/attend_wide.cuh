@@ -35,7 +35,10 @@ constexpr int kWideUnit = 128;                     // tokens of a step
 constexpr int kWideRows = 128;                     // query rows of a segment
 constexpr int kWideWarps = 28, kWideThreads = kWideWarps * 32;   // eight softmax warps, sixteen expanding ones, an issuing one (and three that idle)
 constexpr int kWideMaxCtas = 160;
-constexpr float kWideAbove = 8.f, kTotalMax = 32768.f;   // 64 weights of 2^8 add up to less
+constexpr float kTotalMax = 32768.f;               // 64 weights of 2^8 add up to less
+// How far below the largest score the reference is set.  Pages out of a list differ more from one another than neighbours do, so that
+// it is raised more often: less below leaves more room above, and weights keep all 11 bits down to 2^-18 of the largest, not 2^-22.
+template <bool kListed> constexpr float kWideAbove = kListed ? 4.f : 8.f;
 // columns of tensor memory
 constexpr uint32_t kColQ = 0, kColS = 64, kColO = 320;
 
@@ -141,7 +144,7 @@ __device__ __forceinline__ void wide_tile(const AttendArgs& a, int tiles, int64_
     g.b = static_cast<int>(quotient(e, tiles));
     g.rt = static_cast<int>(e - static_cast<int64_t>(g.b) * tiles);
     g.ri = row_info<kWideUnit, kListed>(a, g.b);
-    g.rows = min(g.ri.n * a.group - g.rt * kWideRows, kWideRows);
+    g.rows = min(run_rows<kListed>(a, g.ri.n) - g.rt * kWideRows, kWideRows);   // a launch of this kernel begins with row 0
     g.steps = 0;
     if (g.rows <= 0) return;
     const int i0 = g.rt * kWideRows / a.group, i1 = (g.rt * kWideRows + g.rows - 1) / a.group, cap = a.c.capacity();
@@ -216,7 +219,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
     barrier_init_fence();
 
     // ---- how many units there are, and where our share begins
-    const int tiles = static_cast<int>((static_cast<int64_t>(a.share) * a.group + kWideRows - 1) / kWideRows);
+    const int tiles = static_cast<int>(((kListed ? a.row1 : static_cast<int64_t>(a.share) * a.group) + kWideRows - 1) / kWideRows);
     const int64_t n_tiles = static_cast<int64_t>(a.runs) * tiles;
     auto block_sum = [&](int64_t x, int64_t* before) -> int64_t {
         int64_t y = x;
@@ -419,7 +422,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
 #pragma unroll
                         for (int i = 0; i < 16; ++i) top = fmaxf(top, __uint_as_float(x[0][i]));
                         top = larger(top);
-                        if (m == -INFINITY) m = top * factor - kWideAbove;
+                        if (m == -INFINITY) m = top * factor - kWideAbove<kListed>;
                     }
                     const float ref = m == -INFINITY ? 0.f : m;
 #pragma unroll
@@ -481,8 +484,8 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                         for (int i = 0; i < 32; ++i) top = fmaxf(top, (bits >> i) & 1 ? __uint_as_float(x[i]) : -INFINITY);
                     }
                     top = larger(top) * factor;
-                    if (__any_sync(0xffffffffu, top > m + kWideAbove)) {
-                        const float to = top > m + kWideAbove ? top - kWideAbove : m;
+                    if (__any_sync(0xffffffffu, top > m + kWideAbove<kListed>)) {
+                        const float to = top > m + kWideAbove<kListed> ? top - kWideAbove<kListed> : m;
                         const float keep = m == -INFINITY ? 0.f : exp2_fast(m - to);
                         if (k > 0) {                     // the sums so far
                             product(n - 1);

@@ -31,7 +31,14 @@ struct AttendArgs {
     // the kernels take for a row ("run"): number v of it is run v % lists of row v / lists.  Otherwise a run is a row.
     const int32_t* blocks;    // [B, lists, n_kv, n_blocks]
     int32_t runs, lists, share, n_blocks;
+    int32_t row0, row1;       // query rows row0 .. row1 - 1 of each run and key/value head are this launch's
 };
+
+// Query rows of a run and key/value head that are this launch's.
+template <bool kListed>
+__device__ __forceinline__ int run_rows(const AttendArgs& a, int n) {
+    return kListed ? min(n * a.group, a.row1) - a.row0 : n * a.group;
+}
 
 // Row of the batch and first query token of a run.
 struct RunPlace {

@@ -116,6 +116,7 @@ int launch_read(const CacheView& v, int32_t layer, int32_t B, int32_t Q, const i
 constexpr int kMaxCtas = 512;
 constexpr int64_t kCounterBytes = kMaxCtas * 4;
 constexpr int64_t kNarrowRows = 32;   // query rows per key/value head up to which the streaming kernel is used
+constexpr int64_t kSplitRows = 8;     // with lists also for up to so many behind the wide kernel's last full tile
 
 template <int D>
 int64_t partial_bytes(int64_t rows) {
@@ -164,13 +165,23 @@ int launch_attend(const AttendArgs& a, cudaStream_t s) {
 }
 
 template <typename T, int D>
-int launch_attend_blocks(const AttendArgs& a, cudaStream_t s) {
+int launch_attend_blocks(AttendArgs a, cudaStream_t s) {
     DeviceInfo di;
     if (int e = device_info(&di)) return e;
-    const int64_t rows = static_cast<int64_t>(a.share) * a.group;
-    if (rows <= 8) return launch_stream<T, D, 1, true>(a, di.sms, s);
-    if (rows <= kNarrowRows) return launch_stream<T, D, 2, true>(a, di.sms, s);
-    return launch_wide<T, D, true>(a, di.sms, s);
+    // What a row tile of the wide kernel costs does not depend on how full it is; up to eight rows behind the last full one take
+    // the streaming kernel less (48 streams of 17 tokens, 64/8 heads, 2,048 positions each: 182 against 223 us; with 8 to 17 tokens a stream, so that
+    // few have a second tile, 172 against 171; sixteen rows 193 against 219, and 169 against 143).
+    const int64_t rows = static_cast<int64_t>(a.share) * a.group, rest = rows % kWideRows;
+    a.row0 = 0;
+    a.row1 = static_cast<int32_t>(rows);
+    if (rows > kNarrowRows) {
+        if (rest <= kSplitRows) a.row1 -= static_cast<int32_t>(rest);
+        if (int e = launch_wide<T, D, true>(a, di.sms, s)) return e;
+        if (a.row1 == rows) return SAM_OK;
+        a.row0 = a.row1;
+        a.row1 = static_cast<int32_t>(rows);
+    }
+    return a.row1 - a.row0 <= 8 ? launch_stream<T, D, 1, true>(a, di.sms, s) : launch_stream<T, D, 2, true>(a, di.sms, s);
 }
 
 // Scores and picks for all lists, as many at a time as the keys have room for.
@@ -398,7 +409,7 @@ int sam_cache_attend(const sam_cache* c, int32_t layer, const void* q, int32_t d
     a.runs = B;
     a.lists = 1;
     a.share = Q;
-    a.n_blocks = 0;
+    a.n_blocks = a.row0 = a.row1 = 0;
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     const bool bf16 = dtype == SAM_CACHE_BF16;
     if (c->head_dim == 64) return bf16 ? launch_attend<__nv_bfloat16, 64>(a, s) : launch_attend<__half, 64>(a, s);

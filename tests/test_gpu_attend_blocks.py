@@ -68,6 +68,9 @@ CASES = [
     ([4000], [3], 3, 64, 8, 128, 16, 3, 200),
     ([0], [300], 300, 4, 2, 128, 16, 16, 6),
     ([40] * 300, [2] * 300, 2, 2, 1, 64, 16, 1, 3),              # more runs than a block has threads
+    ([600, 90, 333], [17, 9, 16], 17, 16, 2, 128, 16, 17, 12),   # 136 query rows a list, and fewer
+    ([300, 50], [65, 64], 65, 2, 1, 64, 16, 65, 9),              # 130
+    ([100, 900], [90, 11], 90, 3, 1, 128, 32, 90, 14),           # 270
 ]
 
 
