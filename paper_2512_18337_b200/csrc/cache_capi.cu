@@ -184,25 +184,50 @@ int launch_attend_blocks(AttendArgs a, cudaStream_t s) {
     return a.row1 - a.row0 <= 8 ? launch_stream<T, D, 1, true>(a, di.sms, s) : launch_stream<T, D, 2, true>(a, di.sms, s);
 }
 
+template <int kTeam, int kKeys>
+int launch_pick(const SelectArgs& a, int64_t rows, cudaStream_t s) {
+    constexpr int kLists = kPickThreads / kTeam;
+    select_pick_kernel<kTeam, kKeys><<<static_cast<unsigned>((rows + kLists - 1) / kLists), kPickThreads, 0, s>>>(a, rows);
+    return launched();
+}
+
+int64_t key_stride(const sam_cache* c) { return (static_cast<int64_t>(c->max_pages) + 3) & ~int64_t(3); }
+constexpr int64_t kKeyBytes = int64_t(128) << 20;   // of the keys that are in flight at a time, where there are as many
+
+// Most lists of a row that are scored together: their keys are there together.
+int64_t most_team(const sam_cache* c, int64_t lists) {
+    return std::max<int64_t>(std::min({lists, int64_t(kScoreTeam), kKeyBytes / (c->n_kv_heads * key_stride(c) * 4)}), 1);
+}
+
+// Lists of a row that one block scores: as many as fit its columns, but no more than leave two blocks an SM.
+int32_t select_team(const sam_cache* c, int32_t B, int64_t lists, int64_t rows, int sms) {
+    const int64_t fit = std::max<int64_t>(kScoreColumns / ((rows + 7) / 8 * 8), 1);
+    const int64_t wanted = static_cast<int64_t>(B) * lists * c->n_kv_heads / (2 * sms);
+    return static_cast<int32_t>(std::max<int64_t>(std::min({fit, wanted, most_team(c, lists)}), 1));
+}
+
 // Scores and picks for all lists, as many at a time as the keys have room for.
 template <typename T>
-int launch_select(SelectArgs a, int64_t key_bytes, cudaStream_t s) {
-    DeviceInfo di;
-    if (int e = device_info(&di)) return e;
-    const int64_t runs = static_cast<int64_t>(a.B) * a.lists, each = static_cast<int64_t>(a.c.n_kv) * a.c.max_pages * 4;
+int launch_select(SelectArgs a, int64_t key_bytes, int sms, cudaStream_t s) {
+    const int64_t all = static_cast<int64_t>(a.B) * a.teams, each = a.team * a.c.n_kv * a.key_stride * 4;   // bytes of a team's keys
     const int64_t most = std::min<int64_t>(std::max<int64_t>(key_bytes / each, 1), 65535);
-    for (int64_t at = 0; at < runs; at += most) {
-        a.first_run = at;
-        a.runs = static_cast<int32_t>(std::min(runs - at, most));
-        // a warp takes sixteen pages; about eight blocks an SM
+    for (int64_t at = 0; at < all; at += most) {
+        const int64_t n = std::min(all - at, most);
+        a.first_team = at;
+        // a warp takes sixteen pages at a time; about four blocks an SM
         const int64_t full = (static_cast<int64_t>(a.c.max_pages) + kScoreThreads / 2 - 1) / (kScoreThreads / 2);
-        const int64_t wanted = (static_cast<int64_t>(di.sms) * 8 + a.runs * a.c.n_kv - 1) / (static_cast<int64_t>(a.runs) * a.c.n_kv);
-        const dim3 grid(static_cast<unsigned>(std::min(full, wanted)), a.c.n_kv, a.runs);
+        const int64_t wanted = (static_cast<int64_t>(sms) * 4 + n * a.c.n_kv - 1) / (n * a.c.n_kv);
+        const dim3 grid(static_cast<unsigned>(std::min(full, wanted)), a.c.n_kv, static_cast<unsigned>(n));
         if (a.c.D == 64) select_score_kernel<T, 64><<<grid, kScoreThreads, 0, s>>>(a);
         else select_score_kernel<T, 128><<<grid, kScoreThreads, 0, s>>>(a);
         if (int e = launched()) return e;
-        select_pick_kernel<<<dim3(a.c.n_kv, a.runs), kPickThreads, 0, s>>>(a);
-        if (int e = launched()) return e;
+        const int64_t rows = n * a.team * a.c.n_kv;
+        const int e = a.c.max_pages <= 512    ? launch_pick<32, 16>(a, rows, s)
+                      : a.c.max_pages <= 1024 ? launch_pick<32, 32>(a, rows, s)
+                      : a.c.max_pages <= 2048 ? launch_pick<256, 8>(a, rows, s)
+                      : a.c.max_pages <= 8192 ? launch_pick<256, 32>(a, rows, s)
+                                              : launch_pick<256, 0>(a, rows, s);
+        if (e) return e;
     }
     return SAM_OK;
 }
@@ -216,8 +241,6 @@ int check_layer_call(const sam_cache* c, int32_t layer, int32_t B, int32_t Q, co
 }
 
 int check_bounds(const int8_t* codes, const int8_t* exps) { return codes && exps && aligned(codes, 16) ? SAM_OK : SAM_ERR_INVALID_ARG; }
-
-constexpr int64_t kKeyBytes = int64_t(128) << 20;   // of the keys that are in flight at a time, where there are as many
 
 template <typename T>
 int launch_turn(const TurnArgs& a, cudaStream_t s) {
@@ -555,8 +578,9 @@ int64_t sam_cache_select_workspace_bytes(const sam_cache* c, int32_t B, int32_t 
     if (int e = check_cache(c)) return e;
     if (B < 0 || Q < 0 || share < 1) return SAM_ERR_INVALID_ARG;
     if (B > SAM_CACHE_MAX_B || Q > kLargest) return SAM_ERR_TOO_LARGE;
-    const int64_t each = static_cast<int64_t>(c->n_kv_heads) * c->max_pages * 4, runs = B * ((static_cast<int64_t>(Q) + share - 1) / share);
-    return std::max<int64_t>(std::min(runs * each, kKeyBytes), each);
+    // the last team of a row may be short of lists
+    const int64_t each = static_cast<int64_t>(c->n_kv_heads) * key_stride(c) * 4, lists = (static_cast<int64_t>(Q) + share - 1) / share;
+    return std::max<int64_t>(std::min(B * (lists + most_team(c, lists) - 1) * each, kKeyBytes), each);
 }
 
 int sam_cache_select(const sam_cache* c, int32_t layer, const int8_t* codes, const int8_t* exps, const void* q, int32_t dtype, int64_t q_row_stride,
@@ -595,11 +619,16 @@ int sam_cache_select(const sam_cache* c, int32_t layer, const int8_t* codes, con
     a.n_blocks = n_blocks;
     a.n_sink = n_sink;
     a.n_recent = n_recent;
+    DeviceInfo di;
+    if (int e = device_info(&di)) return e;
+    a.team = select_team(c, B, lists, static_cast<int64_t>(share) * a.group, di.sms);
+    a.teams = static_cast<int32_t>((lists + a.team - 1) / a.team);
+    a.key_stride = key_stride(c);
     a.keys = static_cast<uint32_t*>(workspace);
     a.out = blocks;
     a.q_wide = aligned(q, 16) && (q_row_stride | q_token_stride | q_head_stride) % 8 == 0;
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-    return dtype == SAM_CACHE_BF16 ? launch_select<__nv_bfloat16>(a, workspace_bytes, s) : launch_select<__half>(a, workspace_bytes, s);
+    return dtype == SAM_CACHE_BF16 ? launch_select<__nv_bfloat16>(a, workspace_bytes, di.sms, s) : launch_select<__half>(a, workspace_bytes, di.sms, s);
 }
 
 }  // extern "C"

@@ -134,73 +134,106 @@ struct SelectArgs {
     int64_t q_row, q_token, q_head;
     int32_t layer, B, Q, H, group;
     int32_t lists, share, n_blocks, n_sink, n_recent;
-    int64_t first_run;           // of this launch: run v is list v % lists of row v / lists
-    int32_t runs;
-    uint32_t* keys;              // [runs, n_kv, max_pages]
+    int32_t team, teams;         // lists of a row that are scored together; such teams in a row
+    int64_t first_team;          // of this launch
+    int64_t key_stride;          // of a list and head: max_pages, rounded up to a multiple of 4
+    uint32_t* keys;              // [teams of the launch, team, n_kv, key_stride]
     int32_t* out;                // [B, lists, n_kv, n_blocks]
     bool q_wide;
 };
 
-// A run of query tokens with a list in common.
+// A run of query tokens with a list in common: list l of row b.
 struct SelectRun {
     int s, n;          // stream, -1 = unknown; query tokens in use
     int pages;         // blocks up to the last query's own, within the table
     int old;           // blocks [n_sink, old) are scored, those behind are listed
-    int b, i0;
 };
-__device__ __forceinline__ SelectRun select_run(const SelectArgs& a, int64_t v) {
+__device__ __forceinline__ SelectRun select_run(const SelectArgs& a, int b, int l) {
     SelectRun r;
-    r.b = static_cast<int>(quotient(v, a.lists));
-    r.i0 = static_cast<int>(v - static_cast<int64_t>(r.b) * a.lists) * a.share;
-    r.s = a.c.stream_of(a.streams, r.b);
-    r.n = r.s < 0 ? 0 : min(max((a.n_new ? min(a.n_new[r.b], a.Q) : a.Q) - r.i0, 0), a.share);
-    const int64_t first = r.s < 0 ? 0 : static_cast<int64_t>(a.c.length_of(r.s)) + r.i0;
+    const int i0 = l * a.share;
+    r.s = a.c.stream_of(a.streams, b);
+    r.n = r.s < 0 ? 0 : min(max((a.n_new ? min(a.n_new[b], a.Q) : a.Q) - i0, 0), a.share);
+    const int64_t first = r.s < 0 ? 0 : static_cast<int64_t>(a.c.length_of(r.s)) + i0;
     r.pages = r.n > 0 ? static_cast<int>(min(((first + r.n - 1) >> a.c.log_p) + 1, static_cast<int64_t>(a.c.max_pages))) : 0;
     r.old = static_cast<int>(min(max((first >> a.c.log_p) + 1 - a.n_recent, int64_t(0)), static_cast<int64_t>(r.pages)));
     return r;
 }
 
-// Monotone in the float: larger keys for larger scores; 1 or more, and below the keys that go first.
+// Monotone in the float: larger keys for larger scores; above 1, and below the keys that go first.
 __device__ __forceinline__ uint32_t score_key(float x) {
     const uint32_t u = __float_as_uint(x + 0.f);
     return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 
-constexpr int kScoreThreads = 256, kScoreColumns = 64;   // query rows in shared memory at a time
+constexpr int kScoreThreads = 256, kScoreColumns = 128, kScoreTeam = kScoreColumns / 8;   // query rows in shared memory at a time; most lists of a team
 
 __device__ __forceinline__ void mma_s8(int (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// Keys of the pages of one run and head: sixteen pages of a warp are the M side, eight query rows the N side.
-// Grid: (shares of the pages, heads, runs).
+// Keys of the pages of a team of lists and a head: sixteen pages of a warp are the M side, eight query rows the N side.  The bounds of a
+// page come straight from memory into the fragments (the order of the summed index is free, so that a thread has sixteen neighbouring
+// bytes at a time), the next sixteen pages' while these are multiplied, and serve all lists of the team.
+// Grid: (shares of the pages, heads, teams).
 template <typename T, int D>
 __global__ void __launch_bounds__(kScoreThreads) select_score_kernel(const __grid_constant__ SelectArgs a) {
     constexpr int kStride = 2 * D + 64;                   // of a column in shared memory: two columns fill all banks
     constexpr int kParts = 2 * D / 64;                    // sixteen-byte parts of a row or column that a thread has
     __shared__ alignas(16) uint8_t columns[kScoreColumns * kStride];
     __shared__ float unit[kScoreColumns];
+    __shared__ SelectRun runs[kScoreTeam];
     const CacheView& c = a.c;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, j = lane & 3;
     const int head = blockIdx.y;
-    const SelectRun run = select_run(a, a.first_run + blockIdx.z);
-    if (run.pages == 0) return;
-    const bool scored = run.pages > a.n_blocks;           // else all of them are listed
-    uint32_t* keys = a.keys + (static_cast<int64_t>(blockIdx.z) * c.n_kv + head) * c.max_pages;
-    const int rows = run.n * a.group, step = gridDim.x * (kScoreThreads / 2);
-    for (int col0 = 0; col0 == 0 || (scored && col0 < rows); col0 += kScoreColumns) {
-        const int cols = min(rows - col0, kScoreColumns), tiles = (cols + 7) >> 3;
+    const int64_t team = a.first_team + blockIdx.z;
+    const int b = static_cast<int>(quotient(team, a.teams)), l0 = static_cast<int>(team - static_cast<int64_t>(b) * a.teams) * a.team;
+    if (threadIdx.x < a.team) {
+        SelectRun run{-1, 0, 0, 0};
+        if (l0 + static_cast<int>(threadIdx.x) < a.lists) run = select_run(a, b, l0 + threadIdx.x);
+        runs[threadIdx.x] = run;
+    }
+    __syncthreads();
+    int most = 0, s = -1;                                 // pages of the list that has most
+    for (int l = 0; l < a.team; ++l) {
+        most = max(most, runs[l].pages);
+        if (runs[l].n > 0) s = runs[l].s;
+    }
+    if (most == 0) return;
+    const bool scored = most > a.n_blocks;                // else all blocks are listed
+    uint32_t* const keys = a.keys + (static_cast<int64_t>(blockIdx.z) * a.team * c.n_kv + head) * a.key_stride;
+    const int64_t list_stride = c.n_kv * a.key_stride;
+    const int each = a.share * a.group, padded = (each + 7) & ~7;   // columns of a list; more than fit are taken in turns
+    const int first = (blockIdx.x * (kScoreThreads / 32) + warp) * 16, step = gridDim.x * (kScoreThreads / 2);
+    auto page_of = [&](int i) { return i < most ? c.page_at(s, i) : -1; };
+    auto fetch = [&](const int (&page)[2], uint4 (&x)[2][kParts], int (&e)[2]) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int64_t at = (static_cast<int64_t>(max(page[h], 0)) * c.n_layers + a.layer) * c.n_kv + head;
+            e[h] = page[h] < 0 ? 0 : a.o.exps[at];
+#pragma unroll
+            for (int k = 0; k < kParts; ++k)
+                x[h][k] = page[h] < 0 ? make_uint4(0, 0, 0, 0) : __ldg(reinterpret_cast<const uint4*>(a.o.codes + at * 2 * D) + k * 4 + j);
+        }
+    };
+    for (int col0 = 0; col0 == 0 || (scored && col0 < each); col0 += kScoreColumns) {
+        uint4 next[2][kParts];
+        int page[2], next_page[2], next_e[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) page[h] = page_of(first + r + 8 * h);
+        if (scored) fetch(page, next, next_e);
+        const int tiles = min(padded - col0, kScoreColumns) >> 3;   // of a list; more than one list only if all its columns fit
         __syncthreads();
         if (scored) {
             // queries in eight bits, their positive and their negative parts: a warp takes a row
-            for (int n = warp; n < tiles * 8; n += kScoreThreads / 32) {
+            for (int n = warp; n < a.team * tiles * 8; n += kScoreThreads / 32) {
+                const int l = n / (tiles * 8), rho = col0 + n - l * tiles * 8;
+                const bool used = rho < runs[l].n * a.group;
                 float x[D / 32];
 #pragma unroll
                 for (int k = 0; k < D / 32; ++k) x[k] = 0.f;
-                if (n < cols) {
-                    const int rho = col0 + n;
-                    const T* q = static_cast<const T*>(a.q) + run.b * a.q_row + (run.i0 + rho / a.group) * a.q_token +
+                if (used) {
+                    const T* q = static_cast<const T*>(a.q) + b * a.q_row + (static_cast<int64_t>(l0 + l) * a.share + rho / a.group) * a.q_token +
                                  (head * a.group + rho % a.group) * a.q_head + lane * (D / 32);
                     if (a.q_wide) {
                         alignas(8) T y[D / 32];
@@ -219,8 +252,7 @@ __global__ void __launch_bounds__(kScoreThreads) select_score_kernel(const __gri
                     const float y = fabsf(x[k]);
                     if (y < INFINITY) big = fmaxf(big, y);
                 }
-#pragma unroll
-                for (int d = 16; d > 0; d >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, d));
+                big = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(big)));   // not negative: in the order of its bits
                 const int e = big >= 1.17549435e-38f ? max(eight_bit_exponent(big), -100) : 0;
                 uint32_t up = 0, dn = 0;
 #pragma unroll
@@ -237,173 +269,230 @@ __global__ void __launch_bounds__(kScoreThreads) select_score_kernel(const __gri
                     *reinterpret_cast<uint16_t*>(col) = static_cast<uint16_t>(up);
                     *reinterpret_cast<uint16_t*>(col + D) = static_cast<uint16_t>(dn);
                 }
-                if (lane == 0) unit[n] = n < cols ? pow2(e) : 0.f;
+                if (lane == 0) unit[n] = used ? pow2(e) : -1.f;
             }
             __syncthreads();
         }
-        for (int i0 = (blockIdx.x * (kScoreThreads / 32) + warp) * 16; i0 < run.pages; i0 += step) {
-            // pages i0 + r and + 8: what there is, and their keys
-            int page[2];
-            uint32_t key[2];
-            float size[2];
+        for (int i0 = first; i0 < most; i0 += step) {
+            // pages i0 + r and + 8, and the next ones
             uint4 x[2][kParts];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int i = i0 + r + 8 * h;
-                page[h] = i < run.pages ? c.page_at(run.s, i) : -1;
-                key[h] = page[h] < 0 ? 0u : !scored || i < a.n_sink || i >= run.old ? kForced : 1u;
-                size[h] = 0.f;
-                const int64_t at = (static_cast<int64_t>(max(page[h], 0)) * c.n_layers + a.layer) * c.n_kv + head;
-#pragma unroll
-                for (int k = 0; k < kParts; ++k) x[h][k] = make_uint4(0, 0, 0, 0);
-                if (key[h] == 1u) {
-                    const int e = a.o.exps[at];
-                    if (e == kNanPage) key[h] = kNanKey;
-                    size[h] = pow2(e == kNanPage ? 0 : e);
-#pragma unroll
-                    for (int k = 0; k < kParts; ++k) x[h][k] = __ldg(reinterpret_cast<const uint4*>(a.o.codes + at * 2 * D) + k * 4 + j);
-                }
-            }
-            if (__any_sync(0xffffffffu, key[0] == 1u || key[1] == 1u)) {
-                float best[2] = {-INFINITY, -INFINITY};
-                for (int t = 0; t < tiles; ++t) {
-                    int acc[4] = {0, 0, 0, 0};
-                    const uint8_t* col = columns + (t * 8 + r) * kStride + j * 16;
-#pragma unroll
-                    for (int k = 0; k < kParts; ++k) {
-                        const uint4 y = *reinterpret_cast<const uint4*>(col + k * 64);
-                        mma_s8(acc, x[0][k].x, x[1][k].x, x[0][k].y, x[1][k].y, y.x, y.y);
-                        mma_s8(acc, x[0][k].z, x[1][k].z, x[0][k].w, x[1][k].w, y.z, y.w);
-                    }
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        const int n = t * 8 + 2 * j + k;
-                        if (n < cols) {
-                            best[0] = fmaxf(best[0], static_cast<float>(acc[k]) * unit[n]);
-                            best[1] = fmaxf(best[1], static_cast<float>(acc[2 + k]) * unit[n]);
-                        }
-                    }
-                }
+            float size[2];
+            bool nan[2];
+            const int here[2] = {page[0], page[1]};
+            if (scored) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    best[h] = fmaxf(best[h], __shfl_xor_sync(0xffffffffu, best[h], 1));
-                    best[h] = fmaxf(best[h], __shfl_xor_sync(0xffffffffu, best[h], 2));
-                    if (key[h] == 1u) key[h] = score_key(best[h] * size[h]);
+                    nan[h] = next_e[h] == kNanPage;
+                    size[h] = pow2(nan[h] ? 0 : next_e[h]);
+#pragma unroll
+                    for (int k = 0; k < kParts; ++k) x[h][k] = next[h][k];
                 }
             }
-            if (j < 2) {                                  // lane j = 0: page r, j = 1: page r + 8
-                const int i = i0 + r + 8 * j;
-                const uint32_t y = j ? key[1] : key[0];
-                if (i < run.pages) keys[i] = col0 == 0 ? y : max(keys[i], y);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) page[h] = next_page[h] = page_of(i0 + step + r + 8 * h);
+            if (scored && i0 + step < most) fetch(next_page, next, next_e);
+            for (int l = 0; l < a.team; ++l) {
+                const int pages = runs[l].pages, old = runs[l].old;
+                if (i0 >= pages) continue;
+                float best[2] = {-INFINITY, -INFINITY};
+                if (pages > a.n_blocks && i0 < old) {
+                    for (int t = 0; t < tiles; ++t) {
+                        int acc[4] = {0, 0, 0, 0};
+                        const int n0 = (l * tiles + t) * 8;
+                        const uint8_t* col = columns + (n0 + r) * kStride + j * 16;
+#pragma unroll
+                        for (int k = 0; k < kParts; ++k) {
+                            const uint4 y = *reinterpret_cast<const uint4*>(col + k * 64);
+                            mma_s8(acc, x[0][k].x, x[1][k].x, x[0][k].y, x[1][k].y, y.x, y.y);
+                            mma_s8(acc, x[0][k].z, x[1][k].z, x[0][k].w, x[1][k].w, y.z, y.w);
+                        }
+                        const float2 u = *reinterpret_cast<const float2*>(&unit[n0 + 2 * j]);
+                        if (u.x >= 0.f) {
+                            best[0] = fmaxf(best[0], static_cast<float>(acc[0]) * u.x);
+                            best[1] = fmaxf(best[1], static_cast<float>(acc[2]) * u.x);
+                        }
+                        if (u.y >= 0.f) {
+                            best[0] = fmaxf(best[0], static_cast<float>(acc[1]) * u.y);
+                            best[1] = fmaxf(best[1], static_cast<float>(acc[3]) * u.y);
+                        }
+                    }
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        best[h] = fmaxf(best[h], __shfl_xor_sync(0xffffffffu, best[h], 1));
+                        best[h] = fmaxf(best[h], __shfl_xor_sync(0xffffffffu, best[h], 2));
+                    }
+                }
+                if (j < 2) {                              // lane j = 0: page r, j = 1: page r + 8
+                    const int i = i0 + r + 8 * j;
+                    uint32_t key = 0;
+                    if ((j ? here[1] : here[0]) >= 0)
+                        key = pages <= a.n_blocks || i < a.n_sink || i >= old ? kForced : (j ? nan[1] : nan[0]) ? kNanKey : score_key(j ? best[1] * size[1] : best[0] * size[0]);
+                    uint32_t* at = keys + l * list_stride + i;
+                    if (i < pages) *at = col0 == 0 ? key : max(*at, key);
+                }
             }
         }
     }
 }
 
-// ---- the best pages of a run and head: the n_blocks-th largest key by eight bits at a time, then all pages above it and the first of
-// those that equal it, in order.
-constexpr int kPickThreads = 256, kPickKeep = 4096;      // keys in shared memory
+// ---- the best pages of a list: the keys lie in registers, kKeys neighbouring ones a thread; the n_blocks-th largest is found bit by bit,
+// and listed are all pages above it and the first of those that equal it, in order.  A list is a warp's or a block's.
+constexpr int kPickThreads = 256;
 
-// Exclusive prefix sum of two counts below 2^31 over the block; *total gets the sums.
-__device__ __forceinline__ int2 block_scan2(int2 x, int2* total) {
-    __shared__ int2 sums[kPickThreads / 32];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int2 y = x;
+template <int kTeam>
+struct PickTeam {
+    static constexpr int kWarps = kTeam / 32;
+    int2 (*sums)[kWarps > 1 ? kWarps : 1];   // [2][warps]
+    int flip = 0;
+    // Sums of two counts over the team; *before: over its earlier threads.
+    __device__ __forceinline__ int2 scan(int2 x, int2* before) {
+        const int lane = threadIdx.x & 31;
+        int2 y = x;
 #pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const int u = __shfl_up_sync(0xffffffffu, y.x, d), v = __shfl_up_sync(0xffffffffu, y.y, d);
-        if (lane >= d) {
-            y.x += u;
-            y.y += v;
+        for (int d = 1; d < 32; d <<= 1) {
+            const int u = __shfl_up_sync(0xffffffffu, y.x, d), v = __shfl_up_sync(0xffffffffu, y.y, d);
+            if (lane >= d) {
+                y.x += u;
+                y.y += v;
+            }
+        }
+        int2 all = make_int2(__shfl_sync(0xffffffffu, y.x, 31), __shfl_sync(0xffffffffu, y.y, 31)), earlier = make_int2(0, 0);
+        if constexpr (kWarps > 1) {
+            const int warp = threadIdx.x >> 5;
+            if (lane == 0) sums[flip][warp] = all;
+            __syncthreads();
+            all = make_int2(0, 0);
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                if (w == warp) earlier = all;
+                all.x += sums[flip][w].x;
+                all.y += sums[flip][w].y;
+            }
+            flip ^= 1;
+        }
+        *before = make_int2(earlier.x + y.x - x.x, earlier.y + y.y - x.y);
+        return all;
+    }
+    __device__ __forceinline__ int sum(int x) {
+        int all = __reduce_add_sync(0xffffffffu, x);
+        if constexpr (kWarps > 1) {
+            if ((threadIdx.x & 31) == 0) sums[flip][threadIdx.x >> 5].x = all;
+            __syncthreads();
+            all = 0;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) all += sums[flip][w].x;
+            flip ^= 1;
+        }
+        return all;
+    }
+    // Bitwise "or" and "and" over the team.
+    __device__ __forceinline__ void bits(uint32_t& any, uint32_t& every) {
+        any = __reduce_or_sync(0xffffffffu, any);
+        every = __reduce_and_sync(0xffffffffu, every);
+        if constexpr (kWarps > 1) {
+            if ((threadIdx.x & 31) == 0) sums[flip][threadIdx.x >> 5] = make_int2(static_cast<int>(any), static_cast<int>(every));
+            __syncthreads();
+            any = 0;
+            every = 0xffffffffu;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                any |= static_cast<uint32_t>(sums[flip][w].x);
+                every &= static_cast<uint32_t>(sums[flip][w].y);
+            }
+            flip ^= 1;
         }
     }
-    __syncthreads();
-    if (lane == 31) sums[warp] = y;
-    __syncthreads();
-    int2 before = make_int2(0, 0), all = make_int2(0, 0);
-#pragma unroll
-    for (int w = 0; w < kPickThreads / 32; ++w) {
-        if (w == warp) before = all;
-        all.x += sums[w].x;
-        all.y += sums[w].y;
-    }
-    *total = all;
-    return make_int2(before.x + y.x - x.x, before.y + y.y - x.y);
-}
+};
 
-// Grid: (heads, runs).
-__global__ void __launch_bounds__(kPickThreads) select_pick_kernel(const __grid_constant__ SelectArgs a) {
-    __shared__ uint32_t kept[kPickKeep];
-    __shared__ int bins[256];
-    __shared__ uint32_t chosen;
-    __shared__ int above;
+// kKeys = 0: any number of pages, the keys read again each time.  Grid: (lists and heads of the launch in runs of kPickThreads / kTeam).
+template <int kTeam, int kKeys>
+__global__ void __launch_bounds__(kPickThreads) select_pick_kernel(const __grid_constant__ SelectArgs a, int64_t n_lists) {
+    using Team = PickTeam<kTeam>;
+    __shared__ int2 sums[2][Team::kWarps];
+    Team team{sums};
     const CacheView& c = a.c;
-    const int tid = threadIdx.x, head = blockIdx.x;
-    const SelectRun run = select_run(a, a.first_run + blockIdx.y);
-    int32_t* out = a.out + ((a.first_run + blockIdx.y) * c.n_kv + head) * a.n_blocks;
-    const uint32_t* keys = a.keys + (static_cast<int64_t>(blockIdx.y) * c.n_kv + head) * c.max_pages;
-    const int n = run.pages;
-    const bool keep = n <= kPickKeep;
-    if (keep)
-        for (int i = tid; i < n; i += kPickThreads) kept[i] = keys[i];
-    __syncthreads();
-    auto key = [&](int i) { return keep ? kept[i] : keys[i]; };
-    // the key of the last page that is listed, and how many with that key are
-    uint32_t limit = 1;
-    int ties = a.n_blocks;
-    if (n > a.n_blocks) {
-        uint32_t prefix = 0, mask = 0;
-        int want = a.n_blocks;                            // from the keys that begin with the prefix
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            bins[tid] = 0;
-            __syncthreads();
-            for (int i = tid; i < n; i += kPickThreads) {
-                const uint32_t k = key(i);
-                if ((k & mask) == prefix) atomicAdd(&bins[(k >> shift) & 255], 1);
-            }
-            __syncthreads();
-            int2 total;
-            const int mine = bins[255 - tid];
-            const int before = block_scan2(make_int2(mine, 0), &total).x;   // keys in higher bins
-            if (before < want && before + mine >= want) {
-                chosen = 255 - tid;
-                above = before;
-            }
-            __syncthreads();
-            prefix |= chosen << shift;
-            mask |= 255u << shift;
-            want -= above;
-            __syncthreads();
-        }
-        limit = prefix;
-        ties = want;
-        if (limit == 0) {                                 // fewer pages present than wanted
-            limit = 1;
-            ties = a.n_blocks;
+    const int t = threadIdx.x % kTeam;
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * (kPickThreads / kTeam) + threadIdx.x / kTeam;   // of the keys
+    if (row >= n_lists) return;                           // the whole team
+    const int64_t g = quotient(row, c.n_kv), w = quotient(g, a.team), v = a.first_team + w;
+    const int head = static_cast<int>(row - g * c.n_kv), b = static_cast<int>(quotient(v, a.teams));
+    const int l = static_cast<int>(v - static_cast<int64_t>(b) * a.teams) * a.team + static_cast<int>(g - w * a.team);
+    if (l >= a.lists) return;
+    const int n = select_run(a, b, l).pages;
+    int32_t* const out = a.out + ((static_cast<int64_t>(b) * a.lists + l) * c.n_kv + head) * a.n_blocks;
+    const uint32_t* const keys = a.keys + row * a.key_stride;
+    const int each = kKeys ? kKeys : (n + kTeam - 1) / kTeam, i0 = t * each;   // the thread's pages: i0 .. i0 + each - 1
+    uint32_t kept[kKeys ? kKeys : 1];
+    if constexpr (kKeys > 0) {
+#pragma unroll
+        for (int k = 0; k < kKeys; k += 4) {
+            uint4 x = make_uint4(0, 0, 0, 0);
+            if (i0 + k < n) x = *reinterpret_cast<const uint4*>(keys + i0 + k);
+            kept[k] = i0 + k < n ? x.x : 0u;
+            kept[k + 1] = i0 + k + 1 < n ? x.y : 0u;
+            kept[k + 2] = i0 + k + 2 < n ? x.z : 0u;
+            kept[k + 3] = i0 + k + 3 < n ? x.w : 0u;
         }
     }
-    // in order: a thread takes neighbouring pages
-    const int each = (n + kPickThreads - 1) / kPickThreads, i0 = min(tid * each, n), i1 = min(i0 + each, n);
+    auto for_keys = [&](auto f) {
+        if constexpr (kKeys > 0) {
+#pragma unroll
+            for (int k = 0; k < kKeys; ++k) f(kept[k], i0 + k);
+        } else {
+            for (int k = 0; k < each; ++k)
+                if (i0 + k < n) f(keys[i0 + k], i0 + k);
+        }
+    };
+    // the key of the last page that is listed: the largest for which n_blocks pages reach it, 1 if fewer are present
+    uint32_t limit = 1;
+    if (n > a.n_blocks) {
+        int present = 0, forced = 0;
+        uint32_t any = 0, every = 0xffffffffu;            // bits of the keys in between
+        for_keys([&](uint32_t k, int) {
+            present += k != 0;
+            forced += k == kForced;
+            if (k != 0 && k != kForced) {
+                any |= k;
+                every &= k;
+            }
+        });
+        int2 unused;
+        const int2 all = team.scan(make_int2(present, forced), &unused);
+        team.bits(any, every);
+        const int want = a.n_blocks - all.y;              // of them: forced ones always fit
+        if (all.x > a.n_blocks) {
+            if (want <= 0) {
+                limit = kForced;
+            } else {
+                uint32_t differ = any & ~every;           // where they are not all alike
+                limit = every;
+                while (differ) {
+                    const uint32_t bit = 0x80000000u >> __clz(differ);
+                    differ &= ~bit;
+                    const uint32_t to = limit | bit;
+                    int count = 0;
+                    for_keys([&](uint32_t k, int) { count += k >= to && k != kForced; });
+                    if (team.sum(count) >= want) limit = to;
+                }
+            }
+        }
+    }
     int2 count = make_int2(0, 0);
-    for (int i = i0; i < i1; ++i) {
-        const uint32_t k = key(i);
+    for_keys([&](uint32_t k, int) {
         count.x += k > limit;
         count.y += k == limit;
-    }
-    int2 total;
-    const int2 before = block_scan2(count, &total);
-    int greater = before.x, equal = before.y;
-    for (int i = i0; i < i1; ++i) {
-        const uint32_t k = key(i);
-        if (k > limit || (k == limit && equal < ties)) {
-            const int at = greater + min(equal, ties);
-            if (at < a.n_blocks) out[at] = i;
-        }
-        greater += k > limit;
+    });
+    int2 before;
+    const int2 total = team.scan(count, &before);
+    const int ties = a.n_blocks - total.x;                // so many of the pages at the limit
+    int at = before.x + min(before.y, ties), equal = before.y;
+    for_keys([&](uint32_t k, int i) {
+        const bool on = k > limit || (k == limit && equal < ties);
+        if (on && at < a.n_blocks) out[at] = i;
+        at += on;
         equal += k == limit;
-    }
-    const int used = min(total.x + min(total.y, ties), a.n_blocks);
-    for (int i = used + tid; i < a.n_blocks; i += kPickThreads) out[i] = -1;
+    });
+    for (int i = min(total.x + min(total.y, ties), a.n_blocks) + t; i < a.n_blocks; i += kTeam) out[i] = -1;
 }
 
 }  // namespace samb200

@@ -93,7 +93,7 @@ def test_bounds_and_select_refuse():
     assert lib.sam_cache_bounds_rebuild(c, 16, 1, -1, None, None) == -1 and lib.sam_cache_bounds_rebuild(c, 16, 1, 9, None, None) == -1
     assert lib.sam_cache_bounds_rebuild(c, None, 1, 1, None, None) == -1 and lib.sam_cache_bounds_rebuild(c, 16, 1, 0, None, None) == 0
     need = lib.sam_cache_select_workspace_bytes(c, 2, 5, 2)
-    assert need == 2 * 3 * 2 * 4 * 4
+    assert need == 2 * (3 + 2) * 2 * 4 * 4                                         # lists of two rows, some to spare, heads, pages
     wide = C.addressof(w := _struct(max_pages=1 << 16, n_kv_heads=8))
     assert lib.sam_cache_select_workspace_bytes(wide, 64, 2048, 1) == 1 << 27      # as much as is in flight at a time
     huge = C.addressof(h := _struct(max_pages=1 << 26, n_streams=1, n_kv_heads=8))
