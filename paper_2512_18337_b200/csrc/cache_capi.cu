@@ -199,11 +199,29 @@ int64_t most_team(const sam_cache* c, int64_t lists) {
     return std::max<int64_t>(std::min({lists, int64_t(kScoreTeam), kKeyBytes / (c->n_kv_heads * key_stride(c) * 4)}), 1);
 }
 
-// Lists of a row that one block scores: as many as fit its columns, but no more than leave two blocks an SM.
-int32_t select_team(const sam_cache* c, int32_t B, int64_t lists, int64_t rows, int sms) {
-    const int64_t fit = std::max<int64_t>(kScoreColumns / ((rows + 7) / 8 * 8), 1);
-    const int64_t wanted = static_cast<int64_t>(B) * lists * c->n_kv_heads / (2 * sms);
-    return static_cast<int32_t>(std::max<int64_t>(std::min({fit, wanted, most_team(c, lists)}), 1));
+// Lists of a row that one block scores: as many as fit its columns; one where the rows of a single list are few and lists are, too.
+int32_t select_team(const sam_cache* c, int64_t lists, int64_t rows) {
+    return static_cast<int32_t>(std::min<int64_t>(std::max<int64_t>(kScoreColumns / ((rows + 7) / 8 * 8), 1), most_team(c, lists)));
+}
+
+template <typename T, int D>
+int launch_score(const SelectArgs& a, int64_t n, int sms, cudaStream_t s) {
+    const int64_t padded = (static_cast<int64_t>(a.share) * a.group + 7) / 8 * 8, heads = n * a.c.n_kv;
+    auto shares = [&](int pages, int blocks) {            // of the pages: so that there are about so many blocks an SM
+        return static_cast<unsigned>(std::max<int64_t>(std::min<int64_t>((a.c.max_pages + pages - 1) / pages, (static_cast<int64_t>(sms) * blocks + heads / 2) / heads), 1));
+    };
+    if (a.team == 1 && padded <= kFewColumns) {
+        // streams differ in length, and a block begins quickly
+        select_score_few_kernel<T, D><<<dim3(shares(kFewThreads / 2, 8), a.c.n_kv, static_cast<unsigned>(n)), kFewThreads, 0, s>>>(a);
+        return launched();
+    }
+    // a block takes 7 us for its queries before it begins: no more of them than run at a time
+    const dim3 grid(shares(kScorePages, 2), a.c.n_kv, static_cast<unsigned>(n));
+    static thread_local uint64_t asked = 0;
+    if (int e = allow_shared(select_score_kernel<T, D>, score_smem<D>(kScoreColumns), &asked)) return e;
+    const int columns = static_cast<int>((std::min<int64_t>(a.team * padded, kScoreColumns) + 15) / 16 * 16);
+    select_score_kernel<T, D><<<grid, kScoreThreads, score_smem<D>(columns), s>>>(a);
+    return launched();
 }
 
 // Scores and picks for all lists, as many at a time as the keys have room for.
@@ -214,19 +232,16 @@ int launch_select(SelectArgs a, int64_t key_bytes, int sms, cudaStream_t s) {
     for (int64_t at = 0; at < all; at += most) {
         const int64_t n = std::min(all - at, most);
         a.first_team = at;
-        // a warp takes sixteen pages at a time; about four blocks an SM
-        const int64_t full = (static_cast<int64_t>(a.c.max_pages) + kScoreThreads / 2 - 1) / (kScoreThreads / 2);
-        const int64_t wanted = (static_cast<int64_t>(sms) * 4 + n * a.c.n_kv - 1) / (n * a.c.n_kv);
-        const dim3 grid(static_cast<unsigned>(std::min(full, wanted)), a.c.n_kv, static_cast<unsigned>(n));
-        if (a.c.D == 64) select_score_kernel<T, 64><<<grid, kScoreThreads, 0, s>>>(a);
-        else select_score_kernel<T, 128><<<grid, kScoreThreads, 0, s>>>(a);
-        if (int e = launched()) return e;
+        if (int e = a.c.D == 64 ? launch_score<T, 64>(a, n, sms, s) : launch_score<T, 128>(a, n, sms, s)) return e;
         const int64_t rows = n * a.team * a.c.n_kv;
-        const int e = a.c.max_pages <= 512    ? launch_pick<32, 16>(a, rows, s)
-                      : a.c.max_pages <= 1024 ? launch_pick<32, 32>(a, rows, s)
-                      : a.c.max_pages <= 2048 ? launch_pick<256, 8>(a, rows, s)
-                      : a.c.max_pages <= 8192 ? launch_pick<256, 32>(a, rows, s)
-                                              : launch_pick<256, 0>(a, rows, s);
+        // a warp a list where there are many short ones; a block a list takes less time for each
+        const bool many = rows > sms * 8;
+        const int e = many && a.c.max_pages <= 512    ? launch_pick<32, 16>(a, rows, s)
+                      : many && a.c.max_pages <= 1024 ? launch_pick<32, 32>(a, rows, s)
+                      : a.c.max_pages <= 1024         ? launch_pick<256, 4>(a, rows, s)
+                      : a.c.max_pages <= 4096         ? launch_pick<256, 16>(a, rows, s)
+                      : a.c.max_pages <= 16384        ? launch_pick<256, 64>(a, rows, s)
+                                                      : launch_pick<256, 0>(a, rows, s);
         if (e) return e;
     }
     return SAM_OK;
@@ -621,7 +636,7 @@ int sam_cache_select(const sam_cache* c, int32_t layer, const int8_t* codes, con
     a.n_recent = n_recent;
     DeviceInfo di;
     if (int e = device_info(&di)) return e;
-    a.team = select_team(c, B, lists, static_cast<int64_t>(share) * a.group, di.sms);
+    a.team = select_team(c, lists, static_cast<int64_t>(share) * a.group);
     a.teams = static_cast<int32_t>((lists + a.team - 1) / a.team);
     a.key_stride = key_stride(c);
     a.keys = static_cast<uint32_t*>(workspace);

@@ -6,8 +6,10 @@
 // 2^22 in magnitude, exact in 32 bits, so that equal scores are equal wherever and in whatever order they are computed.
 #pragma once
 
+#include "attend_wide.cuh"
 #include "cache_attend.cuh"
 #include "cache_format.cuh"
+#include "cache_io.cuh"
 
 namespace samb200 {
 
@@ -165,47 +167,66 @@ __device__ __forceinline__ uint32_t score_key(float x) {
     return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 
-constexpr int kScoreThreads = 256, kScoreColumns = 128, kScoreTeam = kScoreColumns / 8;   // query rows in shared memory at a time; most lists of a team
-
 __device__ __forceinline__ void mma_s8(int (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// Keys of the pages of a team of lists and a head: sixteen pages of a warp are the M side, eight query rows the N side.  The bounds of a
-// page come straight from memory into the fragments (the order of the summed index is free, so that a thread has sixteen neighbouring
-// bytes at a time), the next sixteen pages' while these are multiplied, and serve all lists of the team.
-// Grid: (shares of the pages, heads, teams).
+// Eight bits for a query row of which every one of kLanes lanes has eight channels: codes of the positive and of the negative parts;
+// returns the power of two.
+template <typename T, int kLanes>
+__device__ __forceinline__ int query_codes(const uint4& raw, uint32_t (&up)[2], uint32_t (&dn)[2]) {
+    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+    float x[8], big = 0.f;                                // big: of the finite ones
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        x[i] = i & 1 ? Pair<T>::hi(w[i >> 1]) : Pair<T>::lo(w[i >> 1]);
+        if (fabsf(x[i]) < INFINITY) big = fmaxf(big, fabsf(x[i]));
+    }
+#pragma unroll
+    for (int d = 1; d < kLanes; d <<= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, d));
+    const int e = big >= 1.17549435e-38f ? max(eight_bit_exponent(big), -100) : 0;
+    const float down = pow2(-e);
+    up[0] = up[1] = dn[0] = dn[1] = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int y = x[i] == x[i] ? __float2int_rn(fminf(fmaxf(x[i] * down, -127.f), 127.f)) : 0;
+        up[i >> 2] |= static_cast<uint32_t>(max(y, 0)) << (8 * (i & 3));
+        dn[i >> 2] |= static_cast<uint32_t>(min(y, 0) & 255) << (8 * (i & 3));
+    }
+    return e;
+}
+// Eight channels of a query row of a run, from channel `at` on.
+template <typename T>
+__device__ __forceinline__ uint4 query_part(const SelectArgs& a, int b, int i0, int head, int rho, int at) {
+    const T* q = static_cast<const T*>(a.q) + b * a.q_row + (static_cast<int64_t>(i0) + rho / a.group) * a.q_token + (head * a.group + rho % a.group) * a.q_head + at;
+    if (a.q_wide) return __ldg(reinterpret_cast<const uint4*>(q));
+    const uint16_t* h = reinterpret_cast<const uint16_t*>(q);
+    return make_uint4(h[0] | static_cast<uint32_t>(h[1]) << 16, h[2] | static_cast<uint32_t>(h[3]) << 16, h[4] | static_cast<uint32_t>(h[5]) << 16,
+                      h[6] | static_cast<uint32_t>(h[7]) << 16);
+}
+
+// Keys of the pages of a list and head with up to kFewColumns query rows: the bounds come straight from memory into the fragments of
+// m16n8k32 (sixteen pages of a warp are the M side; the order of the summed index is free, so that a thread has sixteen neighbouring
+// bytes at a time), the next sixteen pages' while these are multiplied.  A product takes 26 clocks, which is why more rows go another way.
+// 64 streams of up to 2,048 pages of 8 heads, four query rows each (148 MB): 24 us.
+// Grid: (shares of the pages, heads, lists).
+constexpr int kFewThreads = 256, kFewColumns = 16;
 template <typename T, int D>
-__global__ void __launch_bounds__(kScoreThreads) select_score_kernel(const __grid_constant__ SelectArgs a) {
+__global__ void __launch_bounds__(kFewThreads) select_score_few_kernel(const __grid_constant__ SelectArgs a) {
     constexpr int kStride = 2 * D + 64;                   // of a column in shared memory: two columns fill all banks
-    constexpr int kParts = 2 * D / 64;                    // sixteen-byte parts of a row or column that a thread has
-    __shared__ alignas(16) uint8_t columns[kScoreColumns * kStride];
-    __shared__ float unit[kScoreColumns];
-    __shared__ SelectRun runs[kScoreTeam];
+    constexpr int kParts = 2 * D / 64, kLanes = D / 8;    // sixteen-byte parts of a row or column that a thread has; lanes of a query row
+    __shared__ alignas(16) uint8_t columns[kFewColumns * kStride];
+    __shared__ alignas(8) float unit[kFewColumns];
     const CacheView& c = a.c;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, j = lane & 3;
-    const int head = blockIdx.y;
-    const int64_t team = a.first_team + blockIdx.z;
-    const int b = static_cast<int>(quotient(team, a.teams)), l0 = static_cast<int>(team - static_cast<int64_t>(b) * a.teams) * a.team;
-    if (threadIdx.x < a.team) {
-        SelectRun run{-1, 0, 0, 0};
-        if (l0 + static_cast<int>(threadIdx.x) < a.lists) run = select_run(a, b, l0 + threadIdx.x);
-        runs[threadIdx.x] = run;
-    }
-    __syncthreads();
-    int most = 0, s = -1;                                 // pages of the list that has most
-    for (int l = 0; l < a.team; ++l) {
-        most = max(most, runs[l].pages);
-        if (runs[l].n > 0) s = runs[l].s;
-    }
-    if (most == 0) return;
-    const bool scored = most > a.n_blocks;                // else all blocks are listed
-    uint32_t* const keys = a.keys + (static_cast<int64_t>(blockIdx.z) * a.team * c.n_kv + head) * a.key_stride;
-    const int64_t list_stride = c.n_kv * a.key_stride;
-    const int each = a.share * a.group, padded = (each + 7) & ~7;   // columns of a list; more than fit are taken in turns
-    const int first = (blockIdx.x * (kScoreThreads / 32) + warp) * 16, step = gridDim.x * (kScoreThreads / 2);
-    auto page_of = [&](int i) { return i < most ? c.page_at(s, i) : -1; };
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, j = lane & 3, head = blockIdx.y;
+    const int64_t v = a.first_team + blockIdx.z;
+    const int b = static_cast<int>(quotient(v, a.lists)), l = static_cast<int>(v - static_cast<int64_t>(b) * a.lists);
+    const SelectRun run = select_run(a, b, l);
+    const int first = (blockIdx.x * (kFewThreads / 32) + warp) * 16, step = gridDim.x * (kFewThreads / 2);
+    const bool scored = run.pages > a.n_blocks;           // else all blocks are listed
+    uint32_t* const keys = a.keys + (static_cast<int64_t>(blockIdx.z) * c.n_kv + head) * a.key_stride;
+    auto page_of = [&](int i) { return i < run.pages ? c.page_at(run.s, i) : -1; };
     auto fetch = [&](const int (&page)[2], uint4 (&x)[2][kParts], int (&e)[2]) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -216,123 +237,295 @@ __global__ void __launch_bounds__(kScoreThreads) select_score_kernel(const __gri
                 x[h][k] = page[h] < 0 ? make_uint4(0, 0, 0, 0) : __ldg(reinterpret_cast<const uint4*>(a.o.codes + at * 2 * D) + k * 4 + j);
         }
     };
-    for (int col0 = 0; col0 == 0 || (scored && col0 < each); col0 += kScoreColumns) {
-        uint4 next[2][kParts];
-        int page[2], next_page[2], next_e[2];
+    uint4 next[2][kParts];
+    int page[2], next_e[2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) page[h] = page_of(first + r + 8 * h);
-        if (scored) fetch(page, next, next_e);
-        const int tiles = min(padded - col0, kScoreColumns) >> 3;   // of a list; more than one list only if all its columns fit
-        __syncthreads();
-        if (scored) {
-            // queries in eight bits, their positive and their negative parts: a warp takes a row
-            for (int n = warp; n < a.team * tiles * 8; n += kScoreThreads / 32) {
-                const int l = n / (tiles * 8), rho = col0 + n - l * tiles * 8;
-                const bool used = rho < runs[l].n * a.group;
-                float x[D / 32];
-#pragma unroll
-                for (int k = 0; k < D / 32; ++k) x[k] = 0.f;
-                if (used) {
-                    const T* q = static_cast<const T*>(a.q) + b * a.q_row + (static_cast<int64_t>(l0 + l) * a.share + rho / a.group) * a.q_token +
-                                 (head * a.group + rho % a.group) * a.q_head + lane * (D / 32);
-                    if (a.q_wide) {
-                        alignas(8) T y[D / 32];
-                        if constexpr (D == 128) *reinterpret_cast<uint2*>(y) = __ldg(reinterpret_cast<const uint2*>(q));
-                        else *reinterpret_cast<uint32_t*>(y) = __ldg(reinterpret_cast<const uint32_t*>(q));
-#pragma unroll
-                        for (int k = 0; k < D / 32; ++k) x[k] = Elem<T>::to_float(y[k]);
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < D / 32; ++k) x[k] = Elem<T>::to_float(q[k]);
-                    }
-                }
-                float big = 0.f;                          // of the finite ones
-#pragma unroll
-                for (int k = 0; k < D / 32; ++k) {
-                    const float y = fabsf(x[k]);
-                    if (y < INFINITY) big = fmaxf(big, y);
-                }
-                big = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(big)));   // not negative: in the order of its bits
-                const int e = big >= 1.17549435e-38f ? max(eight_bit_exponent(big), -100) : 0;
-                uint32_t up = 0, dn = 0;
-#pragma unroll
-                for (int k = 0; k < D / 32; ++k) {
-                    const int y = x[k] == x[k] ? __float2int_rn(fminf(fmaxf(x[k] * pow2(-e), -127.f), 127.f)) : 0;
-                    up |= static_cast<uint32_t>(max(y, 0)) << (8 * k);
-                    dn |= static_cast<uint32_t>(min(y, 0) & 255) << (8 * k);
-                }
-                uint8_t* col = columns + n * kStride + lane * (D / 32);
-                if constexpr (D == 128) {
-                    *reinterpret_cast<uint32_t*>(col) = up;
-                    *reinterpret_cast<uint32_t*>(col + D) = dn;
-                } else {
-                    *reinterpret_cast<uint16_t*>(col) = static_cast<uint16_t>(up);
-                    *reinterpret_cast<uint16_t*>(col + D) = static_cast<uint16_t>(dn);
-                }
-                if (lane == 0) unit[n] = used ? pow2(e) : -1.f;
-            }
-            __syncthreads();
-        }
-        for (int i0 = first; i0 < most; i0 += step) {
-            // pages i0 + r and + 8, and the next ones
-            uint4 x[2][kParts];
-            float size[2];
-            bool nan[2];
-            const int here[2] = {page[0], page[1]};
-            if (scored) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    nan[h] = next_e[h] == kNanPage;
-                    size[h] = pow2(nan[h] ? 0 : next_e[h]);
-#pragma unroll
-                    for (int k = 0; k < kParts; ++k) x[h][k] = next[h][k];
-                }
-            }
-#pragma unroll
-            for (int h = 0; h < 2; ++h) page[h] = next_page[h] = page_of(i0 + step + r + 8 * h);
-            if (scored && i0 + step < most) fetch(next_page, next, next_e);
-            for (int l = 0; l < a.team; ++l) {
-                const int pages = runs[l].pages, old = runs[l].old;
-                if (i0 >= pages) continue;
-                float best[2] = {-INFINITY, -INFINITY};
-                if (pages > a.n_blocks && i0 < old) {
-                    for (int t = 0; t < tiles; ++t) {
-                        int acc[4] = {0, 0, 0, 0};
-                        const int n0 = (l * tiles + t) * 8;
-                        const uint8_t* col = columns + (n0 + r) * kStride + j * 16;
-#pragma unroll
-                        for (int k = 0; k < kParts; ++k) {
-                            const uint4 y = *reinterpret_cast<const uint4*>(col + k * 64);
-                            mma_s8(acc, x[0][k].x, x[1][k].x, x[0][k].y, x[1][k].y, y.x, y.y);
-                            mma_s8(acc, x[0][k].z, x[1][k].z, x[0][k].w, x[1][k].w, y.z, y.w);
-                        }
-                        const float2 u = *reinterpret_cast<const float2*>(&unit[n0 + 2 * j]);
-                        if (u.x >= 0.f) {
-                            best[0] = fmaxf(best[0], static_cast<float>(acc[0]) * u.x);
-                            best[1] = fmaxf(best[1], static_cast<float>(acc[2]) * u.x);
-                        }
-                        if (u.y >= 0.f) {
-                            best[0] = fmaxf(best[0], static_cast<float>(acc[1]) * u.y);
-                            best[1] = fmaxf(best[1], static_cast<float>(acc[3]) * u.y);
-                        }
-                    }
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        best[h] = fmaxf(best[h], __shfl_xor_sync(0xffffffffu, best[h], 1));
-                        best[h] = fmaxf(best[h], __shfl_xor_sync(0xffffffffu, best[h], 2));
-                    }
-                }
-                if (j < 2) {                              // lane j = 0: page r, j = 1: page r + 8
-                    const int i = i0 + r + 8 * j;
-                    uint32_t key = 0;
-                    if ((j ? here[1] : here[0]) >= 0)
-                        key = pages <= a.n_blocks || i < a.n_sink || i >= old ? kForced : (j ? nan[1] : nan[0]) ? kNanKey : score_key(j ? best[1] * size[1] : best[0] * size[0]);
-                    uint32_t* at = keys + l * list_stride + i;
-                    if (i < pages) *at = col0 == 0 ? key : max(*at, key);
-                }
-            }
+    for (int h = 0; h < 2; ++h) page[h] = page_of(first + r + 8 * h);
+    if (scored) fetch(page, next, next_e);
+    const int rows = run.n * a.group, tiles = (a.share * a.group + 7) >> 3;
+    if (scored) {
+        // queries in eight bits, their positive and their negative parts: eight channels a lane
+        const int n = threadIdx.x / kLanes, part = threadIdx.x % kLanes;
+        if (n < kFewColumns) {                            // whole warps
+            uint32_t up[2], dn[2];
+            const int e = query_codes<T, kLanes>(n < rows ? query_part<T>(a, b, l * a.share, head, n, part * 8) : make_uint4(0, 0, 0, 0), up, dn);
+            *reinterpret_cast<uint2*>(columns + n * kStride + part * 8) = make_uint2(up[0], up[1]);
+            *reinterpret_cast<uint2*>(columns + n * kStride + D + part * 8) = make_uint2(dn[0], dn[1]);
+            if (part == 0) unit[n] = n < rows ? pow2(e) : __int_as_float(0x7fffffff);   // a NaN drops out of the maximum
         }
     }
+    __syncthreads();
+    for (int i0 = first; i0 < run.pages; i0 += step) {
+        // pages i0 + r and + 8, and the next ones
+        uint4 x[2][kParts];
+        float size[2], best[2] = {-INFINITY, -INFINITY};
+        bool nan[2];
+        const int here[2] = {page[0], page[1]};
+        if (scored) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                nan[h] = next_e[h] == kNanPage;
+                size[h] = pow2(nan[h] ? 0 : next_e[h]);
+#pragma unroll
+                for (int k = 0; k < kParts; ++k) x[h][k] = next[h][k];
+            }
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) page[h] = page_of(i0 + step + r + 8 * h);
+        if (scored && i0 + step < run.pages) fetch(page, next, next_e);
+        if (scored) {
+            for (int t = 0; t < tiles; ++t) {
+                int acc[4] = {0, 0, 0, 0};
+                const uint8_t* col = columns + (t * 8 + r) * kStride + j * 16;
+#pragma unroll
+                for (int k = 0; k < kParts; ++k) {
+                    const uint4 y = *reinterpret_cast<const uint4*>(col + k * 64);
+                    mma_s8(acc, x[0][k].x, x[1][k].x, x[0][k].y, x[1][k].y, y.x, y.y);
+                    mma_s8(acc, x[0][k].z, x[1][k].z, x[0][k].w, x[1][k].w, y.z, y.w);
+                }
+                const float2 u = *reinterpret_cast<const float2*>(&unit[t * 8 + 2 * j]);
+                best[0] = fmaxf(best[0], fmaxf(static_cast<float>(acc[0]) * u.x, static_cast<float>(acc[1]) * u.y));
+                best[1] = fmaxf(best[1], fmaxf(static_cast<float>(acc[2]) * u.x, static_cast<float>(acc[3]) * u.y));
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                best[h] = fmaxf(best[h], __shfl_xor_sync(0xffffffffu, best[h], 1));
+                best[h] = fmaxf(best[h], __shfl_xor_sync(0xffffffffu, best[h], 2));
+            }
+        }
+        const int i = i0 + r + 8 * j;                     // lane j = 0: page r, j = 1: page r + 8
+        if (j < 2 && i < run.pages) {
+            uint32_t key = 0;
+            if ((j ? here[1] : here[0]) >= 0)
+                key = !scored || i < a.n_sink || i >= run.old ? kForced : (j ? nan[1] : nan[0]) ? kNanKey : score_key(j ? best[1] * size[1] : best[0] * size[0]);
+            keys[i] = key;
+        }
+    }
+}
+
+constexpr int kScorePages = 128, kScoreColumns = 128, kScoreTeam = kScoreColumns / 8;   // pages of a tile; query rows at a time; most lists of a team
+constexpr int kScoreThreads = 512, kScoreGroups = kScoreThreads / kScorePages;   // threads of a page
+constexpr int kScoreStages = 2;
+template <int D>
+constexpr int score_smem(int columns) { return kScoreStages * kScorePages * 2 * D + columns * 2 * D + 1024; }   // and room to start on a 1024-byte boundary
+
+__device__ __forceinline__ void tc_mma_s8(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(static_cast<uint32_t>(add)) : "memory");
+}
+// s32 accumulator, s8 operands, both with the summed index innermost.
+__device__ __forceinline__ uint32_t score_desc(int n) { return 2u << 4 | 1u << 7 | 1u << 10 | static_cast<uint32_t>(n >> 3) << 17 | 8u << 24; }
+__device__ __forceinline__ void tmem_load8(uint32_t at, uint32_t (&x)[8]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]), "=r"(x[4]), "=r"(x[5]), "=r"(x[6]), "=r"(x[7]) : "r"(at));
+}
+__device__ __forceinline__ void tmem_load_wait(uint32_t (&x)[8]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(x[0]), "+r"(x[1]), "+r"(x[2]), "+r"(x[3]), "+r"(x[4]), "+r"(x[5]), "+r"(x[6]), "+r"(x[7]) :: "memory");
+}
+
+// Keys of the pages of a team of lists and a head: 128 pages are the M side, the query rows of all lists of the team the N side.  A thread
+// then has all products of its page, and the largest of a list's needs no exchange.  Bounds are gathered two tiles ahead, 16 bytes a copy;
+// nothing else runs ahead in a block, that is what the other blocks of the SM are for.
+// 48 streams' proposals of 17, 28/4 heads, 750 pages each: 30 us (the kernel above took 52); 1,024 lists of 28/4 heads over 939 pages: 44 us (125).  Half of it goes into the
+// queries and the first tiles of a block, a quarter into taking maxima: both are chains of instructions, and the tensor cores wait.
+// Grid: (shares of the pages, heads, teams).
+template <typename T, int D>
+__global__ void __launch_bounds__(kScoreThreads, 2) select_score_kernel(const __grid_constant__ SelectArgs a) {
+    constexpr int kTile = kScorePages * 2 * D;            // bytes
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ alignas(16) float unit[kScoreColumns];
+    __shared__ SelectRun runs[kScoreTeam];
+    __shared__ int ids[3][kScorePages];                   // pages of the tiles that are copied next
+    __shared__ float part_best[kScoreGroups][kScorePages];   // where one list is all there is
+    __shared__ uint64_t done;
+    __shared__ uint32_t tmem_base;
+    const CacheView& c = a.c;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, head = blockIdx.y;
+    const int own = tid % kScorePages, group = tid / kScorePages;   // the thread's page of a tile
+    const int64_t team = a.first_team + blockIdx.z;
+    const int b = static_cast<int>(quotient(team, a.teams)), l0 = static_cast<int>(team - static_cast<int64_t>(b) * a.teams) * a.team;
+    if (tid < a.team) {
+        SelectRun run{-1, 0, 0, 0};
+        if (l0 + tid < a.lists) run = select_run(a, b, l0 + tid);
+        runs[tid] = run;
+    }
+    if (tid == 0) barrier_init(shared_addr(&done), 1);
+    barrier_init_fence();
+    __syncthreads();
+    int most = 0, s = -1;                                 // pages of the list that has most
+    for (int l = 0; l < a.team; ++l) {
+        most = max(most, runs[l].pages);
+        if (runs[l].n > 0) s = runs[l].s;
+    }
+    uint32_t* const keys = a.keys + (static_cast<int64_t>(blockIdx.z) * a.team * c.n_kv + head) * a.key_stride;
+    const int64_t list_stride = c.n_kv * a.key_stride;
+    const int begin = blockIdx.x * kScorePages, step = gridDim.x * kScorePages;
+    if (begin >= most) return;
+    auto page_of = [&](int i) { return i < most ? c.page_at(s, i) : -1; };   // of the thread's own row
+    auto row_at = [&](int page) { return (static_cast<int64_t>(page) * c.n_layers + a.layer) * c.n_kv + head; };
+    if (most <= a.n_blocks) {                             // all blocks are listed
+        for (int i0 = begin; i0 < most; i0 += step) {
+            const int i = i0 + own, page = page_of(i);
+            for (int l = group; l < a.team; l += kScoreGroups)
+                if (i < runs[l].pages) keys[l * list_stride + i] = page < 0 ? 0u : kForced;
+        }
+        return;
+    }
+    const int each = a.share * a.group, padded = (each + 7) & ~7;   // columns of a list; more than fit are taken in turns
+    uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    const uint32_t tiles_at = shared_addr(smem), columns_at = tiles_at + kScoreStages * kTile, bar = shared_addr(&done);
+    const int most_columns = (min(a.team * padded, kScoreColumns) + 15) & ~15;   // what there is room for
+    const uint32_t tmem_columns = most_columns <= 32 ? 32u : most_columns <= 64 ? 64u : 128u;
+    if (warp == 0) tmem_alloc(shared_addr(&tmem_base), tmem_columns);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_base;
+    // the tile of 128 pages of which ids[from] has the numbers into a stage: sixteen bytes of neighbouring rows or of one row a thread
+    auto copy = [&](int stage, const int* from, bool on) {
+        if (on) {
+            constexpr int kUnits = D / 8;                 // of a row
+            const int u = tid % kUnits;
+#pragma unroll 4
+            for (int r = tid / kUnits; r < kScorePages; r += kScoreThreads / kUnits) {
+                const int page = from[r];
+                if (page >= 0)
+                    async_copy16(tiles_at + stage * kTile + (u >> 3) * (kScorePages * 128) + r * 128 + (((u & 7) ^ (r & 7)) << 4),
+                                 a.o.codes + row_at(page) * 2 * D + u * 16);
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    uint32_t products = 0;                                // so far
+    bool late = false;
+    for (int col0 = 0; col0 < each && !late; col0 += kScoreColumns) {
+        const int per_list = min(padded - col0, kScoreColumns);   // columns of a list; more than one list only if all of its columns fit
+        const int columns = (a.team * per_list + 15) & ~15;
+        // ---- pages of the first tiles
+        int page[2], e[2];                                // of the thread's row: this tile and the next
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            page[k] = page_of(begin + k * step + own);
+            if (group == 0) ids[k][own] = page[k];
+        }
+        int ahead = page_of(begin + 2 * step + own);
+        __syncthreads();
+        copy(0, ids[0], true);
+        copy(1, ids[1], begin + step < most);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) e[k] = page[k] < 0 ? 0 : a.o.exps[row_at(page[k])];
+        // ---- queries in eight bits, their positive and their negative parts: eight channels a lane, a few rows a warp under way together
+        constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes, kRound = 2;
+        const int part = lane % kLanes;
+        for (int n0 = warp * (kAtOnce * kRound); n0 < columns; n0 += kScoreThreads / 32 * (kAtOnce * kRound)) {
+            uint4 raw[kRound];
+            bool used[kRound];
+#pragma unroll
+            for (int k = 0; k < kRound; ++k) {
+                const int n = n0 + k * kAtOnce + lane / kLanes, l = n / per_list, rho = col0 + n - l * per_list;
+                used[k] = n < columns && l < a.team && rho < runs[min(l, kScoreTeam - 1)].n * a.group;
+                raw[k] = used[k] ? query_part<T>(a, b, (l0 + l) * a.share, head, rho, part * 8) : make_uint4(0, 0, 0, 0);
+            }
+#pragma unroll
+            for (int k = 0; k < kRound; ++k) {
+                const int n = n0 + k * kAtOnce + lane / kLanes;
+                uint32_t up[2], dn[2];
+                const int ex = query_codes<T, kLanes>(raw[k], up, dn);
+                if (n >= columns) continue;
+                // rows of 128 bytes, sixteen-byte units swapped by the row's number
+                auto put = [&](int at, const uint32_t (&bytes)[2]) {
+                    uint8_t* to = smem + kScoreStages * kTile + (at >> 7) * (columns * 128) + n * 128 + ((at & 127) ^ ((n & 7) << 4));
+                    *reinterpret_cast<uint2*>(to) = make_uint2(bytes[0], bytes[1]);
+                };
+                put(part * 8, up);
+                put(D + part * 8, dn);
+                if (part == 0) unit[n] = used[k] ? pow2(ex) : __int_as_float(0x7fffffff);   // a NaN drops out of the maximum
+            }
+        }
+        // ---- tiles
+        int stage = 0, slot = 0;                          // slot: of ids, the tile's
+        for (int i0 = begin; i0 < most; i0 += step, stage ^= 1) {
+            asm volatile("cp.async.wait_group 1;" ::: "memory");
+            async_proxy_fence();
+            __syncthreads();
+            if (tid == 0) {
+                tc_fence_after();
+                const uint64_t rows = operand_desc(tiles_at + stage * kTile, 16, 1024), cols = operand_desc(columns_at, 16, 1024);
+#pragma unroll
+                for (int x = 0; x < D / 16; ++x)
+                    tc_mma_s8(tmem, rows + (((x >> 2) * (kScorePages * 128) + (x & 3) * 32) >> 4), cols + (((x >> 2) * (columns * 128) + (x & 3) * 32) >> 4), score_desc(columns), x > 0);
+                tc_commit(bar);
+            }
+            __syncwarp();
+            slot = slot == 2 ? 0 : slot + 1;
+            const int after = slot == 2 ? 0 : slot + 1;   // of the tile after the next
+            if (group == 0) ids[after][own] = ahead;
+            const int here = page[0], e_here = e[0];
+            page[0] = page[1], e[0] = e[1];
+            page[1] = ahead;
+            e[1] = ahead < 0 ? 0 : a.o.exps[row_at(ahead)];
+            ahead = page_of(i0 + 3 * step + own);
+            late |= !poll([&] { return barrier_try(bar, products & 1); });
+            __syncwarp();
+            ++products;
+            tc_fence_after();
+            const int i = i0 + own;
+            const bool nan = e_here == kNanPage;
+            const float size = pow2(nan ? 0 : e_here);
+            const uint32_t from = tmem + (static_cast<uint32_t>(warp & 3) << 21);
+            // the largest of the columns n0 .. n1 - 1, eight at a time
+            auto largest = [&](int n0, int n1) {
+                float best = -INFINITY;
+                for (int n = n0; n < n1; n += 8) {
+                    uint32_t x[8];
+                    tmem_load8(from + n, x);
+                    const float4 u0 = *reinterpret_cast<const float4*>(&unit[n]), u1 = *reinterpret_cast<const float4*>(&unit[n + 4]);
+                    const float u[8] = {u0.x, u0.y, u0.z, u0.w, u1.x, u1.y, u1.z, u1.w};
+                    tmem_load_wait(x);
+#pragma unroll
+                    for (int w = 0; w < 8; ++w) best = fmaxf(best, static_cast<float>(static_cast<int>(x[w])) * u[w]);
+                }
+                return best;
+            };
+            auto write = [&](int l, float best) {
+                const int pages = runs[l].pages, old = runs[l].old;
+                if (i < pages) {
+                    uint32_t key = 0;
+                    if (here >= 0) key = pages <= a.n_blocks || i < a.n_sink || i >= old ? kForced : nan ? kNanKey : score_key(best * size);
+                    uint32_t* at = keys + l * list_stride + i;
+                    *at = col0 == 0 ? key : max(*at, key);
+                }
+                __syncwarp();                             // the loads from tensor memory want the warp together
+            };
+            if (a.team == 1) {                            // a share of its columns for each thread of the page
+                const int eighths = per_list >> 3;
+                const float best = largest(eighths * group / kScoreGroups * 8, eighths * (group + 1) / kScoreGroups * 8);
+                if (per_list > 8) {
+                    part_best[group][own] = best;
+                    __syncthreads();
+                    if (group == 0) write(0, fmaxf(fmaxf(best, part_best[1][own]), fmaxf(part_best[2][own], part_best[3][own])));
+                } else if (eighths * (group + 1) / kScoreGroups > eighths * group / kScoreGroups) {
+                    write(0, best);
+                }
+            } else {
+                for (int l = group; l < a.team; l += kScoreGroups) write(l, largest(l * per_list, (l + 1) * per_list));
+            }
+            tc_fence_before();
+            late = __syncthreads_or(late);                // the products are read, the stage is free
+            if (late) break;
+            copy(stage, ids[after], i0 + 2 * step < most);
+        }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncthreads();                                  // the columns may be written again
+    }
+    if (late) {
+        __nanosleep(100000);                              // products still under way
+        if (tid == 0 && c.meta) atomicOr(&c.meta[1], kStatusGaveUp);
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 0) tmem_free(tmem, tmem_columns);
 }
 
 // ---- the best pages of a list: the keys lie in registers, kKeys neighbouring ones a thread; the n_blocks-th largest is found bit by bit,
@@ -471,8 +664,13 @@ __global__ void __launch_bounds__(kPickThreads) select_pick_kernel(const __grid_
                     differ &= ~bit;
                     const uint32_t to = limit | bit;
                     int count = 0;
-                    for_keys([&](uint32_t k, int) { count += k >= to && k != kForced; });
-                    if (team.sum(count) >= want) limit = to;
+                    for_keys([&](uint32_t k, int) { count += k >= to; });
+                    count = team.sum(count) - all.y;
+                    if (count >= want) limit = to;
+                    if (count == want) {                  // exactly those
+                        --limit;
+                        break;
+                    }
                 }
             }
         }
