@@ -259,7 +259,9 @@ int check_bounds(const int8_t* codes, const int8_t* exps) { return codes && exps
 
 template <typename T>
 int launch_turn(const TurnArgs& a, cudaStream_t s) {
-    append_rotated_kernel<T><<<dim3((a.Q + a.tokens - 1) / a.tokens, a.B), kTurnThreads, 0, s>>>(a);
+    const dim3 grid((a.Q + a.tokens - 1) / a.tokens, a.B);
+    if (a.c.D == 64) append_rotated_kernel<T, 64><<<grid, kTurnThreads, 0, s>>>(a);
+    else append_rotated_kernel<T, 128><<<grid, kTurnThreads, 0, s>>>(a);
     return launched();
 }
 
@@ -554,7 +556,7 @@ int sam_cache_append_rotated(const sam_cache* c, int32_t layer, const void* q, i
     a.interleaved = rope->interleaved != 0;
     // more tokens share a CTA once there are enough CTAs; unit numbers stay below 2^16, where the multiplier divides exactly
     const int32_t heads = H + 2 * c->n_kv_heads;
-    a.tokens = static_cast<int32_t>(std::min<int64_t>({int64_t(kTurnTokens), std::max<int64_t>(1, static_cast<int64_t>(B) * Q / (di.sms * 4)), 65535 / heads}));
+    a.tokens = static_cast<int32_t>(std::min<int64_t>({int64_t(kTurnTokens), std::max<int64_t>(1, static_cast<int64_t>(B) * Q / (di.sms * 32)), 65535 / heads}));
     a.magic = static_cast<uint32_t>(((int64_t(1) << 32) + heads - 1) / heads);
     auto wide = [](const void* p, const KvStrides& t) { return aligned(p, 16) && (t.row | t.token | t.head) % 8 == 0; };
     a.q_wide = wide(q, a.qs);

@@ -5,15 +5,21 @@
 // to round is the fraction's top 32 bits to a float, 2^-25 of a half turn.  Products and sums are in 32 bits; a query is rounded once, to its
 // own type, and a key once, to its code: it does not pass through 16 bits in between.
 //
-// A CTA takes a few tokens: their sines and cosines go to shared memory once and serve all heads.  Then a thread takes 32
-// channels of a head: two blocks of 16, which hold both halves of their pairs.
+// A CTA takes a few tokens: their sines and cosines go to shared memory once and serve all heads.  Then a thread takes two pieces
+// of eight channels of a head, which hold both halves of their pairs; neighbouring threads take neighbouring pieces, so that loads and stores
+// fill sectors, and share the scale of their sixteen channels.
+//
+// 256 streams of up to 17 tokens, 32/8 heads of 128 (80 MB): 27 us; 20,000 tokens, 28/4 heads (338 MB): 70 us, 4.8 TB/s.  Bound by
+// instructions: 280 for the sixteen channels of a thread, 0.7 of the issue slots, most of them to find out where a unit lies.  Tried: two
+// blocks of 16 channels a thread (half-filled sectors: 29 and 74 us), the next unit's loads ahead of this one's products (30 and 84), a
+// thread that keeps to its channels token after token (29 and 85: keys and values become a chain of a few microseconds).
 #pragma once
 
 #include "cache_io.cuh"
 
 namespace samb200 {
 
-constexpr int kTurnThreads = 256, kTurnTokens = 8;   // most tokens of a CTA
+constexpr int kTurnThreads = 128, kTurnTokens = 8, kTurnCtasPerSm = 10;   // most tokens of a CTA
 
 struct TurnArgs {
     CacheView c;
@@ -32,61 +38,56 @@ struct TurnArgs {
     bool q_wide, k_wide, o_wide;
 };
 
-// Sixteen 32-bit values -> codes and a scale byte.  The quotient by the scale is a product with its reciprocal, off by less than two
-// units in the last place: rounded to 22 bits, one that is a tie between two codes is that tie (ties have three bits).
-__device__ __forceinline__ uint2 quantise_block32(const float (&x)[16], int exp, uint8_t* scale) {
-    float big = 0.f;
-    bool nan = false;
+// Eight 32-bit values of a block whose other eight the neighbouring lane has -> four bytes of codes, and the block's scale byte.  The
+// quotient by the scale is a product with its reciprocal, off by less than two units in the last place: rounded to 22 bits, one that is a
+// tie between two codes is that tie (ties have three bits).
+__device__ __forceinline__ uint32_t quantise_half(const float (&x)[8], int exp, uint8_t* scale) {
+    uint32_t big = 0;                                     // magnitudes in the order of their bits, NaN above all
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        big = fmaxf(big, fabsf(x[i]));
-        nan |= x[i] != x[i];
-    }
+    for (int i = 0; i < 8; ++i) big = max(big, __float_as_uint(x[i]) & 0x7fffffffu);
+    big = max(big, __shfl_xor_sync(3u << (threadIdx.x & 30), big, 1));
     const float down = pow2(-exp);
-    const uint8_t s8 = nan ? 0x7f : float_to_e4m3(__fdiv_rn(big * down, 6.f));
+    const bool nan = big > 0x7f800000u;
+    const uint8_t s8 = nan ? 0x7f : float_to_e4m3(__fdiv_rn(__uint_as_float(big) * down, 6.f));
     *scale = s8;
-    if (nan || s8 == 0) return make_uint2(0, 0);
+    if (nan || s8 == 0) return 0;
     const float r = __frcp_rn(e4m3_to_float(s8)) * down;
     auto rounded = [&](float y) { return __uint_as_float((__float_as_uint(y * r) + 2u) & ~3u); };
-    uint32_t byte[8];
+    uint32_t codes = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) byte[i] = float2_to_e2m1(rounded(x[2 * i]), rounded(x[2 * i + 1]));
-    return make_uint2(byte[0] | byte[1] << 8 | byte[2] << 16 | byte[3] << 24, byte[4] | byte[5] << 8 | byte[6] << 16 | byte[7] << 24);
+    for (int i = 0; i < 4; ++i) codes |= float2_to_e2m1(rounded(x[2 * i]), rounded(x[2 * i + 1])) << (8 * i);
+    return codes;
 }
 
+// Eight channels, by ordinary loads: the turned queries may take the place of the queries.
 template <typename T>
-__device__ __forceinline__ void store_block(T* p, bool wide, const uint32_t (&x)[8]) {
+__device__ __forceinline__ uint4 load_piece(const T* p, bool wide) {
+    if (wide) return *reinterpret_cast<const uint4*>(p);
+    const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
+    return make_uint4(h[0] | static_cast<uint32_t>(h[1]) << 16, h[2] | static_cast<uint32_t>(h[3]) << 16, h[4] | static_cast<uint32_t>(h[5]) << 16,
+                      h[6] | static_cast<uint32_t>(h[7]) << 16);
+}
+template <typename T>
+__device__ __forceinline__ void store_piece(T* p, bool wide, const float (&x)[8]) {
+    const uint4 y = make_uint4(Pair<T>::pack(x[0], x[1]), Pair<T>::pack(x[2], x[3]), Pair<T>::pack(x[4], x[5]), Pair<T>::pack(x[6], x[7]));
     if (wide) {
-        reinterpret_cast<uint4*>(p)[0] = make_uint4(x[0], x[1], x[2], x[3]);
-        reinterpret_cast<uint4*>(p)[1] = make_uint4(x[4], x[5], x[6], x[7]);
+        *reinterpret_cast<uint4*>(p) = y;
     } else {
         uint16_t* h = reinterpret_cast<uint16_t*>(p);
+        const uint32_t w[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            h[2 * i] = static_cast<uint16_t>(x[i]);
-            h[2 * i + 1] = static_cast<uint16_t>(x[i] >> 16);
+        for (int i = 0; i < 4; ++i) {
+            h[2 * i] = static_cast<uint16_t>(w[i]);
+            h[2 * i + 1] = static_cast<uint16_t>(w[i] >> 16);
         }
     }
 }
 
-// Sixteen elements by ordinary loads: the turned queries may take the place of the queries.
-template <typename T>
-__device__ __forceinline__ void load_block_in_place(const T* p, bool wide, uint32_t (&x)[8]) {
-    if (wide) {
-        const uint4 a = reinterpret_cast<const uint4*>(p)[0], b = reinterpret_cast<const uint4*>(p)[1];
-        x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w;
-        x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
-    } else {
-        const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = h[2 * i] | static_cast<uint32_t>(h[2 * i + 1]) << 16;
-    }
-}
-
 // Grid: (runs of tokens, rows).
-template <typename T>
-__global__ void __launch_bounds__(kTurnThreads) append_rotated_kernel(const __grid_constant__ TurnArgs a) {
-    __shared__ float2 turn[kTurnTokens][64];            // cosine, sine
+template <typename T, int D>
+__global__ void __launch_bounds__(kTurnThreads, kTurnCtasPerSm) append_rotated_kernel(const __grid_constant__ TurnArgs a) {
+    constexpr int kUnits = D / 16;                        // of a head
+    __shared__ alignas(16) float2 turn[kTurnTokens][D / 2];   // cosine, sine
     const CacheView& c = a.c;
     const int b = blockIdx.y;
     const int s = c.stream_of(a.streams, b);
@@ -102,13 +103,17 @@ __global__ void __launch_bounds__(kTurnThreads) append_rotated_kernel(const __gr
         turn[t][f] = make_float2(y.x * a.factor, y.y * a.factor);
     }
     __syncthreads();
-    const int log_d = c.D == 128 ? 2 : 1, heads = a.H + 2 * c.n_kv, turned = a.rotary >> 5;   // units of a head; of them turned
-    for (int e = threadIdx.x; e < (here * heads) << log_d; e += kTurnThreads) {
-        const uint32_t g = e >> log_d, t = __umulhi(g, a.magic);
-        const int head = g - t * heads, u = e & ((1 << log_d) - 1), i = i0 + t;
-        const bool on = i < n, is_q = head < a.H, is_v = head >= a.H + c.n_kv, turns = !is_v && u < turned;
-        // the unit's two blocks
-        const int block0 = turns && !a.interleaved ? u : 2 * u, block1 = turns && !a.interleaved ? u + turned : 2 * u + 1;
+    const int heads = a.H + 2 * c.n_kv, turned = a.rotary >> 4;   // units of a head that hold pairs of halves
+    for (int e = threadIdx.x; e < here * heads * kUnits; e += kTurnThreads) {
+        const uint32_t g = e / kUnits, t = __umulhi(g, a.magic);
+        const int head = g - t * heads, u = e % kUnits, i = i0 + t;
+        const bool on = i < n, is_q = head < a.H, is_v = head >= a.H + c.n_kv;
+        // the unit's two pieces of eight channels
+        int piece0 = u, piece1 = u + kUnits;
+        if (!a.interleaved) {
+            piece0 = u < turned ? u : u + turned;
+            piece1 = u < turned ? u + turned : u + kUnits;
+        }
         uint8_t* tile = nullptr;
         const int64_t at = static_cast<int64_t>(len) + i;
         const int slot = static_cast<int>(at) & (c.page_tokens() - 1), kv = is_v ? head - a.H - c.n_kv : head - a.H;
@@ -118,68 +123,65 @@ __global__ void __launch_bounds__(kTurnThreads) append_rotated_kernel(const __gr
             if (page < 0) continue;
             tile = c.tile(page, a.layer, kv, slot);
         }
-        uint32_t x0[8] = {}, x1[8] = {};
+        uint4 r0 = make_uint4(0, 0, 0, 0), r1 = r0;
         if (on) {
             const T* src = is_q ? static_cast<const T*>(a.q) + b * a.qs.row + i * a.qs.token + head * a.qs.head
                                 : static_cast<const T*>(is_v ? a.v : a.k) + b * a.ks.row + i * a.ks.token + kv * a.ks.head;
-            load_block_in_place(src + block0 * 16, is_q ? a.q_wide : a.k_wide, x0);
-            load_block_in_place(src + block1 * 16, is_q ? a.q_wide : a.k_wide, x1);
+            r0 = load_piece(src + piece0 * 8, is_q ? a.q_wide : a.k_wide);
+            r1 = load_piece(src + piece1 * 8, is_q ? a.q_wide : a.k_wide);
         }
-        if (!is_v) {
-            float y0[16], y1[16];
+        const uint32_t w0[4] = {r0.x, r0.y, r0.z, r0.w}, w1[4] = {r1.x, r1.y, r1.z, r1.w};
+        float y0[8], y1[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                y0[2 * k] = Pair<T>::lo(x0[k]), y0[2 * k + 1] = Pair<T>::hi(x0[k]);
-                y1[2 * k] = Pair<T>::lo(x1[k]), y1[2 * k + 1] = Pair<T>::hi(x1[k]);
-            }
-            if (turns && on) {
-                const float2* w = turn[t] + u * 16;
-                if (a.interleaved) {
+        for (int k = 0; k < 4; ++k) {
+            y0[2 * k] = Pair<T>::lo(w0[k]), y0[2 * k + 1] = Pair<T>::hi(w0[k]);
+            y1[2 * k] = Pair<T>::lo(w1[k]), y1[2 * k + 1] = Pair<T>::hi(w1[k]);
+        }
+        if (on && !is_v) {
+            if (a.interleaved) {
+                auto turn_pairs = [&](float (&y)[8], int piece) {
+                    if (piece >= 2 * turned) return;
+                    const float4* w = reinterpret_cast<const float4*>(turn[t] + piece * 4);   // two angles each
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const float2 r0 = w[k], r1 = w[8 + k];
-                        const float p0 = y0[2 * k], p1 = y0[2 * k + 1], p2 = y1[2 * k], p3 = y1[2 * k + 1];
-                        y0[2 * k] = p0 * r0.x - p1 * r0.y;
-                        y0[2 * k + 1] = p1 * r0.x + p0 * r0.y;
-                        y1[2 * k] = p2 * r1.x - p3 * r1.y;
-                        y1[2 * k + 1] = p3 * r1.x + p2 * r1.y;
+                    for (int k = 0; k < 2; ++k) {
+                        const float4 r = w[k];
+                        const float p0 = y[4 * k], p1 = y[4 * k + 2];
+                        y[4 * k] = p0 * r.x - y[4 * k + 1] * r.y;
+                        y[4 * k + 1] = y[4 * k + 1] * r.x + p0 * r.y;
+                        y[4 * k + 2] = p1 * r.z - y[4 * k + 3] * r.w;
+                        y[4 * k + 3] = y[4 * k + 3] * r.z + p1 * r.w;
                     }
-                } else {
+                };
+                turn_pairs(y0, piece0);
+                turn_pairs(y1, piece1);
+            } else if (u < turned) {
+                const float4* w = reinterpret_cast<const float4*>(turn[t] + u * 8);
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) {
-                        const float2 r = w[k];
-                        const float p0 = y0[k], p1 = y1[k];
-                        y0[k] = p0 * r.x - p1 * r.y;
-                        y1[k] = p1 * r.x + p0 * r.y;
-                    }
+                for (int k = 0; k < 8; k += 2) {
+                    const float4 r = w[k >> 1];
+                    const float p0 = y0[k], p1 = y0[k + 1];
+                    y0[k] = p0 * r.x - y1[k] * r.y;
+                    y1[k] = y1[k] * r.x + p0 * r.y;
+                    y0[k + 1] = p1 * r.z - y1[k + 1] * r.w;
+                    y1[k + 1] = y1[k + 1] * r.z + p1 * r.w;
                 }
             }
-            if (is_q) {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    x0[k] = Pair<T>::pack(y0[2 * k], y0[2 * k + 1]);
-                    x1[k] = Pair<T>::pack(y1[2 * k], y1[2 * k + 1]);
-                }
-                T* out = static_cast<T*>(a.q_out) + b * a.os.row + i * a.os.token + head * a.os.head;
-                store_block(out + block0 * 16, a.o_wide, x0);
-                store_block(out + block1 * 16, a.o_wide, x1);
-                continue;
-            }
-            uint8_t s0, s1;
-            uint8_t* codes = tile + (slot & 15) * (c.D >> 1);
-            uint8_t* scales = tile + 16 * c.D + (slot & 15) * (c.D >> 4);
-            *reinterpret_cast<uint2*>(codes + block0 * 8) = quantise_block32(y0, c.k_exp, &s0);
-            *reinterpret_cast<uint2*>(codes + block1 * 8) = quantise_block32(y1, c.k_exp, &s1);
-            scales[block0] = s0;
-            scales[block1] = s1;
+        }
+        if (is_q) {
+            T* out = static_cast<T*>(a.q_out) + b * a.os.row + i * a.os.token + head * a.os.head;
+            store_piece(out + piece0 * 8, a.o_wide, y0);
+            store_piece(out + piece1 * 8, a.o_wide, y1);
         } else {
             uint8_t s0, s1;
-            uint8_t* codes = tile + 8 * c.D + (slot & 15) * (c.D >> 1);
-            uint8_t* scales = tile + 17 * c.D + (slot & 15) * (c.D >> 4);
-            *reinterpret_cast<uint2*>(codes + block0 * 8) = quantise_block<T>(x0, c.v_exp, &s0);
-            *reinterpret_cast<uint2*>(codes + block1 * 8) = quantise_block<T>(x1, c.v_exp, &s1);
-            scales[block0] = s0;
-            scales[block1] = s1;
+            uint8_t* codes = tile + (is_v ? 8 * D : 0) + (slot & 15) * (D / 2);
+            uint8_t* scales = tile + (is_v ? 17 : 16) * D + (slot & 15) * (D / 16);
+            const int exp = is_v ? c.v_exp : c.k_exp;
+            *reinterpret_cast<uint32_t*>(codes + piece0 * 4) = quantise_half(y0, exp, &s0);
+            *reinterpret_cast<uint32_t*>(codes + piece1 * 4) = quantise_half(y1, exp, &s1);
+            if (!(u & 1)) {
+                scales[piece0 >> 1] = s0;
+                scales[piece1 >> 1] = s1;
+            }
         }
     }
 }
