@@ -707,7 +707,7 @@ class SamCache:
             setattr(self, name, t)
         n_scratch = sam_cache_scratch_bytes(n_streams, n_pages)
         self.scratch = self._empty(n_scratch, torch.uint8, device, stream)
-        self.n_streams, self.n_kv_heads, self.head_dim = n_streams, n_kv_heads, head_dim
+        self.n_streams, self.n_kv_heads, self.head_dim, self.page_tokens = n_streams, n_kv_heads, head_dim, page_tokens
         self._struct = _CacheStruct(*(_dev(getattr(self, n)) for n in ("pages", *self.BOOKS, "scratch")), n_scratch,
                                     n_pages, page_tokens, n_streams, max_pages, n_layers, n_kv_heads, head_dim, k_exp,
                                     v_exp)
