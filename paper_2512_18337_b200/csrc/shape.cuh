@@ -154,7 +154,7 @@ __global__ void __launch_bounds__(kShapeThreads, kShapeCtasPerSm) argmax_shaped_
     const int n_items = static_cast<int>(min(i1 - i0, 0x7fffffffll));
     ShapeItem mask_item = x, copy_item = x;
     int to_mask = n_items, to_load = n_items, mask_now = -1, mask_next = -1, stage_in = 0, own_in = 0;
-    uint32_t valid_in = 0, word_in = 0;                    // of the item that is copied next
+    uint32_t valid_in = 0, mask_lo = 0, mask_hi = 0;       // of the item that is copied next
     const uint4* src = nullptr;
     auto fetch_mask = [&]() {
         mask_now = mask_next;
@@ -183,17 +183,23 @@ __global__ void __launch_bounds__(kShapeThreads, kShapeCtasPerSm) argmax_shaped_
             seek();
             if (!kMasks) vectors_in = vectors_of(valid_in);
         }
-        if (kMasks) {
-            word_in = valid_in;
-            if (static_cast<unsigned>(mask_now) < static_cast<unsigned>(a.n_masks))
-                word_in &= bits_from(a.masks + static_cast<long long>(mask_now) * a.words, a.words, own_in);
+        if (kMasks) {                                      // loaded here, looked at when the row is copied
+            mask_lo = mask_hi = 0xffffffffu;
+            if (static_cast<unsigned>(mask_now) < static_cast<unsigned>(a.n_masks)) {
+                const uint32_t* m = a.masks + static_cast<long long>(mask_now) * a.words;
+                const int w = own_in >> 5;
+                mask_lo = mask_hi = 0;
+                if (w >= 0 && w < a.words) mask_lo = __ldg(m + w);
+                if ((own_in & 31) && w + 1 >= 0 && w + 1 < a.words) mask_hi = __ldg(m + w + 1);
+            }
         }
     };
     auto copy = [&]() {
         if (to_load > 0) {
             if (kMasks) {
-                vectors_in = vectors_of(word_in);
-                words[stage_in * kShapeThreads] = word_in;
+                const uint32_t word = valid_in & __funnelshift_r(mask_lo, mask_hi, own_in & 31);
+                vectors_in = vectors_of(word);
+                words[stage_in * kShapeThreads] = word;
             }
             const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(slots)) + stage_in * (kShapeVecs * kShapeThreads * 16);
             copy_vectors<0>(to, src, vectors_in);
