@@ -521,8 +521,8 @@ typedef struct sam_cache {
 #define SAM_CACHE_OUT_OF_PAGES  1   /* a sam_cache_reserve found too few free pages and reserved none */
 #define SAM_CACHE_TABLE_FULL    2   /* a sam_cache_reserve would have needed more than max_pages pages for a stream, and reserved none */
 #define SAM_CACHE_BAD_FORK      4   /* a sam_cache_fork pair named a destination that holds tokens, or an unknown stream */
-#define SAM_CACHE_GAVE_UP       8   /* a sam_cache_attend gave up on an internal (bounded) wait: its outputs are not valid, and its workspace
-                                       has to be zero-filled again */
+#define SAM_CACHE_GAVE_UP       8   /* a sam_cache_attend, sam_cache_attend_blocks or sam_cache_select gave up on an internal (bounded) wait: its
+                                       outputs are not valid, and the workspace of the first two has to be zero-filled again */
 
 #define SAM_CACHE_BF16  0           /* element types of queries, keys, values and outputs */
 #define SAM_CACHE_FP16  1
@@ -622,7 +622,7 @@ typedef struct sam_rope {
 } sam_rope;
 
 /* inv_freq[0 .. n) (host, radians per position, finite, up to 10^6 in magnitude; n <= 64) -> turns (host): the turns per position in units of 2^-64, so that
- * the angle of any position is exact to within 2^-31 of a turn.  Host only. */
+ * the angle is off by less than 2^-25 of a turn at any position.  Host only. */
 int sam_rope_turns(const double* inv_freq, int32_t n, uint64_t* turns);
 
 /* Append with rotation: queries q [B, Q, H, head_dim] are turned into q_out (which may be q itself with the same strides,
