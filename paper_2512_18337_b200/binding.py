@@ -740,6 +740,16 @@ class SamCache:
         with SamCache._on(device, stream):
             return make(shape, dtype=dtype, device=device)
 
+    @staticmethod
+    def _new(like, shape, dtype, stream):
+        """As _empty, on the device of a tensor; shape None: packed, of the tensor's own shape and type."""
+        import torch
+        if stream is not None:
+            return SamCache._empty(like.shape if shape is None else shape, dtype or like.dtype, like.device, stream)
+        if shape is None:
+            return torch.empty_like(like, memory_format=torch.contiguous_format)
+        return like.new_empty(shape, dtype=dtype)
+
     def _dtype(self, t) -> int:
         code = self._codes.get(t)
         if code is None:
@@ -845,7 +855,7 @@ class SamCache:
             raise ValueError("queries of the keys' type, rows and tokens are wanted")
         B, Q, H = q.shape[:3]
         if out is None:
-            out = self._empty(q.shape, q.dtype, q.device, stream)
+            out = self._new(q, None, None, stream)
         elif out.shape != q.shape or out.dtype != q.dtype:
             raise ValueError("out like q is wanted")
         po, so = self._rows(out, H)
@@ -862,11 +872,11 @@ class SamCache:
         pq, sq = self._rows(q, None)
         B, Q, H = q.shape[:3]
         if out is None:
-            out = self._empty(q.shape, q.dtype, q.device, stream)
+            out = self._new(q, None, None, stream)
         elif out.shape != q.shape or out.dtype != q.dtype:
             raise ValueError("out like q is wanted")
         if lse is None:
-            lse = self._empty((B, Q, H), torch.float32, q.device, stream)
+            lse = self._new(q, (B, Q, H), torch.float32, stream)
         elif tuple(lse.shape) != (B, Q, H) or lse.dtype != torch.float32:
             raise ValueError("a float32 lse [B, Q, H] is wanted")
         if share < 1 or tuple(blocks.shape[:3]) != (B, -(-Q // share), self.n_kv_heads) or blocks.dim() != 4 or \
@@ -921,11 +931,11 @@ class SamBounds:
         n = sam_cache_select_workspace_bytes(c.handle, B, Q, share)
         shape = (B, -(-Q // share), c.n_kv_heads, n_blocks)
         if out is None:
-            out = c._empty(shape, torch.int32, q.device, stream)
+            out = c._new(q, shape, torch.int32, stream)
         elif tuple(out.shape) != shape or out.dtype != torch.int32:
             raise ValueError(f"an int32 tensor of shape {shape} is wanted")
         if workspace is None:
-            workspace = c._empty(n, torch.uint8, q.device, stream)
+            workspace = c._new(q, (n,), torch.uint8, stream)
         sam_cache_select(c.handle, layer, self.codes, self.exps, pq, c._dtype(q.dtype), sq, B, Q, H, c._index(streams, B),
                          c._index(n_new, B), share, n_sink, n_recent, out, n_blocks, workspace,
                          workspace.numel() * workspace.element_size(), stream)
