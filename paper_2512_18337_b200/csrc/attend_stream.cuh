@@ -175,10 +175,10 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ uint64_t bars[kStreamWarps][kStages];
     __shared__ int64_t scan[kStreamWarps], row_base[kStreamWarps];
-    __shared__ int row_of[kStreamWarps];
+    __shared__ int row_of[kStreamWarps], seg_scan[kStreamWarps];
     __shared__ RowInfo row_found[kStreamWarps];
     __shared__ StreamPiece pieces[kStreamWarps][2];
-    __shared__ int last_here;
+    __shared__ int last_here[2];
     __shared__ bool gave_up[kStreamWarps];
     __shared__ int2 unit_begin[kListed ? kStreamWarps : 1][kStages];   // listed: positions of the first tokens of a unit's tiles
 
@@ -188,30 +188,35 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
     const int first_row = kListed ? a.row0 : 0;
 
     // ---- how many units there are, and where our share begins
-    int64_t segments = 0;
-    bool count_segments = true;
     RowInfo ri{};                                          // of the row that the thread looked at last
+    int segments_of_row = 0;
     auto units_of = [&](int b) -> int64_t {
         ri = row_info<kStreamUnit, kListed>(a, b);
         const int tiles = max((run_rows<kListed>(a, ri.n) + kRows - 1) / kRows, 0);
-        if (count_segments) segments += tiles * c.n_kv;
-        return static_cast<int64_t>(row_steps<kStreamUnit>(ri)) * tiles * c.n_kv;
+        segments_of_row = tiles * c.n_kv;
+        return static_cast<int64_t>(row_steps<kStreamUnit>(ri)) * segments_of_row;
     };
-    auto block_sum = [&](int64_t x, int64_t* before) -> int64_t {   // the total, and the sum over earlier threads
+    int64_t segments = 0;
+    auto block_sum = [&](int64_t x, int64_t* before) -> int64_t {   // the total, and the sum over earlier threads; adds to the segments
         int64_t y = x;
+        const int s = __reduce_add_sync(0xffffffffu, segments_of_row);
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
             const int64_t up = __shfl_up_sync(0xffffffffu, y, d);
             if (lane >= d) y += up;
         }
         __syncthreads();
-        if (lane == 31) scan[warp] = y;
+        if (lane == 31) {
+            scan[warp] = y;
+            seg_scan[warp] = s;
+        }
         __syncthreads();
         int64_t all = 0, first = 0;
 #pragma unroll
         for (int w = 0; w < kStreamWarps; ++w) {
             if (w == warp) first = all;
             all += scan[w];
+            segments += seg_scan[w];
         }
         *before = first + y - x;
         return all;
@@ -220,13 +225,12 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
     if (tid < kStreamWarps * 2) pieces[tid >> 1][tid & 1].used = 0;
     if (tid < kStreamWarps) gave_up[tid] = false;
     barrier_init_fence();
-    int64_t units = 0, mine = 0, before = 0, unused;
+    int64_t units = 0, mine = 0, before = 0;
     for (int b0 = 0; b0 < a.runs; b0 += kStreamThreads) {
+        segments_of_row = 0;
         mine = b0 + tid < a.runs ? units_of(b0 + tid) : 0;
         units += block_sum(mine, &before);
     }
-    count_segments = false;
-    segments = block_sum(segments, &unused);
     // About a unit a warp at least.  With up to two units a warp in a segment, a CTA
     // per segment: one more unit costs less than joining results across CTAs (one stream, 333 positions: 16.4 -> 11.6 us).
     const int64_t wanted = segments <= gridDim.x && units <= segments * kStreamWarps * 2 ? segments : (units + kStreamWarps - 1) / kStreamWarps;
@@ -658,6 +662,7 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
         if (left) cur.next_segment<kRows, kListed>(a);
     }
     if (gave_up[warp] && c.meta && lane == 0) atomicOr(&c.meta[1], kStatusGaveUp);
+    if constexpr (kListed) asm volatile("griddepcontrol.wait;" ::: "memory");   // behind the wide kernel: its joins use the same workspace
     if (!busy) return;
     __syncthreads();
 
@@ -706,18 +711,30 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
                 });
             }
         }
+    if (crossing < 0) return;
+    // both arrive before either is joined
+    __threadfence();
+    __syncthreads();
+    if (tid % 32 == 0 && warp < 2) {
+        const int at = warp ? crossing2 : crossing;
+        last_here[warp] = 0;
+        if (at >= 0) {
+            const StreamPiece& d = pieces[at >> 1][at & 1];
+            const int c0 = shares.owner(d.seg_begin), c1 = shares.owner(d.seg_begin + d.steps - 1);
+            if (atomicAdd(&a.counters[c0], 1) == c1 - c0) {
+                a.counters[c0] = 0;
+                last_here[warp] = 1;
+            }
+        }
+    }
+    __syncthreads();
+    if (!(last_here[0] | last_here[1])) return;
+    __threadfence();
     for (int k = 0; k < 2; ++k) {
+        if (!last_here[k]) continue;
         const int at = k ? crossing2 : crossing;
-        if (at < 0) break;
         const StreamPiece& d = pieces[at >> 1][at & 1];
         const int c0 = shares.owner(d.seg_begin), c1 = shares.owner(d.seg_begin + d.steps - 1);
-        __threadfence();
-        __syncthreads();
-        if (tid == 0) last_here = atomicAdd(&a.counters[c0], 1) == c1 - c0;
-        __syncthreads();
-        if (!last_here) continue;
-        __threadfence();
-        if (tid == 0) a.counters[c0] = 0;
         join_partials<D, kRows, true>(c1 - c0 + 1, [&](int i) { return const_cast<const float*>(a.partials + (2ll * (c0 + i) + (i == 0)) * Plan::kPiece); },
                                 [&](int n, int ch, float4 x, float top, float l) { write_row(d, n, ch, x, top, l); });
     }

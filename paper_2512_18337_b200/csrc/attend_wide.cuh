@@ -179,6 +179,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
     __shared__ int last_here;
     __shared__ volatile int abort_flag;
 
+    if constexpr (kListed) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the streaming kernel for rows behind the last full tile
     const CacheView& c = a.c;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));

@@ -85,6 +85,23 @@ int copy_grid(int64_t pages, int64_t page_bytes, int* grid) {
     return SAM_OK;
 }
 
+// Launches a kernel that may be placed while the one before it in the stream ends, where that one allows it.
+template <typename... P, typename... A>
+int launch_behind(void (*kernel)(P...), dim3 grid, int threads, int shared, cudaStream_t s, const A&... a) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = shared;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    SAM_CUDA(cudaLaunchKernelEx(&cfg, kernel, P(a)...));
+    return launched();
+}
+
 // Grid of append and read, and the multiplier that divides by the blocks of a token.
 dim3 io_grid(const CacheView& v, int32_t B, int32_t Q, uint32_t* magic) {
     const int64_t per_token = static_cast<int64_t>(v.n_kv) * (v.D / 16);
@@ -137,11 +154,13 @@ int allow_shared(K* kernel, int bytes, uint64_t* asked) {   // asked: the kernel
 }
 
 template <typename T, int D, int NT, bool kListed>
-int launch_stream(const AttendArgs& a, int sms, cudaStream_t s) {
+int launch_stream(const AttendArgs& a, int sms, cudaStream_t s, bool behind_wide = false) {
     using Plan = StreamPlan<D, NT>;
     static thread_local uint64_t asked = 0;
     if (int e = allow_shared(attend_stream_kernel<T, D, NT, kListed>, Plan::kSmem, &asked)) return e;
-    attend_stream_kernel<T, D, NT, kListed><<<std::min(sms * Plan::kCtasPerSm, kMaxCtas), kStreamThreads, Plan::kSmem, s>>>(a);
+    const int grid = std::min(sms * Plan::kCtasPerSm, kMaxCtas);
+    if (behind_wide) return launch_behind(attend_stream_kernel<T, D, NT, kListed>, grid, kStreamThreads, Plan::kSmem, s, a);
+    attend_stream_kernel<T, D, NT, kListed><<<grid, kStreamThreads, Plan::kSmem, s>>>(a);
     return launched();
 }
 
@@ -181,14 +200,14 @@ int launch_attend_blocks(AttendArgs a, cudaStream_t s) {
         a.row0 = a.row1;
         a.row1 = static_cast<int32_t>(rows);
     }
-    return a.row1 - a.row0 <= 8 ? launch_stream<T, D, 1, true>(a, di.sms, s) : launch_stream<T, D, 2, true>(a, di.sms, s);
+    const bool behind_wide = a.row0 > 0;
+    return a.row1 - a.row0 <= 8 ? launch_stream<T, D, 1, true>(a, di.sms, s, behind_wide) : launch_stream<T, D, 2, true>(a, di.sms, s, behind_wide);
 }
 
 template <int kTeam, int kKeys>
 int launch_pick(const SelectArgs& a, int64_t rows, cudaStream_t s) {
     constexpr int kLists = kPickThreads / kTeam;
-    select_pick_kernel<kTeam, kKeys><<<static_cast<unsigned>((rows + kLists - 1) / kLists), kPickThreads, 0, s>>>(a, rows);
-    return launched();
+    return launch_behind(select_pick_kernel<kTeam, kKeys>, static_cast<unsigned>((rows + kLists - 1) / kLists), kPickThreads, 0, s, a, rows);
 }
 
 int64_t key_stride(const sam_cache* c) { return (static_cast<int64_t>(c->max_pages) + 3) & ~int64_t(3); }
@@ -212,16 +231,14 @@ int launch_score(const SelectArgs& a, int64_t n, int sms, cudaStream_t s) {
     };
     if (a.team == 1 && padded <= kFewColumns) {
         // streams differ in length, and a block begins quickly
-        select_score_few_kernel<T, D><<<dim3(shares(kFewThreads / 2, 8), a.c.n_kv, static_cast<unsigned>(n)), kFewThreads, 0, s>>>(a);
-        return launched();
+        return launch_behind(select_score_few_kernel<T, D>, dim3(shares(kFewThreads / 2, 8), a.c.n_kv, static_cast<unsigned>(n)), kFewThreads, 0, s, a);
     }
     // a block takes 7 us for its queries before it begins: no more of them than run at a time
     const dim3 grid(shares(kScorePages, 2), a.c.n_kv, static_cast<unsigned>(n));
     static thread_local uint64_t asked = 0;
     if (int e = allow_shared(select_score_kernel<T, D>, score_smem<D>(kScoreColumns), &asked)) return e;
     const int columns = static_cast<int>((std::min<int64_t>(a.team * padded, kScoreColumns) + 15) / 16 * 16);
-    select_score_kernel<T, D><<<grid, kScoreThreads, score_smem<D>(columns), s>>>(a);
-    return launched();
+    return launch_behind(select_score_kernel<T, D>, grid, kScoreThreads, score_smem<D>(columns), s, a);
 }
 
 // Scores and picks for all lists, as many at a time as the keys have room for.

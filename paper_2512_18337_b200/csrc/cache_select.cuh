@@ -105,6 +105,7 @@ __device__ __forceinline__ void bound_page(const CacheView& c, const BoundsView&
 
 // Pages that the new tokens fill up.  Grid: (heads, rows, pages of a row).
 __global__ void __launch_bounds__(kBoundThreads) bounds_update_kernel(CacheView c, BoundsView o, int layer, int Q, const int32_t* streams, const int32_t* n_new) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the scores' kernel may be placed; it waits for the end of this one
     const int b = blockIdx.y;
     const int s = c.stream_of(streams, b);
     if (s < 0) return;
@@ -143,6 +144,14 @@ struct SelectArgs {
     int32_t* out;                // [B, lists, n_kv, n_blocks]
     bool q_wide;
 };
+
+// The kernels of a selection are placed while the one before them ends.  Scores wait for everything before them and only then let
+// the picks be placed, so that picks may read whatever scores do not write before they wait themselves.
+__device__ __forceinline__ void await_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void await_and_release() {
+    await_before();
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
 
 // A run of query tokens with a list in common: list l of row b.
 struct SelectRun {
@@ -218,6 +227,7 @@ __global__ void __launch_bounds__(kFewThreads) select_score_few_kernel(const __g
     constexpr int kParts = 2 * D / 64, kLanes = D / 8;    // sixteen-byte parts of a row or column that a thread has; lanes of a query row
     __shared__ alignas(16) uint8_t columns[kFewColumns * kStride];
     __shared__ alignas(8) float unit[kFewColumns];
+    await_and_release();
     const CacheView& c = a.c;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, j = lane & 3, head = blockIdx.y;
     const int64_t v = a.first_team + blockIdx.z;
@@ -339,6 +349,7 @@ __global__ void __launch_bounds__(kScoreThreads, 2) select_score_kernel(const __
     __shared__ float part_best[kScoreGroups][kScorePages];   // where one list is all there is
     __shared__ uint64_t done;
     __shared__ uint32_t tmem_base;
+    await_and_release();
     const CacheView& c = a.c;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, head = blockIdx.y;
     const int own = tid % kScorePages, group = tid / kScorePages;   // the thread's page of a tile
@@ -606,12 +617,16 @@ __global__ void __launch_bounds__(kPickThreads) select_pick_kernel(const __grid_
     const CacheView& c = a.c;
     const int t = threadIdx.x % kTeam;
     const int64_t row = static_cast<int64_t>(blockIdx.x) * (kPickThreads / kTeam) + threadIdx.x / kTeam;   // of the keys
-    if (row >= n_lists) return;                           // the whole team
+    if (row >= n_lists) {                                 // the whole team
+        await_before();
+        return;
+    }
     const int64_t g = quotient(row, c.n_kv), w = quotient(g, a.team), v = a.first_team + w;
     const int head = static_cast<int>(row - g * c.n_kv), b = static_cast<int>(quotient(v, a.teams));
     const int l = static_cast<int>(v - static_cast<int64_t>(b) * a.teams) * a.team + static_cast<int>(g - w * a.team);
+    const int n = l < a.lists ? select_run(a, b, l).pages : 0;
+    await_before();
     if (l >= a.lists) return;
-    const int n = select_run(a, b, l).pages;
     int32_t* const out = a.out + ((static_cast<int64_t>(b) * a.lists + l) * c.n_kv + head) * a.n_blocks;
     const uint32_t* const keys = a.keys + row * a.key_stride;
     const int each = kKeys ? kKeys : (n + kTeam - 1) / kTeam, i0 = t * each;   // the thread's pages: i0 .. i0 + each - 1
