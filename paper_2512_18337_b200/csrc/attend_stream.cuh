@@ -712,7 +712,7 @@ __global__ void __launch_bounds__(kStreamThreads, StreamPlan<D, NT>::kCtasPerSm)
             }
         }
     if (crossing < 0) return;
-    // both arrive before either is joined
+    // both arrive before either is joined (one after the other: 4 streams of 2,500 positions 28.8 us instead of 26.7)
     __threadfence();
     __syncthreads();
     if (tid % 32 == 0 && warp < 2) {

@@ -188,8 +188,8 @@ int launch_attend_blocks(AttendArgs a, cudaStream_t s) {
     DeviceInfo di;
     if (int e = device_info(&di)) return e;
     // What a row tile of the wide kernel costs does not depend on how full it is; up to eight rows behind the last full one take
-    // the streaming kernel less (48 streams of 17 tokens, 64/8 heads, 2,048 positions each: 182 against 223 us; with 8 to 17 tokens a stream, so that
-    // few have a second tile, 172 against 171; sixteen rows 193 against 219, and 169 against 143).
+    // the streaming kernel less, which is placed while the other one ends (48 streams of 17 tokens, 64/8 heads, 2,048 positions each: 155 against
+    // 185 us; with 12 to 17 tokens a stream, so that few have a second tile, 141 against 145; sixteen rows 168 against 184, and 149 against 144).
     const int64_t rows = static_cast<int64_t>(a.share) * a.group, rest = rows % kWideRows;
     a.row0 = 0;
     a.row1 = static_cast<int32_t>(rows);
