@@ -1037,12 +1037,18 @@ class SamShape:
         self._struct = _ShapeStruct(*address.values(), 0 if counts is None else counts.shape[0], n_bias_columns,
                                     0 if masks is None else masks.shape[0])
         self.handle = C.addressof(self._struct)
+        per_row = [self.tensors[n] for n in self._PER_ROW]
+        self._most = min((t.shape[0] for t in per_row if t is not None), default=None)   # rows of a call
+
+    _PER_ROW = ("repetition", "presence", "frequency", "bias_tokens", "n_bias", "mask_of")
 
     def check(self, B: int, K: int, V: int) -> int:
         """The handle, if the tensors fit a call of this shape."""
         if V != self.V:
             raise ValueError("made for another vocabulary")
-        for name in ("repetition", "presence", "frequency", "bias_tokens", "n_bias", "mask_of"):
+        if (self._most is None or B <= self._most) and (self.mask_of is None or self.mask_of.shape[1] == K + 1):
+            return self.handle
+        for name in self._PER_ROW:
             t = self.tensors[name]
             if t is not None and (t.shape[0] < B or (name == "mask_of" and t.shape[1] != K + 1)):
                 raise ValueError(f"{name}: too small for {B} rows of {K + 1}")
