@@ -632,6 +632,24 @@ int sync_updates(sam_index* idx, cudaStream_t st, const Renorm* rn, int64_t* tok
     return SAM_OK;
 }
 
+// Launches a kernel that may be placed while the one before it in the stream ends, where that one allows it.
+template <typename... P, typename... A>
+int launch_behind(void (*kernel)(P...), unsigned grid, int threads, int shared, cudaStream_t st, const A&... a) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = shared;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    SAM_CUDA(cudaLaunchKernelEx(&cfg, kernel, P(a)...));
+    ++g_launches;
+    return SAM_OK;
+}
+
 template <bool kMasks>
 int launch_shaped(const ShapeArgs& a, unsigned grid, cudaStream_t st) {
     static thread_local uint64_t asked = 0;               // one bit per device
@@ -642,10 +660,11 @@ int launch_shaped(const ShapeArgs& a, unsigned grid, cudaStream_t st) {
         SAM_CUDA(cudaFuncSetAttribute(argmax_shaped_kernel<kMasks>, cudaFuncAttributeMaxDynamicSharedMemorySize, shape_smem(kMasks)));
         asked |= bit;
     }
-    argmax_shaped_kernel<kMasks><<<grid, kShapeThreads, shape_smem(kMasks), st>>>(a);
+    const int64_t rows = static_cast<int64_t>(a.B) * (a.K + 1);
+    clear_keys_kernel<<<static_cast<unsigned>(std::min<int64_t>((rows + 255) / 256, 1024)), 256, 0, st>>>(a.keys, rows);
     SAM_CUDA(cudaGetLastError());
     ++g_launches;
-    return SAM_OK;
+    return launch_behind(argmax_shaped_kernel<kMasks>, grid, kShapeThreads, shape_smem(kMasks), st, a);
 }
 
 int64_t shape_words(int32_t V) { return (static_cast<int64_t>(V) + 31) / 32; }
@@ -940,7 +959,7 @@ int sam_verify_from_keys(int64_t* keys, int32_t B, int32_t K, const int32_t* dra
     if (!keys || !aligned(keys, 8) || !drafts || !n_draft || !argmax_out || !accepted || !n_accepted || !aligned(values, 4)) return SAM_ERR_INVALID_ARG;
     AcceptArgs aa{nullptr, 0, B, K, drafts, n_draft, argmax_out, accepted, n_accepted, reinterpret_cast<unsigned long long*>(keys)};
     aa.values = values;
-    return launch_accept<kTailVerifyOnly>(DeviceSam{}, aa, static_cast<cudaStream_t>(cuda_stream), false);
+    return launch_behind(verify_keys_kernel, static_cast<unsigned>((static_cast<int64_t>(B) + 3) / 4), 128, 0, static_cast<cudaStream_t>(cuda_stream), aa);
 }
 
 int sam_argmax_shaped(const void* logits_bf16, int64_t row_stride_elems, int32_t B, int32_t K, int32_t V, const int32_t* drafts,
@@ -955,7 +974,6 @@ int sam_argmax_shaped(const void* logits_bf16, int64_t row_stride_elems, int32_t
     if (int e = device_info(&di)) return e;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     const int64_t R = static_cast<int64_t>(B) * (K + 1);
-    SAM_CUDA(cudaMemsetAsync(keys, 0, static_cast<size_t>(R) * 8, st));
     ShapeArgs a{};
     a.logits = static_cast<const __nv_bfloat16*>(logits_bf16);
     a.stride = row_stride_elems;

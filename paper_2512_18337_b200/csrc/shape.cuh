@@ -5,7 +5,7 @@
 // allowed at all, comes as bits, 1/16 of the logits' bytes each.  The others take part in a maximum of pairs of bf16; a special token is worked
 // out only where its logit reaches the best so far, which no usual penalty can raise.
 //
-// 192 streams of 17 rows of 151,936 logits with 6,000 tokens said and up to 64 biases each (1.0 GB): 184 us, 5.4 TB/s (without penalties
+// 192 streams of 17 rows of 151,936 logits with 6,000 tokens said and up to 64 biases each (1.0 GB): 180 to 184 us, 5.4 TB/s (without penalties
 // and biases 160, the plain argmax 146).  What it took: every token of a row looked at with its bits, loads into registers: 742 us; bits
 // once for all rows of a tile: 430; copies to shared memory some rows ahead by the threads that read them: 265; special tokens
 // in the order of their tiles and by one lane: 193; a lane for each token: 184.  All of it fits 80 registers a thread, which
@@ -124,6 +124,7 @@ __global__ void __launch_bounds__(kShapeThreads, kShapeCtasPerSm) argmax_shaped_
     __shared__ uint16_t listed[kShapeThreads];             // biases of the tile
     __shared__ int n_listed, n_waiting;
     __shared__ int2 waiting[kShapeWaiting];                // token; its logit, and below it the row
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, K1 = a.K + 1;
     const long long total = static_cast<long long>(a.B) * K1 * a.tiles_per_row;
     const long long i0 = total * blockIdx.x / gridDim.x, i1 = total * (blockIdx.x + 1) / gridDim.x;
@@ -230,6 +231,7 @@ __global__ void __launch_bounds__(kShapeThreads, kShapeCtasPerSm) argmax_shaped_
     uint32_t seen_next = 0;
     uint32_t out[kShapeVecs][4], odd = 0;                  // what takes tokens out of the maximum; special tokens of the vectors
     auto flush = [&]() {
+        asm volatile("griddepcontrol.wait;" ::: "memory");   // the keys are cleared
         __syncthreads();
         if (cur_b >= 0 && tid < K1 && best[tid]) atomicMax(a.keys + static_cast<long long>(cur_b) * K1 + tid, best[tid]);
         __syncthreads();
@@ -493,6 +495,21 @@ __global__ void __launch_bounds__(kShapeThreads, kShapeCtasPerSm) argmax_shaped_
     }
     settle();
     flush();
+}
+
+// The kernel above is placed while this one ends: it needs no key before it has its first result, and all that came before this one
+// has ended when this one begins.
+__global__ void __launch_bounds__(256) clear_keys_kernel(unsigned long long* keys, long long n) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    for (long long i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) keys[i] = 0;
+}
+
+// Accepts from keys; placed while the kernel before it ends, whatever that is, and waits for that end first of all.  (4 streams of three
+// drafts, 151,936 logits: 10.5 us for the three kernels, 14.4 with a fill and kernels that are placed one after the other.)
+__global__ void __launch_bounds__(128) verify_keys_kernel(AcceptArgs p) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int b = blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
+    if (b < p.B) accept_stream<kTailVerifyOnly, false>(DeviceSam{}, p, b, threadIdx.x & 31);
 }
 
 // ---- what was told and said

@@ -127,3 +127,65 @@ def test_two_threads_of_one_stream():
     torch.cuda.synchronize()
     for k in range(2):
         assert len(got[k]) == 10 and all(_same(g, w) for calls in got[k] for g, w in zip(calls, want[k]))
+
+
+@pytest.mark.parametrize("B,K,V,masks", [(1, 1, 5, False), (4, 3, 50257, True), (40, 16, 9000, False), (7, 8, 151936, True)])
+@pytest.mark.parametrize("how", ["calls", "recorded", "recorded behind a stream"])
+def test_shaped_choices(B, K, V, masks, how):
+    """Keys that hold anything before, logits and drafts that were written just before, drafts that change between the two calls."""
+    gen = torch.Generator(device=DEV).manual_seed(B + V)
+    logits = torch.empty(B, K + 1, V, dtype=torch.bfloat16, device=DEV)
+    src = [torch.randn(B, K + 1, V, generator=gen, device=DEV).bfloat16() for _ in range(3)]
+    words = -(-V // 32)
+    mask = torch.randint(-(1 << 31), 1 << 31, (3, words), generator=gen, dtype=torch.int64, device=DEV).int() if masks else None
+    mask_of = torch.randint(-1, 3, (B, K + 1), generator=gen, device=DEV).int() if masks else None
+    shape = S.SamShape(V, masks=mask, mask_of=mask_of)
+    keys = torch.empty(B * (K + 1), dtype=torch.int64, device=DEV)
+    drafts, out = torch.zeros(B, K, dtype=torch.int32, device=DEV), torch.zeros(B, K + 1, dtype=torch.int32, device=DEV)
+    accepted, n = torch.zeros_like(out), torch.zeros(B, dtype=torch.int32, device=DEV)
+    values = torch.zeros(B, K + 1, device=DEV)
+    n_draft = torch.full((B,), K, dtype=torch.int32, device=DEV)
+    # what it comes to: rows without penalties are the first largest of what is allowed
+    wants = []
+    for x in src:
+        y = x.float()
+        if masks:
+            bits = (mask[:, :, None] >> torch.arange(32, device=DEV)) & 1
+            allowed = bits.flatten(1)[:, :V].bool()
+            allowed = torch.cat([allowed, torch.ones(1, V, dtype=torch.bool, device=DEV)])[torch.where(mask_of < 0, 3, mask_of).long()]
+            y = torch.where(allowed, y, -float("inf"))
+        top = y.amax(-1)
+        wants.append((torch.where(y == top[..., None], torch.arange(V, device=DEV), V).amin(-1).int(), top))
+    now = src[0].clone()
+
+    def call():
+        keys.fill_(-1)
+        logits.copy_(now)
+        drafts.fill_(7)
+        S.sam_argmax_shaped(logits, V, B, K, V, drafts, shape, keys)
+        drafts.copy_(chosen)
+        S.sam_verify_from_keys(keys, B, K, drafts, n_draft, out, accepted, n, values=values)
+
+    chosen = wants[0][0][:, :K].clone()
+    call()
+    torch.cuda.synchronize()
+    if how != "calls":
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            if how != "recorded":
+                main, side = torch.cuda.current_stream(), torch.cuda.Stream()
+                side.wait_stream(main)
+                with torch.cuda.stream(side):
+                    values.fill_(3)
+                n.fill_(9)
+                main.wait_stream(side)
+            call()
+    for i in (0, 1, 2, 1, 0, 2) * 3:
+        now.copy_(src[i])
+        chosen.copy_(wants[i][0][:, :K])
+        if i == 2:
+            chosen[:, -1] += 1
+        call() if how == "calls" else g.replay()
+        argmax, top = wants[i]
+        assert torch.equal(out, argmax) and torch.equal(values, top)
+        assert (n == (K if i == 2 else K + 1)).all()
