@@ -377,7 +377,9 @@ __global__ void __launch_bounds__(kShapeThreads, kShapeCtasPerSm) argmax_shaped_
         copy();
         const int j = x.j;
         const uint32_t here = kMasks ? words[stage * kShapeThreads] : valid;
-        const unsigned so_far = static_cast<unsigned>(*reinterpret_cast<volatile unsigned long long*>(&best[j]) >> 32);
+        // The block's other warps raise it meanwhile, and lanes that load it apart may find different values.  Whole-warp steps below
+        // depend on it: it is lane 0's for all, and the shuffle brings the warp together.
+        const unsigned so_far = __shfl_sync(kFull, static_cast<unsigned>(*reinterpret_cast<volatile unsigned long long*>(&best[j]) >> 32), 0);
         unsigned bound = so_far;
         auto element = [&](int vector, int l, int k) {     // of what lane l copied: the bits of a float
             return static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(slots - lane + l + (stage * kShapeVecs + vector) * kShapeThreads)[k]) << 16;
