@@ -594,6 +594,8 @@ int sam_cache_read(const sam_cache* c, int32_t layer, int32_t B, int32_t Q, cons
  * A row that sees nothing, and rows from n_new[b] on: out = 0, lse = -inf.  So the keys and values of the new tokens
  * are appended first; one call serves a single token, a proposal, or a chunk of a prompt.  Masked positions are never
  * computed with: what their bytes hold (NaN included) does not matter.
+ * Scores, statistics and sums are in 32 bits.  A weight is rounded to fp16 before its product with the values: to 11 bits, down to 2^-21
+ * of the row's largest weight (smaller ones are off by up to 2^-32 of the largest).  The result is rounded once, to dtype.
  * workspace: sam_cache_attend_workspace_bytes() of device memory, 256-byte aligned, zero-filled once by
  * sam_workspace_init before the first call; calls that share it must not overlap on the device. */
 int64_t sam_cache_attend_workspace_bytes(const sam_cache* c, int32_t B, int32_t Q, int32_t H);
@@ -672,7 +674,7 @@ int sam_cache_select(const sam_cache* c, int32_t layer, const int8_t* codes, con
                      int32_t* blocks, int32_t n_blocks, void* workspace, int64_t workspace_bytes, void* cuda_stream);
 
 /* Attend over listed blocks: as sam_cache_attend without a window, but a query token sees, of the positions up to its own, only
- * those in the blocks of its list (blocks as sam_cache_select leaves them; any other list will do).  Of a list the first
+ * those in the blocks of its list (blocks as sam_cache_select leaves them; any other list will do); weights are rounded as there.  Of a list the first
  * min(n_blocks, blocks up to the run's last position) entries are looked at: no list of different blocks is longer.
  * Entries out of range, blocks without a page and blocks behind the run are passed over; a block that stands there twice counts twice.
  * workspace as for sam_cache_attend, with sam_cache_attend_blocks_workspace_bytes(). */

@@ -35,10 +35,13 @@ constexpr int kWideUnit = 128;                     // tokens of a step
 constexpr int kWideRows = 128;                     // query rows of a segment
 constexpr int kWideWarps = 28, kWideThreads = kWideWarps * 32;   // eight softmax warps, sixteen expanding ones, an issuing one (and three that idle)
 constexpr int kWideMaxCtas = 160;
-constexpr float kTotalMax = 32768.f;               // 64 weights of 2^8 add up to less
-// How far below the largest score the reference is set.  Pages out of a list differ more from one another than neighbours do, so that
-// it is raised more often: less below leaves more room above, and weights keep all 11 bits down to 2^-18 of the largest, not 2^-22.
-template <bool kListed> constexpr float kWideAbove = kListed ? 4.f : 8.f;
+// How far below the largest score the reference is set, and what a thread's 64 weights of a step may add up to before it is raised.  Pages
+// out of a list differ more from one another than neighbours do, so that it is raised more often: with lists it takes the largest
+// of all scores of the first step, not of a quarter, the sum may be all that a single fp16 weight can, and the reference lies 7 below, so that weights keep
+// all 11 bits down to 2^-21 of the largest, as in the streaming kernel.  (48 proposals of 17 over 64 blocks of 32, and 2,048 queries, every sixteen over 32 blocks of
+// 64: 143 and 114 us; as without lists 162 and 139, so but 8 below 148 and 123, 6 below 142 and 108.)
+template <bool kListed> constexpr float kWideAbove = kListed ? 7.f : 8.f;
+template <bool kListed> constexpr float kTotalMax = kListed ? 65504.f : 32768.f;
 // columns of tensor memory
 constexpr uint32_t kColQ = 0, kColS = 64, kColO = 320;
 
@@ -417,11 +420,20 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                     float2 total = make_float2(0.f, 0.f);
                     uint32_t x[2][16], p[2][16];
                     tmem_load16(s_at, x[0]);
-                    if (__any_sync(0xffffffffu, m == -INFINITY)) {   // a first reference from some of the scores
+                    if (__any_sync(0xffffffffu, m == -INFINITY)) {   // a first reference from some of the scores; with lists, from all
                         tmem_load_wait(x[0]);
                         float top = -INFINITY;
 #pragma unroll
                         for (int i = 0; i < 16; ++i) top = fmaxf(top, __uint_as_float(x[0][i]));
+                        if constexpr (kListed) {
+#pragma unroll 1
+                            for (int q = 1; q < 4; ++q) {
+                                tmem_load16(s_at + q * 16, x[1]);
+                                tmem_load_wait(x[1]);
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) top = fmaxf(top, __uint_as_float(x[1][i]));
+                            }
+                        }
                         top = larger(top);
                         if (m == -INFINITY) m = top * factor - kWideAbove<kListed>;
                     }
@@ -441,7 +453,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) attend_wide_kernel(const __gr
                         }
                     }
                     const float sum = total.x + total.y;
-                    done = !any_of_pair(sum > kTotalMax);
+                    done = !any_of_pair(sum > kTotalMax<kListed>);
                     if (done) {
                         l += sum;
                         tmem_store16(s_at, p[0]);
