@@ -623,8 +623,8 @@ typedef struct sam_rope {
     float factor;            /* finite; 1 for none */
 } sam_rope;
 
-/* inv_freq[0 .. n) (host, radians per position, finite, up to 10^6 in magnitude; n <= 64) -> turns (host): the turns per position in units of 2^-64, so that
- * the angle is off by less than 2^-25 of a turn at any position.  Host only. */
+/* inv_freq[0 .. n) (host, radians per position, finite, up to 10^6 in magnitude; n <= 64) -> turns (host): the turns per position to the nearest
+ * multiple of 2^-64, so that the angle is off by less than 2^-25 of a turn at any position.  Host only. */
 int sam_rope_turns(const double* inv_freq, int32_t n, uint64_t* turns);
 
 /* Append with rotation: queries q [B, Q, H, head_dim] are turned into q_out (which may be q itself with the same strides,

@@ -274,6 +274,33 @@ int check_layer_call(const sam_cache* c, int32_t layer, int32_t B, int32_t Q, co
 
 int check_bounds(const int8_t* codes, const int8_t* exps) { return codes && exps && aligned(codes, 16) ? SAM_OK : SAM_ERR_INVALID_ARG; }
 
+// f / 2 pi modulo 1 in units of 2^-64, to nearest; |f| < 2^20.  f is m 2^e with a whole number m below 2^53, 1 / 2 pi stands here in 192 bits: their
+// product is a whole number below 2^243, of which the lowest 128 - e bits lie behind the unit.
+uint64_t turns_of(double f) {
+    constexpr uint64_t kInverse[3] = {0x36d8a5664f10e410u, 0x7f09d5f47d4d3770u, 0x28be60db9391054au};   // lowest first
+    int exponent;
+    const uint64_t m = static_cast<uint64_t>(std::ldexp(std::frexp(std::fabs(f), &exponent), 53));
+    const int behind = 128 - (exponent - 53);              // 161 or more
+    if (behind > 255) return 0;                            // less than half a unit
+    uint64_t product[5] = {0, 0, 0, 0, 0};
+    unsigned __int128 carry = 0;
+    for (int i = 0; i < 3; ++i) {
+        carry += static_cast<unsigned __int128>(m) * kInverse[i];
+        product[i] = static_cast<uint64_t>(carry);
+        carry >>= 64;
+    }
+    product[3] = static_cast<uint64_t>(carry);
+    carry = uint64_t(1) << ((behind - 1) & 63);            // half a unit
+    for (int i = (behind - 1) >> 6; i < 4; ++i) {
+        carry += product[i];
+        product[i] = static_cast<uint64_t>(carry);
+        carry >>= 64;
+    }
+    const int word = behind >> 6, bit = behind & 63;       // the product stays below 2^256: product[4] is zero
+    const uint64_t turns = product[word] >> bit | (bit ? product[word + 1] << (64 - bit) : 0);
+    return f < 0 ? 0 - turns : turns;
+}
+
 template <typename T>
 int launch_turn(const TurnArgs& a, cudaStream_t s) {
     const dim3 grid((a.Q + a.tokens - 1) / a.tokens, a.B);
@@ -529,9 +556,7 @@ int sam_rope_turns(const double* inv_freq, int32_t n, uint64_t* turns) {
     if (n < 1 || n > 64 || !inv_freq || !turns) return SAM_ERR_INVALID_ARG;
     for (int32_t i = 0; i < n; ++i) {
         if (!std::isfinite(inv_freq[i]) || std::fabs(inv_freq[i]) > 1e6) return SAM_ERR_INVALID_ARG;
-        const long double x = static_cast<long double>(inv_freq[i]) / 6.283185307179586476925286766559L;
-        const long double part = x - floorl(x);                      // of a turn, 0 .. 1
-        turns[i] = part >= 1.0L ? 0 : static_cast<uint64_t>(part * 18446744073709551616.0L);
+        turns[i] = turns_of(inv_freq[i]);
     }
     return SAM_OK;
 }
