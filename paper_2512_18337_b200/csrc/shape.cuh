@@ -256,7 +256,7 @@ __global__ void __launch_bounds__(kShapeThreads, kShapeCtasPerSm) argmax_shaped_
         if (tid == 0) n_waiting = 0;
     };
     auto enter_stream = [&](int b) {
-        flush();
+        if (cur_b >= 0) flush();                           // the first stream's facts need no wait for the keys
         cur_b = b;
         if (tid < K1) best[tid] = 0;
         if (tid < a.K) drafts[tid] = a.drafts[static_cast<long long>(b) * a.K + tid];
