@@ -951,8 +951,12 @@ class _ShapeStruct(C.Structure):
 
 
 def sam_argmax_shaped(logits, row_stride, B, K, V, drafts, shape, keys, streams=None, stream=None) -> None:
-    """shape: a SamShape (or the address of a sam_shape); keys: int64 [B * (K + 1)]."""
+    """shape: a SamShape (or the address of a sam_shape); keys: int64 [B * (K + 1)]; streams: int32 [B] (or an address)."""
     handle = shape.check(B, K, V) if isinstance(shape, SamShape) else shape
+    if streams is not None and not isinstance(streams, int):
+        import torch
+        if streams.dtype != torch.int32 or streams.numel() != B:
+            raise ValueError("int32 streams with one entry per row are wanted")
     _check(_load().sam_argmax_shaped(_dev(logits), row_stride, B, K, V, _dev(drafts), _dev(streams), handle, _dev(keys),
                                      _stream(stream)), "sam_argmax_shaped")
 
