@@ -69,8 +69,7 @@ class CachedDecoder:
     """Greedy decoding of B streams with drafts of up to K tokens from a SamIndex (or none).
 
     n_blocks > 0: attention over so many selected blocks of the context (at least 4: one sink, two recent, one more that a
-    proposal runs into).  penalties: (repetition, presence, frequency) for what the prompt told and the stream said; the
-    counters of accepted drafts are not kept then."""
+    proposal runs into).  penalties: (repetition, presence, frequency) for what the prompt told and the stream said."""
 
     def __init__(self, model: TinyDecoder, B: int, K: int, n_pages: int, page_tokens=16, max_pages=64, min_match=2,
                  index: S.SamIndex | None = None, device="cuda:0", n_blocks: int = 0, penalties=None):
@@ -152,6 +151,7 @@ class CachedDecoder:
                 S.sam_verify_from_keys(self.keys, self.B, self.K, self.drafts, self.n_draft, self.argmax, self.accepted,
                                        self.n_accepted)
             self.history.add(self.accepted, n=self.n_accepted)
+            self.count(n_new - 1)
         elif self.index is not None:
             S.sam_step_ex(self.index.handle, logits, logits.shape[-1], self.B, self.K, self.model.vocab, self.drafts,
                           self.n_draft, self.argmax, self.accepted, self.n_accepted, self.state, self.mlen, self.min_match,
@@ -164,6 +164,13 @@ class CachedDecoder:
         last = (self.n_accepted - 1).clamp(min=0).long()[:, None]
         self.pending.copy_(self.accepted.gather(1, last)[:, 0])
         return self.accepted, self.n_accepted
+
+    def count(self, proposed):
+        """The counters of sam_step_ex for a step that was verified from keys; proposed: drafts of each stream."""
+        committed = self.n_accepted.sum()
+        per_call = torch.full_like(committed, self.B)
+        self.counters += torch.stack([per_call, committed, proposed.sum(), committed - self.B, (proposed > 0).sum(),
+                                      per_call * (self.K + 1)])
 
     def decode(self, steps: int):
         out = [[] for _ in range(self.B)]
