@@ -133,7 +133,7 @@ int launch_read(const CacheView& v, int32_t layer, int32_t B, int32_t Q, const i
 constexpr int kMaxCtas = 512;
 constexpr int64_t kCounterBytes = kMaxCtas * 4;
 constexpr int64_t kNarrowRows = 32;   // query rows per key/value head up to which the streaming kernel is used
-constexpr int64_t kSplitRows = 8;     // with lists also for up to so many behind the wide kernel's last full tile
+constexpr int64_t kSplitRows = 8;     // with many lists also for up to so many behind the wide kernel's last full tile
 
 template <int D>
 int64_t partial_bytes(int64_t rows) {
@@ -188,13 +188,15 @@ int launch_attend_blocks(AttendArgs a, cudaStream_t s) {
     DeviceInfo di;
     if (int e = device_info(&di)) return e;
     // What a row tile of the wide kernel costs does not depend on how full it is; up to eight rows behind the last full one take
-    // the streaming kernel less, which is placed while the other one ends (48 streams of 17 tokens, 64/8 heads, 2,048 positions each: 155 against
-    // 185 us; with 12 to 17 tokens a stream, so that few have a second tile, 141 against 145; sixteen rows 168 against 184, and 149 against 144).
+    // the streaming kernel less, which is placed while the other one ends, once there is more than one list and head for every two SMs: with fewer
+    // the tile runs beside the full ones on SMs that would idle.  (Proposals of 17, 64/8 heads, lists of 2,048 positions: 48 streams 155 against 182
+    // us, 24 101 against 105, 16 81 against 79, 8 65 against 52; of 256 positions: 48 streams 63 against 67, 12 31 against 33, 8 31 against 24.  Proposals of 33, which
+    // have three tiles: 48 streams 232 against 252, 8 74 against 67.  Sixteen rows behind the tile, 48 streams: 168 against 184, and 149 against 144 with 12 to 17 tokens a stream.)
     const int64_t rows = static_cast<int64_t>(a.share) * a.group, rest = rows % kWideRows;
     a.row0 = 0;
     a.row1 = static_cast<int32_t>(rows);
     if (rows > kNarrowRows) {
-        if (rest <= kSplitRows) a.row1 -= static_cast<int32_t>(rest);
+        if (rest <= kSplitRows && 2 * static_cast<int64_t>(a.runs) * a.c.n_kv > di.sms) a.row1 -= static_cast<int32_t>(rest);
         if (int e = launch_wide<T, D, true>(a, di.sms, s)) return e;
         if (a.row1 == rows) return SAM_OK;
         a.row0 = a.row1;
