@@ -85,23 +85,6 @@ int copy_grid(int64_t pages, int64_t page_bytes, int* grid) {
     return SAM_OK;
 }
 
-// Launches a kernel that may be placed while the one before it in the stream ends, where that one allows it.
-template <typename... P, typename... A>
-int launch_behind(void (*kernel)(P...), dim3 grid, int threads, int shared, cudaStream_t s, const A&... a) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3(threads);
-    cfg.dynamicSmemBytes = shared;
-    cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    SAM_CUDA(cudaLaunchKernelEx(&cfg, kernel, P(a)...));
-    return launched();
-}
-
 // Grid of append and read, and the multiplier that divides by the blocks of a token.
 dim3 io_grid(const CacheView& v, int32_t B, int32_t Q, uint32_t* magic) {
     const int64_t per_token = static_cast<int64_t>(v.n_kv) * (v.D / 16);
@@ -236,7 +219,7 @@ int launch_score(const SelectArgs& a, int64_t n, int sms, cudaStream_t s) {
         return launch_behind(select_score_few_kernel<T, D>, dim3(shares(kFewThreads / 2, 8), a.c.n_kv, static_cast<unsigned>(n)), kFewThreads, 0, s, a);
     }
     // A block takes 7 us for its queries before it begins: about as many of them as run at a time, to the nearest share.  (Rounded down, so that they all do: 48 proposals
-    // of 17, 28/4 heads, contexts of 6,000 to 12,000 34.5 -> 32.9 us, but of 16 to 12,000, which more blocks even out, 39.2 -> 41.0; 176 list teams and heads 55.8 -> 58.8.)
+    // of 17, 28/4 heads, contexts of 6,000 to 12,000 34.5 -> 32.9 us, but of 1,200 to 12,000, which more blocks even out, 39.2 -> 41.0; 176 list teams and heads 55.8 -> 58.8.)
     const dim3 grid(shares(kScorePages, 2), a.c.n_kv, static_cast<unsigned>(n));
     static thread_local uint64_t asked = 0;
     if (int e = allow_shared(select_score_kernel<T, D>, score_smem<D>(kScoreColumns), &asked)) return e;

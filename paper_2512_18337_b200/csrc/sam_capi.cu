@@ -632,24 +632,6 @@ int sync_updates(sam_index* idx, cudaStream_t st, const Renorm* rn, int64_t* tok
     return SAM_OK;
 }
 
-// Launches a kernel that may be placed while the one before it in the stream ends, where that one allows it.
-template <typename... P, typename... A>
-int launch_behind(void (*kernel)(P...), unsigned grid, int threads, int shared, cudaStream_t st, const A&... a) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid);
-    cfg.blockDim = dim3(threads);
-    cfg.dynamicSmemBytes = shared;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    SAM_CUDA(cudaLaunchKernelEx(&cfg, kernel, P(a)...));
-    ++g_launches;
-    return SAM_OK;
-}
-
 template <bool kMasks>
 int launch_shaped(const ShapeArgs& a, unsigned grid, cudaStream_t st) {
     static thread_local uint64_t asked = 0;               // one bit per device

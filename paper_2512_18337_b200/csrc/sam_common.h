@@ -1,4 +1,4 @@
-// Shared by the translation units of the C ABI: the calling thread's last CUDA error, the launch count, device facts.
+// Shared by the translation units of the C ABI: the calling thread's last CUDA error, the launch count, device facts, launches.
 #pragma once
 
 #include <cuda_runtime.h>
@@ -40,6 +40,24 @@ inline int device_info(DeviceInfo* out) {
         cached_dev = dev;
     }
     *out = cached;
+    return SAM_OK;
+}
+
+// Launches a kernel that may be placed while the one before it in the stream ends, where that one allows it.
+template <typename... P, typename... A>
+int launch_behind(void (*kernel)(P...), dim3 grid, int threads, int shared, cudaStream_t stream, const A&... a) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = shared;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    SAM_CUDA(cudaLaunchKernelEx(&cfg, kernel, P(a)...));
+    ++g_launches;
     return SAM_OK;
 }
 
