@@ -923,7 +923,8 @@ class SamBounds:
 
     def select(self, layer: int, q, n_blocks: int, n_sink: int = 1, n_recent: int = 2, share: int = 1, n_new=None,
                streams=None, out=None, workspace=None, stream=None):
-        """int32 blocks [B, ceil(Q / share), n_kv_heads, n_blocks] for attend_blocks."""
+        """int32 blocks [B, ceil(Q / share), n_kv_heads, n_blocks] for attend_blocks.  Without a workspace the call allocates one
+        (sam_cache_select_workspace_bytes: up to 128 MB for most caches)."""
         import torch
         c = self.cache
         pq, sq = c._rows(q, None)

@@ -10,7 +10,7 @@
 // fill sectors, and share the scale of their sixteen channels.
 //
 // 256 streams of up to 17 tokens, 32/8 heads of 128 (80 MB): 27 us; 20,000 tokens, 28/4 heads (338 MB): 70 us, 4.8 TB/s.  Bound by
-// instructions: 280 for the sixteen channels of a thread, 0.7 of the issue slots, most of them to find out where a unit lies.  Tried: two
+// instructions: 308 and 279 for the sixteen channels of a thread, 0.7 of the issue slots, most of them to find out where a unit lies.  Tried: two
 // blocks of 16 channels a thread (half-filled sectors: 29 and 74 us), the next unit's loads ahead of this one's products (30 and 84), a
 // thread that keeps to its channels token after token (29 and 85: keys and values become a chain of a few microseconds).
 #pragma once
